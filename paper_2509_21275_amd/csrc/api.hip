@@ -11,6 +11,7 @@
 #include <string>
 
 #include "kernels.hpp"
+#include "operators.hpp"
 
 using namespace chunk_attn;
 
@@ -25,6 +26,12 @@ int hip_fail(hipError_t e, const char* what) {
   g_last_hip_error = std::string(what) + ": " + hipGetErrorString(e);
   return CHUNK_ATTN_HIP_ERROR;
 }
+
+}  // namespace
+
+int chunk_attn::report_hip(hipError_t e, const char* what) { return hip_fail(e, what); }
+
+namespace {
 
 // Schedules reach the device as kernel arguments where they are small (the forward's items with the forward itself, the backward's
 // blob with its pre-pass, a forward blob with a launch of its own), else through pinned staging buffers.
