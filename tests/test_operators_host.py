@@ -21,10 +21,11 @@ def ca():
 
 def test_library_exports_what_the_headers_declare(ca):
     names = set()
-    for h in ("chunk_rope.h", "fused_norm.h"):
+    for h in ("chunk_rope.h", "fused_norm.h", "chunk_linear.h"):
         text = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", h)).read(), flags=re.S)
-        names |= set(re.findall(r"\bint ((?:chunk_rope|fused_norm)_[a-z0-9_]+)\s*\(", text))
-    assert {"chunk_rope_frequencies", "chunk_rope_fwd", "chunk_rope_bwd", "fused_norm_fwd", "fused_norm_bwd", "fused_norm_bwd_workspace_bytes"} == names
+        names |= set(re.findall(r"\bint ((?:chunk_rope|fused_norm|chunk_linear)_[a-z0-9_]+)\s*\(", text))
+    assert {"chunk_rope_frequencies", "chunk_rope_fwd", "chunk_rope_bwd", "fused_norm_fwd", "fused_norm_bwd", "fused_norm_bwd_workspace_bytes",
+            "chunk_linear_validate", "chunk_linear_workspace_bytes", "chunk_linear_fwd", "chunk_linear_bwd", "chunk_linear_step"} == names
     lib = ctypes.CDLL(ca.LIB_PATH)
     assert all(hasattr(lib, n) for n in names)
 
@@ -123,3 +124,51 @@ def test_norm_refusals(ca):
     assert e.value.code == ca.UNSUPPORTED
     with pytest.raises(ValueError):
         fn.fused_norm_fwd(None, None, None, None, None, None, None)
+
+
+def test_linear_refusals(ca):
+    from paper_2509_21275_amd import chunk_linear as cl
+    cl._bind()
+    lib, P = ca._lib, 1 << 20
+
+    def desc(segs=((0, 8, -1, -1),), H=4, Hk=2, d=64, total=8, states=2, scale=0.1):
+        return cl.make_desc(segs, H, Hk, d, total, states, scale)
+
+    ok = [((0, 8, -1, -1),), ((1, 2, 0, 1), (5, 3, 0, 0)), ((0, 1, -1, -1), (1, 1, -1, -1))]
+    assert all(cl.chunk_linear_validate(desc(s)) == ca.OK for s in ok)
+    for kw in (dict(H=0), dict(Hk=0), dict(total=0), dict(states=-1), dict(scale=0.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(segs=())):
+        assert cl.chunk_linear_validate(desc(**kw)) == ca.INVALID_ARG, kw
+    for kw in (dict(d=80), dict(d=32), dict(H=3)):
+        assert cl.chunk_linear_validate(desc(**kw)) == ca.UNSUPPORTED, kw
+    for segs in (((0, 0, -1, -1),), ((0, 9, -1, -1),), ((-1, 3, -1, -1),), ((0, 4, -1, -1), (3, 2, -1, -1)), ((4, 2, -1, -1), (0, 2, -1, -1)), ((0, 8, 2, -1),),
+                 ((0, 8, -2, -1),), ((0, 8, -1, 2),), ((0, 4, -1, 1), (4, 4, -1, 1)), ((1, 2**31 - 1, -1, -1),)):
+        assert cl.chunk_linear_validate(desc(segs)) == ca.BAD_SEGMENT, segs
+    assert lib.chunk_linear_validate(None) == ca.INVALID_ARG
+
+    def fwd(d, q=P, lg=P, s_in=P, o=P, s_out=2 * P, ws=P, size=1 << 40):
+        return lib.chunk_linear_fwd(ctypes.byref(d), q, P, P, lg, s_in, o, s_out, ws, size, None)
+
+    def bwd(d, q=P, s_in=P, ds_out=3 * P, dv=P, ds_in=2 * P, ws=P, size=1 << 40):
+        return lib.chunk_linear_bwd(ctypes.byref(d), q, P, P, P, s_in, P, ds_out, P, P, dv, ds_in, ws, size, None)
+
+    one, long = desc(((0, 8, 0, 1),)), desc(((0, 5000, 0, 1),), total=5000)
+    f, b = cl.chunk_linear_workspace_bytes(long)
+    assert f > 0 and b == 2 * f and cl.chunk_linear_workspace_bytes(one) == (0, 0)
+    for kw in (dict(q=None), dict(q=P + 8), dict(lg=None), dict(lg=P + 2), dict(o=None), dict(s_in=None), dict(s_out=None), dict(s_in=P + 4)):
+        assert fwd(one, **kw) == ca.INVALID_ARG, kw
+    for kw in (dict(q=None), dict(dv=P + 2), dict(s_in=None), dict(ds_in=P + 8)):
+        assert bwd(one, **kw) == ca.INVALID_ARG, kw
+    for call, size in ((fwd, f), (bwd, b)):
+        assert call(long, ws=None) == ca.INVALID_ARG and call(long, ws=P + 128) == ca.INVALID_ARG
+        assert call(long, size=size - 1) == ca.WORKSPACE_TOO_SMALL
+    # slots in place: one segment's state_out may not be another's state_in; and a gradient goes to one place only
+    crossed, shared = desc(((0, 4, 0, 1), (4, 4, 1, -1))), desc(((0, 4, 0, -1), (4, 4, 0, 1)))
+    assert fwd(crossed, s_out=P) == ca.BAD_SEGMENT and bwd(crossed, ds_in=3 * P) == ca.BAD_SEGMENT and bwd(shared) == ca.BAD_SEGMENT
+
+    def step(B=4, H=4, Hk=2, d=64, q=P, s_in=P, s_out=P, n=4, slots=P, o=P, scale=0.1):
+        return lib.chunk_linear_step(B, H, Hk, d, q, P, P, P, s_in, s_out, n, slots, o, scale, None)
+
+    for kw in (dict(B=-1), dict(H=0), dict(n=-1), dict(scale=float("nan")), dict(scale=-1.0), dict(q=None), dict(s_in=None), dict(s_out=P + 4), dict(slots=P + 2),
+               dict(slots=None), dict(o=P + 2), dict(B=2**31 - 1)):
+        assert step(**kw) == ca.INVALID_ARG, kw
+    assert step(d=80) == ca.UNSUPPORTED and step(H=3) == ca.UNSUPPORTED and step(B=0) == ca.OK
