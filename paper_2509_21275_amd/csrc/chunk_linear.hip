@@ -80,35 +80,55 @@ __device__ __forceinline__ Piece find_piece(const LinearSegs& s, int piece) {
 __device__ __forceinline__ float log2_decay(const float* log_decay, int h) { return fmaxf((float)((double)log_decay[h] * 1.4426950408889634), -1000.f); }
 __device__ __forceinline__ float power(float lg, int n) { return __builtin_amdgcn_exp2f(lg * (float)n); }
 
-// A block's rows of one head into LDS: 64 rows of D, 16-byte chunks swizzled as tile_elem has it; zeros behind `rows`.
+// Tiles in LDS are rows of D elements and a few more, so that an element's place is linear in its row and column (one address per lane and kind of read, the rest are constants) and neither 16-byte
+// reads of 16 consecutive rows nor transposed reads of 4 rows x 32 bytes meet in a bank: the rows' stride in 16-byte units is odd, and 1 mod 16 apart.
+constexpr int pitch(int cols) { return cols + (cols % 128 == 0 ? 24 : 8); }
+constexpr size_t tile_bytes(int cols) { return (size_t)kBlock * pitch(cols) * 2; }
+
+// A block's rows of one head on their way to LDS, fetched ahead into registers.  Forwards a block of fewer rows stands at the end of its 64, behind `empty` rows of zeros: the weights of rows in
+// the state are then the same in every block.
 template <int D>
-__device__ __forceinline__ void load_tile(const __bf16* from, int64_t stride, int rows, lds_bf16* to) {
-  constexpr int kChunks = D / 8, kThreads = 2 * D;
+struct Tile {
+  static constexpr int kChunks = D / 8, kThreads = 2 * D, kEach = kBlock * kChunks / kThreads, kRowsApart = kThreads / kChunks;
+  bf16x8 x[kEach];
+  // rows empty .. empty + rows - 1 from `from` on, `stride` bytes apart; the others are zeros
+  __device__ __forceinline__ void fetch(const __bf16* from, unsigned stride, int empty, int rows) {
+    const int row0 = (int)threadIdx.x / kChunks, c = (int)threadIdx.x % kChunks;
+    const char* const base = reinterpret_cast<const char*>(from);
+    if (rows == kBlock) {
 #pragma unroll
-  for (int i = 0; i < kBlock * kChunks / kThreads; ++i) {
-    const int at = i * kThreads + (int)threadIdx.x, row = at / kChunks, c = at % kChunks;
-    bf16x8 x{};
-    if (row < rows) x = *reinterpret_cast<const bf16x8*>(from + row * stride + c * 8);
-    lds_store8(to + tile_elem<kChunks>(row, c), x);
+      for (int i = 0; i < kEach; ++i) x[i] = *reinterpret_cast<const bf16x8*>(base + (unsigned)((row0 + i * kRowsApart) * stride + c * 16));
+    } else {
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        const int row = row0 + i * kRowsApart - empty;
+        x[i] = bf16x8{};
+        if (row >= 0 && row < rows) x[i] = *reinterpret_cast<const bf16x8*>(base + (unsigned)(row * stride + c * 16));
+      }
+    }
   }
-}
+  __device__ __forceinline__ void store(lds_bf16* to) const {
+    lds_bf16* const at = to + (int)threadIdx.x / kChunks * pitch(D) + (int)threadIdx.x % kChunks * 8;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) lds_store8(at + i * kRowsApart * pitch(D), x[i]);
+  }
+};
 // Operand of 32 rows (or columns) x 16 of the contraction along the row: lane l32 holds row0 + l32, eight elements from 16 step + 8 hh on.
 template <int D>
 __device__ __forceinline__ bf16x8 row_operand(const lds_bf16* tile, int row0, int step, int lane) {
-  return lds_load8(tile + tile_elem<D / 8>(row0 + (lane & 31), 2 * step + (lane >> 5)));
+  return lds_load8(tile + ((lane & 31) * pitch(D) + (lane >> 5) * 8) + (row0 * pitch(D) + 16 * step));
 }
 // Operand of 32 columns from col0 on x 16 rows from row0 on as the contraction.  SWAPPED: the column quads of each 16 in the order 0, 2, 1, 3.
 template <int D, bool SWAPPED>
 __device__ __forceinline__ bf16x8 column_operand(const lds_bf16* tile, int row0, int col0, int lane) {
   const int x = lane & 15, quad = x & 3;
-  const int col = col0 + (lane & 16) + 4 * (SWAPPED ? (quad >> 1) | (quad & 1) << 1 : quad);
-  const int row = row0 + 8 * (lane >> 5) + (x >> 2);
+  const lds_bf16* const at = tile + ((8 * (lane >> 5) + (x >> 2)) * pitch(D) + (lane & 16) + 4 * (SWAPPED ? (quad >> 1) | (quad & 1) << 1 : quad)) + (row0 * pitch(D) + col0);
   union {
     s16x4 half[2];
     bf16x8 all;
   } u;
-  u.half[0] = lds_read_tr(tile + tile_elem<D / 8>(row, col >> 3) + (col & 7));
-  u.half[1] = lds_read_tr(tile + tile_elem<D / 8>(row + 4, col >> 3) + (col & 7));
+  u.half[0] = lds_read_tr(at);
+  u.half[1] = lds_read_tr(at + 4 * pitch(D));
   return u.all;
 }
 
@@ -157,12 +177,12 @@ struct State {
     const int o = 8 * (step & 1);
     return pack8(a[o], a[o + 1], a[o + 2], a[o + 3], a[o + 4], a[o + 5], a[o + 6], a[o + 7]);
   }
-  // adds k^T (w v) of 16 rows from row0 on: v's operand as it was read, w the rows' weights
-  __device__ __forceinline__ void add(const lds_bf16* k_tile, int row0, bf16x8 v, const float (&w)[8], int lane) {
+  // adds k^T (w v) of 16 rows from row0 on: v's operand as it was read; element e's row weighs lead * base[e]
+  __device__ __forceinline__ void add(const lds_bf16* k_tile, int row0, bf16x8 v, float lead, const float (&base)[8], int lane) {
     bf16x8 part[3];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      float x = (float)v[e] * w[e];
+      float x = (float)v[e] * (lead * base[e]);
       part[0][e] = (__bf16)x;
       x -= (float)part[0][e];
       part[1][e] = (__bf16)x;
@@ -178,48 +198,52 @@ struct State {
   }
 };
 
-// Weights of a block's rows in its state: rows 16 s + 8 hh + e.
+// Weights of a block's rows in its state, l^(63 - j) or backwards l^(j + 1) for row j = 16 s + 8 hh + e: lead[s] * base[e], both powers with exponents >= 0.
 template <bool REVERSE>
-__device__ __forceinline__ void state_weights(float lg, int s, int rows, int hh, float (&w)[8]) {
+struct StateWeights {
+  float base[8], lead[4];
+  __device__ __forceinline__ StateWeights(float lg, int hh) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const int j = 16 * s + 8 * hh + e;
-    w[e] = power(lg, REVERSE ? j + 1 : max(rows - 1 - j, 0));
+    for (int e = 0; e < 8; ++e) base[e] = power(lg, REVERSE ? e : 7 - e);
+#pragma unroll
+    for (int s = 0; s < 4; ++s) lead[s] = power(lg, REVERSE ? 16 * s + 8 * hh + 1 : 56 - 16 * s - 8 * hh);
   }
-}
+};
 
 // Each piece's own k^T v into its place in the workspace, but for the one at the far end of its sequence, whose nobody needs, and for sequences of one piece.
 template <int D, bool REVERSE>
-__global__ __launch_bounds__(2 * D) void piece_states_kernel(const WalkArgs a, const LinearSegs segs) {
+__global__ __launch_bounds__(2 * D, 2) void piece_states_kernel(const WalkArgs a, const LinearSegs segs) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   lds_bf16* const ks = (lds_bf16*)smem;
-  lds_bf16* const vs = ks + kBlock * D;
+  lds_bf16* const vs = ks + kBlock * pitch(D);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, hh = lane >> 5;
   const int h = blockIdx.x % a.heads;
   const Piece p = find_piece(segs, blockIdx.x / a.heads);
   if (p.index == (REVERSE ? 0 : p.pieces - 1)) return;
   const float lg = log2_decay(a.log_decay, h);
-  const int group = REVERSE ? a.group : 1, heads = a.heads * group;
-  const int64_t stride = (int64_t)heads * D;
+  const int group = REVERSE ? a.group : 1;
+  const int64_t stride = (int64_t)a.heads * group * D;
+  const StateWeights<REVERSE> weights(lg, hh);
   State<D> s;
   s.clear();
-  const int blocks = (p.rows + kBlock - 1) / kBlock;
-  for (int n = 0; n < blocks; ++n) {
-    const int b = REVERSE ? blocks - 1 - n : n, rows = min(kBlock, p.rows - b * kBlock);
-    s.scale(power(lg, rows));
-    for (int g = 0; g < group; ++g) {
-      const int64_t at = (int64_t)(p.row + b * kBlock) * stride + (h * group + g) * D;
-      __syncthreads();
-      load_tile<D>(a.k + at, stride, rows, ks);
-      load_tile<D>(a.v + at, stride, rows, vs);
-      __syncthreads();
+  const int blocks = (p.rows + kBlock - 1) / kBlock, steps = blocks * group;
+  Tile<D> kt, vt;
+  auto fetch = [&](int step) {
+    const int b = REVERSE ? blocks - 1 - step / group : step / group, g = step % group, rows = min(kBlock, p.rows - b * kBlock);
+    const int64_t at = (int64_t)(p.row + b * kBlock) * stride + (h * group + g) * D;
+    kt.fetch(a.k + at, (unsigned)stride * 2, REVERSE ? 0 : kBlock - rows, rows);
+    vt.fetch(a.v + at, (unsigned)stride * 2, REVERSE ? 0 : kBlock - rows, rows);
+  };
+  fetch(0);
+  for (int step = 0; step < steps; ++step) {
+    __syncthreads();
+    kt.store(ks);
+    vt.store(vs);
+    __syncthreads();
+    if (step + 1 < steps) fetch(step + 1);
+    if (step % group == 0) s.scale(power(lg, min(kBlock, p.rows - (REVERSE ? blocks - 1 - step / group : step / group) * kBlock)));
 #pragma unroll
-      for (int st = 0; st < 4; ++st) {
-        float w[8];
-        state_weights<REVERSE>(lg, st, rows, hh, w);
-        s.add(ks, 16 * st, column_operand<D, false>(vs, 16 * st, 32 * wave, lane), w, lane);
-      }
-    }
+    for (int st = 0; st < 4; ++st) s.add(ks, 16 * st, column_operand<D, false>(vs, 16 * st, 32 * wave, lane), weights.lead[st], weights.base, lane);
   }
   s.store(a.inner + ((int64_t)(segs.place0[p.seg] + p.index) * a.heads + h) * D * D, 32 * wave + (lane & 31), hh, 1.f);
 }
@@ -247,21 +271,59 @@ __global__ __launch_bounds__(256) void join_states_kernel(const WalkArgs a, cons
   }
 }
 
-// The walk.  Forwards a workgroup takes all query heads of its key/value head (MANY of q and o to one k, v); backwards all of them stand in the roles of k and v.
+// Four neighbouring elements of a row from either half of the wave (registers 4 g .. 4 g + 3 of an output tile are elements 8 g + 4 hh ..): stored as 16 bytes, the lower half
+// of the lanes takes those of an even g, the upper one those of the odd g behind it.
+__device__ __forceinline__ void store_row(__bf16* row, const f32x16& o, float by, int hh, bool live) {
+#pragma unroll
+  for (int g = 0; g < 4; g += 2) {
+    union {
+      bf16x4 h;
+      unsigned u[2];
+    } even, odd;
+    even.h = pack4(o[4 * g] * by, o[4 * g + 1] * by, o[4 * g + 2] * by, o[4 * g + 3] * by);
+    odd.h = pack4(o[4 * g + 4] * by, o[4 * g + 5] * by, o[4 * g + 6] * by, o[4 * g + 7] * by);
+    const u32x2 x = __builtin_amdgcn_permlane32_swap(even.u[0], odd.u[0], false, false), y = __builtin_amdgcn_permlane32_swap(even.u[1], odd.u[1], false, false);
+    if (live) *reinterpret_cast<u32x4*>(row + 8 * (g + hh)) = u32x4{x[0], y[0], x[1], y[1]};
+  }
+}
+
+// The walk.  Forwards a workgroup takes all query heads of its key/value head, one after the other in each block; backwards all of them stand in the roles of k and v.
+// The next step's rows are fetched while this one's products run; two workgroups share a compute unit (head_dim 128: 56 KB of LDS and at most 256 registers each).
 template <int D, bool REVERSE, bool TRANSPOSED>
-__global__ __launch_bounds__(2 * D) void walk_kernel(const WalkArgs a, const LinearSegs segs) {
+__global__ __launch_bounds__(2 * D, 2) void walk_kernel(const WalkArgs a, const LinearSegs segs) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   lds_bf16* const qs = (lds_bf16*)smem;
-  lds_bf16* const ks = qs + kBlock * D;
-  lds_bf16* const vs = ks + kBlock * D;
-  lds_bf16* const ps = vs + kBlock * D;  // weighted scores, [row][64]
+  lds_bf16* const ks = qs + kBlock * pitch(D);
+  lds_bf16* const vs = ks + kBlock * pitch(D);
+  lds_bf16* const ps = vs + kBlock * pitch(D);  // weighted scores, 64 x 64
   constexpr int kWaves = D / 32;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, hh = lane >> 5, l32 = lane & 31;
   const int h = blockIdx.x % a.heads;
   const Piece p = find_piece(segs, blockIdx.x / a.heads);
   const float lg = log2_decay(a.log_decay, h);
-  const int q_group = REVERSE ? 1 : a.group, kv_group = REVERSE ? a.group : 1;
+  const int group = a.group, q_group = REVERSE ? 1 : group, kv_group = REVERSE ? group : 1;
   const int64_t q_stride = (int64_t)a.heads * q_group * D, kv_stride = (int64_t)a.heads * kv_group * D;
+  const int blocks = (p.rows + kBlock - 1) / kBlock;
+
+  struct Step {  // one block and one query head
+    int g, rows, empty;
+    int64_t row0;
+  };
+  auto step_of = [&](int n, int g) {
+    const int b = REVERSE ? blocks - 1 - n : n, rows = min(kBlock, p.rows - b * kBlock);
+    return Step{g, rows, REVERSE ? 0 : kBlock - rows, (int64_t)p.row + b * kBlock};
+  };
+  Tile<D> qt, kt, vt;
+  auto fetch = [&](const Step& x) {
+    if (!REVERSE || x.g == 0) qt.fetch(a.q + x.row0 * q_stride + (h * q_group + (REVERSE ? 0 : x.g)) * D, (unsigned)q_stride * 2, x.empty, x.rows);
+    if (REVERSE || x.g == 0) {
+      const int64_t at = x.row0 * kv_stride + (h * kv_group + (REVERSE ? x.g : 0)) * D;
+      kt.fetch(a.k + at, (unsigned)kv_stride * 2, x.empty, x.rows);
+      vt.fetch(a.v + at, (unsigned)kv_stride * 2, x.empty, x.rows);
+    }
+  };
+  Step now = step_of(0, 0);
+  fetch(now);
 
   const int col = 32 * wave + l32;
   State<D> s;
@@ -270,86 +332,80 @@ __global__ __launch_bounds__(2 * D) void walk_kernel(const WalkArgs a, const Lin
   else if (a.first && from >= 0) s.template load<TRANSPOSED>(a.first + ((int64_t)from * a.heads + h) * D * D, col, hh, a.first_scale);
   else s.clear();
 
-  const int blocks = (p.rows + kBlock - 1) / kBlock;
+  const StateWeights<REVERSE> weights(lg, hh);
+  // Scores are taken in tiles of 32 x 32, 0: (0, 0), 1: the one off the diagonal, 2: (1, 1); a wave's tiles have the same distances (with two waves the first takes 0 and 2).
+  float near[16];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    const int j = 8 * (e >> 2) + 4 * hh + (e & 3), far = (REVERSE ? j - l32 : l32 - j) + (wave == 1 ? 32 : 0);
+    near[e] = far >= 0 ? power(lg, far) : 0.f;
+  }
+
+  f32x16 o[2];
   for (int n = 0; n < blocks; ++n) {
-    const int b = REVERSE ? blocks - 1 - n : n, rows = min(kBlock, p.rows - b * kBlock);
-    const int64_t row0 = p.row + b * kBlock;
-    f32x16 o[2];
-    bf16x8 vt[4];
-    for (int g = 0; g < a.group; ++g) {  // forwards over the query heads, backwards over what they hand to the key/value head
-      const bool new_q = !REVERSE || g == 0, new_kv = REVERSE || g == 0;
+    for (int g = 0; g < group; ++g) {
+      const bool last = g == group - 1;
       __syncthreads();
-      if (new_q) load_tile<D>(a.q + row0 * q_stride + (h * q_group + (REVERSE ? 0 : g)) * D, q_stride, rows, qs);
-      if (new_kv) {
-        const int64_t at = row0 * kv_stride + (h * kv_group + (REVERSE ? g : 0)) * D;
-        load_tile<D>(a.k + at, kv_stride, rows, ks);
-        load_tile<D>(a.v + at, kv_stride, rows, vs);
+      if (!REVERSE || g == 0) qt.store(qs);
+      if (REVERSE || g == 0) {
+        kt.store(ks);
+        vt.store(vs);
       }
       __syncthreads();
-      // scores of 32 x 32, transposed (lane: one row i, four columns j at a time), weighted, to LDS; tiles with j <= i (backwards j >= i)
+      const Step x = now;
+      if (!last || n + 1 < blocks) {
+        now = step_of(last ? n + 1 : n, last ? 0 : g + 1);
+        fetch(now);
+      }
+      // scores, transposed (a lane: one row i, four columns j at a time), weighted, to LDS; only tiles with j <= i (backwards j >= i)
       for (int tile = wave; tile < 3; tile += kWaves) {
         const int ti = REVERSE ? tile >> 1 : (tile + 1) >> 1, tj = REVERSE ? (tile + 1) >> 1 : tile >> 1;
         f32x16 c{};
 #pragma unroll
         for (int st = 0; st < D / 16; ++st) c = mfma32(row_operand<D>(ks, 32 * tj, st, lane), row_operand<D>(qs, 32 * ti, st, lane), c);
-        const int i = 32 * ti + l32;
 #pragma unroll
-        for (int q4 = 0; q4 < 4; ++q4) {
-          bf16x4 x;
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int j = 32 * tj + 8 * q4 + 4 * hh + r, far = REVERSE ? j - i : i - j;
-            x[r] = (__bf16)(far >= 0 ? c[4 * q4 + r] * power(lg, max(far, 0)) : 0.f);
-          }
-          *(__attribute__((address_space(3))) bf16x4*)(ps + tile_elem<8>(i, 4 * tj + q4) + 4 * hh) = x;
-        }
+        for (int q4 = 0; q4 < 4; ++q4)
+          *(__attribute__((address_space(3))) bf16x4*)(ps + (l32 * pitch(64) + 4 * hh) + (32 * ti * pitch(64) + 32 * tj + 8 * q4)) =
+              pack4(c[4 * q4] * near[4 * q4], c[4 * q4 + 1] * near[4 * q4 + 1], c[4 * q4 + 2] * near[4 * q4 + 2], c[4 * q4 + 3] * near[4 * q4 + 3]);
       }
-      __syncthreads();
-      if (new_q) {
+      if (!REVERSE || g == 0) {  // what the state gives
+        o[0] = f32x16{};
+        o[1] = f32x16{};
+#pragma unroll
+        for (int st = 0; st < D / 16; ++st) {
+          const bf16x8 sb = s.operand(st);
+#pragma unroll
+          for (int ti = 0; ti < 2; ++ti) o[ti] = mfma32(sb, row_operand<D>(qs, 32 * ti, st, lane), o[ti]);
+        }
 #pragma unroll
         for (int ti = 0; ti < 2; ++ti) {
-          o[ti] = f32x16{};
-#pragma unroll
-          for (int st = 0; st < D / 16; ++st) o[ti] = mfma32(s.operand(st), row_operand<D>(qs, 32 * ti, st, lane), o[ti]);
-          const int i = 32 * ti + l32;
-          const float by = power(lg, REVERSE ? max(rows - 1 - i, 0) : i + 1);
+          const int i = 32 * ti + l32 - x.empty;
+          const float by = power(lg, max(REVERSE ? x.rows - 1 - i : i + 1, 0));
 #pragma unroll
           for (int e = 0; e < 16; ++e) o[ti][e] *= by;
         }
       }
-      if (new_kv) {
+      __syncthreads();
+      if (REVERSE ? g == 0 : last) s.scale(power(lg, x.rows));
 #pragma unroll
-        for (int st = 0; st < 4; ++st) vt[st] = column_operand<D, false>(vs, 16 * st, 32 * wave, lane);
+      for (int st = 0; st < 4; ++st) {
+        const bf16x8 vop = column_operand<D, false>(vs, 16 * st, 32 * wave, lane);
+#pragma unroll
+        for (int ti = 0; ti < 2; ++ti)
+          if (REVERSE ? st >= 2 * ti : st < 2 * ti + 2) o[ti] = mfma32(vop, row_operand<64>(ps, 32 * ti, st, lane), o[ti]);
+        if (REVERSE || last) s.add(ks, 16 * st, vop, weights.lead[st], weights.base, lane);
       }
-#pragma unroll
-      for (int ti = 0; ti < 2; ++ti)
-#pragma unroll
-        for (int st = REVERSE ? 2 * ti : 0; st < (REVERSE ? 4 : 2 * ti + 2); ++st) o[ti] = mfma32(vt[st], row_operand<64>(ps, 32 * ti, st, lane), o[ti]);
-      if (g == (REVERSE ? a.group - 1 : g)) {
+      if (!REVERSE || last) {
 #pragma unroll
         for (int ti = 0; ti < 2; ++ti) {
-          const int i = 32 * ti + l32;
-          if (i < rows) {
-            __bf16* const to = a.o + (row0 + i) * q_stride + (h * q_group + (REVERSE ? 0 : g)) * D + 32 * wave + 4 * hh;
-#pragma unroll
-            for (int q4 = 0; q4 < 4; ++q4)
-              *reinterpret_cast<bf16x4*>(to + 8 * q4) = pack4(o[ti][4 * q4] * a.scale, o[ti][4 * q4 + 1] * a.scale, o[ti][4 * q4 + 2] * a.scale, o[ti][4 * q4 + 3] * a.scale);
-          }
-        }
-      }
-      if (g == (REVERSE ? 0 : a.group - 1)) s.scale(power(lg, rows));
-      if (REVERSE || g == a.group - 1) {
-#pragma unroll
-        for (int st = 0; st < 4; ++st) {
-          float w[8];
-          state_weights<REVERSE>(lg, st, rows, hh, w);
-          s.add(ks, 16 * st, vt[st], w, lane);
+          const int i = 32 * ti + l32 - x.empty;
+          store_row(a.o + (x.row0 + i) * q_stride + (h * q_group + (REVERSE ? 0 : g)) * D + 32 * wave, o[ti], a.scale, hh, i >= 0 && i < x.rows);
         }
       }
     }
   }
-  const int slot = REVERSE ? segs.in[p.seg] : segs.out[p.seg];
-  if (a.last && slot >= 0 && p.index == (REVERSE ? 0 : p.pieces - 1)) s.store(a.last + ((int64_t)slot * a.heads + h) * D * D, col, hh, a.last_scale);
+  const int to = REVERSE ? segs.in[p.seg] : segs.out[p.seg];
+  if (a.last && to >= 0 && p.index == (REVERSE ? 0 : p.pieces - 1)) s.store(a.last + ((int64_t)to * a.heads + h) * D * D, col, hh, a.last_scale);
 }
 
 // ---- one token ----
@@ -523,7 +579,7 @@ hipError_t by_dim(int d, F&& f) {
 
 template <int D, bool REVERSE>
 hipError_t launch_piece_states(const WalkArgs& a, const LinearSegs& segs, hipStream_t stream) {
-  constexpr size_t smem = 2 * kBlock * D * 2;
+  constexpr size_t smem = 2 * tile_bytes(D);
   static const hipError_t attr =
       hipFuncSetAttribute(reinterpret_cast<const void*>(&piece_states_kernel<D, REVERSE>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (attr != hipSuccess) return attr;
@@ -533,7 +589,7 @@ hipError_t launch_piece_states(const WalkArgs& a, const LinearSegs& segs, hipStr
 }
 template <int D, bool REVERSE, bool TRANSPOSED>
 hipError_t launch_walk(const WalkArgs& a, const LinearSegs& segs, hipStream_t stream) {
-  constexpr size_t smem = 3 * kBlock * D * 2 + kBlock * kBlock * 2;
+  constexpr size_t smem = 3 * tile_bytes(D) + tile_bytes(kBlock);
   static const hipError_t attr =
       hipFuncSetAttribute(reinterpret_cast<const void*>(&walk_kernel<D, REVERSE, TRANSPOSED>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (attr != hipSuccess) return attr;
