@@ -34,6 +34,8 @@
 extern "C" {
 #endif
 
+#define CHUNK_LINEAR_MAX_HEADS 16384
+
 /* One sequence, or a slice of one: rows start .. start + len - 1; state_in: slot of the state before its first token (-1: zeros); state_out: slot that
  * takes the state behind its last token (-1: not wanted). */
 typedef struct {
@@ -41,7 +43,7 @@ typedef struct {
 } chunk_linear_seg;
 
 typedef struct {
-  int32_t num_q_heads;  /* > 0 */
+  int32_t num_q_heads;  /* 1 .. CHUNK_LINEAR_MAX_HEADS, else CHUNK_ATTN_UNSUPPORTED */
   int32_t num_kv_heads; /* > 0, divides num_q_heads */
   int32_t head_dim;     /* 64, 96, 128 or 256 */
   int32_t total;        /* rows of the tensors */

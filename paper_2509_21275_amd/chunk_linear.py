@@ -4,7 +4,7 @@ from __future__ import annotations
 import ctypes
 
 from . import ChunkAttnError, _lib
-from ._args import call, whole
+from ._args import BF16, F32, I32, call, room, torch, whole
 
 _bound = False
 
@@ -60,7 +60,6 @@ def chunk_linear_workspace_bytes(desc):
 
 def alloc_workspace(desc, device="cuda"):
     """A uint8 tensor large enough for both chunk_linear_fwd and chunk_linear_bwd on this descriptor."""
-    import torch
     return torch.empty(max(*chunk_linear_workspace_bytes(desc), 256), dtype=torch.uint8, device=device)
 
 
@@ -69,45 +68,34 @@ def _shapes(desc):
     return (desc.total, desc.num_q_heads, d), (desc.total, Hk, d), (Hk,), (desc.num_states, Hk, d, d)
 
 
-def _room(workspace):
-    import torch
-    return whole(workspace, (torch.uint8,), (None,), "workspace"), 0 if workspace is None else workspace.nbytes
-
-
 def chunk_linear_fwd(desc, q, k, v, log_decay, states_in, o, states_out, workspace, stream=None) -> None:
     """Writes o [total, num_q_heads, head_dim] and the states that segments leave in states_out [num_states, num_kv_heads, head_dim, head_dim]; states_in and
     states_out may be None where no segment names a slot, or the same tensor."""
-    import torch
-    bf16, f32 = (torch.bfloat16,), (torch.float32,)
     qs, ks, hs, ss = _shapes(desc)
-    call(_lib.chunk_linear_fwd, (q, k, v, log_decay, states_in, o, states_out, workspace), stream, ctypes.byref(desc), whole(q, bf16, qs, "q"), whole(k, bf16, ks, "k"),
-         whole(v, bf16, ks, "v"), whole(log_decay, f32, hs, "log_decay"), whole(states_in, f32, ss, "states_in"), whole(o, bf16, qs, "o"),
-         whole(states_out, f32, ss, "states_out"), *_room(workspace))
+    call(_lib.chunk_linear_fwd, (q, k, v, log_decay, states_in, o, states_out, workspace), stream, ctypes.byref(desc), whole(q, BF16, qs, "q"), whole(k, BF16, ks, "k"),
+         whole(v, BF16, ks, "v"), whole(log_decay, F32, hs, "log_decay"), whole(states_in, F32, ss, "states_in"), whole(o, BF16, qs, "o"),
+         whole(states_out, F32, ss, "states_out"), *room(workspace))
 
 
 def chunk_linear_bwd(desc, q, k, v, log_decay, states_in, d_o, d_states_out, dq, dk, dv, d_states_in, workspace, stream=None) -> None:
     """Writes dq, dk, dv and, if it is given, d_states_in; d_states_out (gradients of the states left, None: zeros)."""
-    import torch
-    bf16, f32 = (torch.bfloat16,), (torch.float32,)
     qs, ks, hs, ss = _shapes(desc)
-    call(_lib.chunk_linear_bwd, (q, k, v, log_decay, states_in, d_o, d_states_out, dq, dk, dv, d_states_in, workspace), stream, ctypes.byref(desc), whole(q, bf16, qs, "q"),
-         whole(k, bf16, ks, "k"), whole(v, bf16, ks, "v"), whole(log_decay, f32, hs, "log_decay"), whole(states_in, f32, ss, "states_in"), whole(d_o, bf16, qs, "d_o"),
-         whole(d_states_out, f32, ss, "d_states_out"), whole(dq, bf16, qs, "dq"), whole(dk, bf16, ks, "dk"), whole(dv, bf16, ks, "dv"),
-         whole(d_states_in, f32, ss, "d_states_in"), *_room(workspace))
+    call(_lib.chunk_linear_bwd, (q, k, v, log_decay, states_in, d_o, d_states_out, dq, dk, dv, d_states_in, workspace), stream, ctypes.byref(desc), whole(q, BF16, qs, "q"),
+         whole(k, BF16, ks, "k"), whole(v, BF16, ks, "v"), whole(log_decay, F32, hs, "log_decay"), whole(states_in, F32, ss, "states_in"), whole(d_o, BF16, qs, "d_o"),
+         whole(d_states_out, F32, ss, "d_states_out"), whole(dq, BF16, qs, "dq"), whole(dk, BF16, ks, "dk"), whole(dv, BF16, ks, "dv"),
+         whole(d_states_in, F32, ss, "d_states_in"), *room(workspace))
 
 
 def chunk_linear_step(q, k, v, log_decay, states_in, states_out, slots, o, scale, stream=None) -> None:
     """One token for each of a batch: q, o [batch, num_q_heads, head_dim], k, v [batch, num_kv_heads, head_dim], slots int32 [batch] into states_in and states_out
     [num_states, num_kv_heads, head_dim, head_dim], which may be the same tensor."""
-    import torch
     if not _bound:
         _bind()
-    bf16, f32 = (torch.bfloat16,), (torch.float32,)
     if not (isinstance(q, torch.Tensor) and q.dim() == 3 and isinstance(k, torch.Tensor) and k.dim() == 3 and isinstance(states_in, torch.Tensor) and states_in.dim() == 4):
         raise ValueError("q, k, states_in: expected tensors of 3, 3 and 4 dimensions")
     B, H, d = q.shape
     Hk, n = k.shape[1], states_in.shape[0]
     ks, ss = (B, Hk, d), (n, Hk, d, d)
-    call(_lib.chunk_linear_step, (q, k, v, log_decay, states_in, states_out, slots, o), stream, B, H, Hk, d, whole(q, bf16, (B, H, d), "q"), whole(k, bf16, ks, "k"),
-         whole(v, bf16, ks, "v"), whole(log_decay, f32, (Hk,), "log_decay"), whole(states_in, f32, ss, "states_in"), whole(states_out, f32, ss, "states_out"), n,
-         whole(slots, (torch.int32,), (B,), "slots"), whole(o, bf16, (B, H, d), "o"), float(scale))
+    call(_lib.chunk_linear_step, (q, k, v, log_decay, states_in, states_out, slots, o), stream, B, H, Hk, d, whole(q, BF16, (B, H, d), "q"), whole(k, BF16, ks, "k"),
+         whole(v, BF16, ks, "v"), whole(log_decay, F32, (Hk,), "log_decay"), whole(states_in, F32, ss, "states_in"), whole(states_out, F32, ss, "states_out"), n,
+         whole(slots, I32, (B,), "slots"), whole(o, BF16, (B, H, d), "o"), float(scale))

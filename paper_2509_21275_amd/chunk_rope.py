@@ -4,7 +4,7 @@ from __future__ import annotations
 import ctypes
 
 from . import ChunkAttnError, Desc, _lib
-from ._args import call, rows
+from ._args import BF16, F32, call, rows
 
 SCALINGS = {"none": 0, "linear": 1, "base": 2, "ramp": 3}
 _bound = False
@@ -58,23 +58,21 @@ def make_rope(rotary_dim, base=10000.0, interleaved=False, scaling="none", facto
 def chunk_rope_fwd(desc, rope, q, k, q_out, k_out, stream=None) -> None:
     """q [total_q, num_q_heads, head_dim], k [total_q, num_kv_heads, head_dim] (rows may be strided) to q_out, of q's shape, and to the chunk's own rows
     of k_out [total_kv, num_kv_heads, head_dim].  Either pair may be None."""
-    import torch
     if not _bound:
         _bind()
-    bf16, d = (torch.bfloat16,), desc.head_dim
-    qs, ks, kvs = (desc.total_q, desc.num_q_heads, d), (desc.total_q, desc.num_kv_heads, d), (desc.total_kv, desc.num_kv_heads, d)
-    call(_lib.chunk_rope_fwd, (q, k, q_out, k_out), stream, ctypes.byref(desc), ctypes.byref(rope), *rows(q, bf16, qs, "q"), *rows(k, bf16, ks, "k"),
-         *rows(q_out, bf16, qs, "q_out"), *rows(k_out, bf16, kvs, "k_out"))
+    d, n, heads, inner = desc.head_dim, desc.total_q, desc.num_kv_heads, (desc.head_dim, 1)
+    qs = (n, desc.num_q_heads, d)
+    call(_lib.chunk_rope_fwd, (q, k, q_out, k_out), stream, ctypes.byref(desc), ctypes.byref(rope), *rows(q, BF16, qs, inner, "q"),
+         *rows(k, BF16, (n, heads, d), inner, "k"), *rows(q_out, BF16, qs, inner, "q_out"), *rows(k_out, BF16, (desc.total_kv, heads, d), inner, "k_out"))
 
 
 def chunk_rope_bwd(desc, rope, dq, dk, dq_out, dk_out, stream=None) -> None:
     """Gradients back: dq to dq_out, the chunk's own rows of dk [total_kv, num_kv_heads, head_dim] (bf16 or float32) to dk_out [total_q, num_kv_heads,
     head_dim], both bf16.  Either pair may be None."""
-    import torch
     if not _bound:
         _bind()
-    bf16, d = (torch.bfloat16,), desc.head_dim
-    qs, ks, kvs = (desc.total_q, desc.num_q_heads, d), (desc.total_q, desc.num_kv_heads, d), (desc.total_kv, desc.num_kv_heads, d)
-    call(_lib.chunk_rope_bwd, (dq, dk, dq_out, dk_out), stream, ctypes.byref(desc), ctypes.byref(rope), *rows(dq, bf16, qs, "dq"),
-         *rows(dk, (torch.bfloat16, torch.float32), kvs, "dk"), int(dk is not None and dk.dtype == torch.float32), *rows(dq_out, bf16, qs, "dq_out"),
-         *rows(dk_out, bf16, ks, "dk_out"))
+    d, n, heads, inner = desc.head_dim, desc.total_q, desc.num_kv_heads, (desc.head_dim, 1)
+    qs, f32 = (n, desc.num_q_heads, d), dk is not None and dk.dtype == F32
+    call(_lib.chunk_rope_bwd, (dq, dk, dq_out, dk_out), stream, ctypes.byref(desc), ctypes.byref(rope), *rows(dq, BF16, qs, inner, "dq"),
+         *rows(dk, F32 if f32 else BF16, (desc.total_kv, heads, d), inner, "dk"), f32, *rows(dq_out, BF16, qs, inner, "dq_out"),
+         *rows(dk_out, BF16, (n, heads, d), inner, "dk_out"))

@@ -85,32 +85,32 @@ __device__ __forceinline__ float power(float lg, int n) { return __builtin_amdgc
 constexpr int pitch(int cols) { return cols + (cols % 128 == 0 ? 24 : 8); }
 constexpr size_t tile_bytes(int cols) { return (size_t)kBlock * pitch(cols) * 2; }
 
-// A block's rows of one head on their way to LDS, fetched ahead into registers.  Forwards a block of fewer rows stands at the end of its 64, behind `empty` rows of zeros: the weights of rows in
-// the state are then the same in every block.
+// A block's rows of one head in memory, as a buffer: reads of other rows give zeros and writes to them are dropped by the hardware, so that no access is behind a branch (the compiler can then
+// count the ones in flight: with branches around the stores every step waited for the stores of the one before).
+struct Rows {
+  __amdgpu_buffer_rsrc_t buffer;
+  int stride;  // bytes
+  // `rows` rows of `bytes` bytes from `first` on
+  __device__ __forceinline__ Rows(const void* first, int stride, int rows, int bytes)
+      : buffer(__builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(first), 0, (rows - 1) * stride + bytes, 0x00027000)), stride(stride) {}
+  __device__ __forceinline__ u32x4 load(int row, int byte) const { return __builtin_amdgcn_raw_buffer_load_b128(buffer, row * stride + byte, 0, 0); }
+  __device__ __forceinline__ void store(int row, int byte, u32x4 x) const { __builtin_amdgcn_raw_buffer_store_b128(x, buffer, row * stride + byte, 0, 0); }
+};
+
+// A block's rows on their way to LDS, fetched ahead into registers.  Forwards a block of fewer rows stands at the end of its 64, behind `empty` rows of zeros: the weights of rows in the state are
+// then the same in every block.
 template <int D>
 struct Tile {
   static constexpr int kChunks = D / 8, kThreads = 2 * D, kEach = kBlock * kChunks / kThreads, kRowsApart = kThreads / kChunks;
-  bf16x8 x[kEach];
-  // rows empty .. empty + rows - 1 from `from` on, `stride` bytes apart; the others are zeros
-  __device__ __forceinline__ void fetch(const __bf16* from, unsigned stride, int empty, int rows) {
-    const int row0 = (int)threadIdx.x / kChunks, c = (int)threadIdx.x % kChunks;
-    const char* const base = reinterpret_cast<const char*>(from);
-    if (rows == kBlock) {
+  u32x4 x[kEach];
+  __device__ __forceinline__ void fetch(const Rows& from, int empty) {
 #pragma unroll
-      for (int i = 0; i < kEach; ++i) x[i] = *reinterpret_cast<const bf16x8*>(base + (unsigned)((row0 + i * kRowsApart) * stride + c * 16));
-    } else {
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) {
-        const int row = row0 + i * kRowsApart - empty;
-        x[i] = bf16x8{};
-        if (row >= 0 && row < rows) x[i] = *reinterpret_cast<const bf16x8*>(base + (unsigned)(row * stride + c * 16));
-      }
-    }
+    for (int i = 0; i < kEach; ++i) x[i] = from.load((int)threadIdx.x / kChunks + i * kRowsApart - empty, (int)threadIdx.x % kChunks * 16);
   }
   __device__ __forceinline__ void store(lds_bf16* to) const {
     lds_bf16* const at = to + (int)threadIdx.x / kChunks * pitch(D) + (int)threadIdx.x % kChunks * 8;
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) lds_store8(at + i * kRowsApart * pitch(D), x[i]);
+    for (int i = 0; i < kEach; ++i) lds_store8(at + i * kRowsApart * pitch(D), __builtin_bit_cast(bf16x8, x[i]));
   }
 };
 // Operand of 32 rows (or columns) x 16 of the contraction along the row: lane l32 holds row0 + l32, eight elements from 16 step + 8 hh on.
@@ -178,23 +178,35 @@ struct State {
     return pack8(a[o], a[o + 1], a[o + 2], a[o + 3], a[o + 4], a[o + 5], a[o + 6], a[o + 7]);
   }
   // adds k^T (w v) of 16 rows from row0 on: v's operand as it was read; element e's row weighs lead * base[e]
+  template <int PARTS>
   __device__ __forceinline__ void add(const lds_bf16* k_tile, int row0, bf16x8 v, float lead, const float (&base)[8], int lane) {
-    bf16x8 part[3];
+    constexpr int kTiles = D / 32, kHalf = (kTiles + 1) / 2;
+    bf16x8 kt[kTiles], part[PARTS];
+#pragma unroll
+    for (int i = 0; i < kHalf; ++i) kt[i] = column_operand<D, true>(k_tile, row0, 32 * i, lane);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       float x = (float)v[e] * (lead * base[e]);
-      part[0][e] = (__bf16)x;
-      x -= (float)part[0][e];
-      part[1][e] = (__bf16)x;
-      x -= (float)part[1][e];
-      part[2][e] = (__bf16)x;
+#pragma unroll
+      for (int p = 0; p < PARTS; ++p) {
+        part[p][e] = (__bf16)x;
+        x -= (float)part[p][e];
+      }
     }
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) {
-      const bf16x8 kt = column_operand<D, true>(k_tile, row0, 32 * i, lane);
+    for (int i = kHalf; i < kTiles; ++i) kt[i] = column_operand<D, true>(k_tile, row0, 32 * i, lane);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int p = 0; p < 3; ++p) t[i] = mfma32(kt, part[p], t[i]);
-    }
+    for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+      for (int i = 0; i < kHalf; ++i) t[i] = mfma32(kt[i], part[p], t[i]);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+      for (int i = kHalf; i < kTiles; ++i) t[i] = mfma32(kt[i], part[p], t[i]);
+    __builtin_amdgcn_sched_barrier(0);
   }
 };
 
@@ -204,14 +216,14 @@ struct StateWeights {
   float base[8], lead[4];
   __device__ __forceinline__ StateWeights(float lg, int hh) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) base[e] = power(lg, REVERSE ? e : 7 - e);
+    for (int e = 0; e < 8; ++e) base[e] = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(power(lg, REVERSE ? e : 7 - e))));
 #pragma unroll
     for (int s = 0; s < 4; ++s) lead[s] = power(lg, REVERSE ? 16 * s + 8 * hh + 1 : 56 - 16 * s - 8 * hh);
   }
 };
 
 // Each piece's own k^T v into its place in the workspace, but for the one at the far end of its sequence, whose nobody needs, and for sequences of one piece.
-template <int D, bool REVERSE>
+template <int D, bool REVERSE, int PARTS>
 __global__ __launch_bounds__(2 * D, 2) void piece_states_kernel(const WalkArgs a, const LinearSegs segs) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   lds_bf16* const ks = (lds_bf16*)smem;
@@ -231,8 +243,9 @@ __global__ __launch_bounds__(2 * D, 2) void piece_states_kernel(const WalkArgs a
   auto fetch = [&](int step) {
     const int b = REVERSE ? blocks - 1 - step / group : step / group, g = step % group, rows = min(kBlock, p.rows - b * kBlock);
     const int64_t at = (int64_t)(p.row + b * kBlock) * stride + (h * group + g) * D;
-    kt.fetch(a.k + at, (unsigned)stride * 2, REVERSE ? 0 : kBlock - rows, rows);
-    vt.fetch(a.v + at, (unsigned)stride * 2, REVERSE ? 0 : kBlock - rows, rows);
+    const int empty = REVERSE ? 0 : kBlock - rows;
+    kt.fetch(Rows(a.k + at, 2 * (int)stride, rows, 2 * D), empty);
+    vt.fetch(Rows(a.v + at, 2 * (int)stride, rows, 2 * D), empty);
   };
   fetch(0);
   for (int step = 0; step < steps; ++step) {
@@ -243,7 +256,7 @@ __global__ __launch_bounds__(2 * D, 2) void piece_states_kernel(const WalkArgs a
     if (step + 1 < steps) fetch(step + 1);
     if (step % group == 0) s.scale(power(lg, min(kBlock, p.rows - (REVERSE ? blocks - 1 - step / group : step / group) * kBlock)));
 #pragma unroll
-    for (int st = 0; st < 4; ++st) s.add(ks, 16 * st, column_operand<D, false>(vs, 16 * st, 32 * wave, lane), weights.lead[st], weights.base, lane);
+    for (int st = 0; st < 4; ++st) s.template add<PARTS>(ks, 16 * st, column_operand<D, false>(vs, 16 * st, 32 * wave, lane), weights.lead[st], weights.base, lane);
   }
   s.store(a.inner + ((int64_t)(segs.place0[p.seg] + p.index) * a.heads + h) * D * D, 32 * wave + (lane & 31), hh, 1.f);
 }
@@ -261,19 +274,27 @@ __global__ __launch_bounds__(256) void join_states_kernel(const WalkArgs a, cons
   f32x4 sum{};
   if (a.first && slot >= 0) sum = *reinterpret_cast<const f32x4*>(a.first + ((int64_t)slot * a.heads + h) * elements + at) * a.first_scale;
   const float whole = power(lg, segs.piece_rows);
-  for (int n = 0; n < pieces; ++n) {
-    const int i = REVERSE ? pieces - 1 - n : n;
-    f32x4* const x = reinterpret_cast<f32x4*>(a.inner + ((int64_t)(segs.place0[seg] + i) * a.heads + h) * elements + at);
-    f32x4 own{};
-    if (n < pieces - 1) own = *x;
-    *x = sum;
-    sum = sum * (i == pieces - 1 ? power(lg, len - i * segs.piece_rows) : whole) + own;
+  f32x4* const x = reinterpret_cast<f32x4*>(a.inner + ((int64_t)segs.place0[seg] * a.heads + h) * elements + at);
+  const int64_t apart = (int64_t)a.heads * elements / 4;
+  constexpr int kAhead = 8;  // states are loaded eight at a time: one after the other a sequence of 32 pieces took 20 us
+  for (int n0 = 0; n0 < pieces; n0 += kAhead) {
+    f32x4 own[kAhead];
+#pragma unroll
+    for (int n = 0; n < kAhead; ++n)
+      if (n0 + n < pieces - 1) own[n] = x[(REVERSE ? pieces - 1 - n0 - n : n0 + n) * apart];
+#pragma unroll
+    for (int n = 0; n < kAhead; ++n)
+      if (n0 + n < pieces) {
+        const int i = REVERSE ? pieces - 1 - n0 - n : n0 + n;
+        x[i * apart] = sum;
+        if (n0 + n < pieces - 1) sum = sum * (i == pieces - 1 ? power(lg, len - i * segs.piece_rows) : whole) + own[n];
+      }
   }
 }
 
 // Four neighbouring elements of a row from either half of the wave (registers 4 g .. 4 g + 3 of an output tile are elements 8 g + 4 hh ..): stored as 16 bytes, the lower half
 // of the lanes takes those of an even g, the upper one those of the odd g behind it.
-__device__ __forceinline__ void store_row(__bf16* row, const f32x16& o, float by, int hh, bool live) {
+__device__ __forceinline__ void store_row(const Rows& to, int row, int byte, const f32x16& o, float by, int hh) {
 #pragma unroll
   for (int g = 0; g < 4; g += 2) {
     union {
@@ -283,19 +304,20 @@ __device__ __forceinline__ void store_row(__bf16* row, const f32x16& o, float by
     even.h = pack4(o[4 * g] * by, o[4 * g + 1] * by, o[4 * g + 2] * by, o[4 * g + 3] * by);
     odd.h = pack4(o[4 * g + 4] * by, o[4 * g + 5] * by, o[4 * g + 6] * by, o[4 * g + 7] * by);
     const u32x2 x = __builtin_amdgcn_permlane32_swap(even.u[0], odd.u[0], false, false), y = __builtin_amdgcn_permlane32_swap(even.u[1], odd.u[1], false, false);
-    if (live) *reinterpret_cast<u32x4*>(row + 8 * (g + hh)) = u32x4{x[0], y[0], x[1], y[1]};
+    to.store(row, byte + 16 * (g + hh), u32x4{x[0], y[0], x[1], y[1]});
   }
 }
 
 // The walk.  Forwards a workgroup takes all query heads of its key/value head, one after the other in each block; backwards all of them stand in the roles of k and v.
 // The next step's rows are fetched while this one's products run; two workgroups share a compute unit (head_dim 128: 56 KB of LDS and at most 256 registers each).
-template <int D, bool REVERSE, bool TRANSPOSED>
+template <int D, bool REVERSE, bool TRANSPOSED, int PARTS>
 __global__ __launch_bounds__(2 * D, 2) void walk_kernel(const WalkArgs a, const LinearSegs segs) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   lds_bf16* const qs = (lds_bf16*)smem;
   lds_bf16* const ks = qs + kBlock * pitch(D);
   lds_bf16* const vs = ks + kBlock * pitch(D);
   lds_bf16* const ps = vs + kBlock * pitch(D);  // weighted scores, 64 x 64
+  lds_f32* const near = (lds_f32*)(ps + kBlock * pitch(64));
   constexpr int kWaves = D / 32;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, hh = lane >> 5, l32 = lane & 31;
   const int h = blockIdx.x % a.heads;
@@ -315,11 +337,11 @@ __global__ __launch_bounds__(2 * D, 2) void walk_kernel(const WalkArgs a, const 
   };
   Tile<D> qt, kt, vt;
   auto fetch = [&](const Step& x) {
-    if (!REVERSE || x.g == 0) qt.fetch(a.q + x.row0 * q_stride + (h * q_group + (REVERSE ? 0 : x.g)) * D, (unsigned)q_stride * 2, x.empty, x.rows);
+    if (!REVERSE || x.g == 0) qt.fetch(Rows(a.q + x.row0 * q_stride + (h * q_group + (REVERSE ? 0 : x.g)) * D, 2 * (int)q_stride, x.rows, 2 * D), x.empty);
     if (REVERSE || x.g == 0) {
       const int64_t at = x.row0 * kv_stride + (h * kv_group + (REVERSE ? x.g : 0)) * D;
-      kt.fetch(a.k + at, (unsigned)kv_stride * 2, x.empty, x.rows);
-      vt.fetch(a.v + at, (unsigned)kv_stride * 2, x.empty, x.rows);
+      kt.fetch(Rows(a.k + at, 2 * (int)kv_stride, x.rows, 2 * D), x.empty);
+      vt.fetch(Rows(a.v + at, 2 * (int)kv_stride, x.rows, 2 * D), x.empty);
     }
   };
   Step now = step_of(0, 0);
@@ -333,14 +355,15 @@ __global__ __launch_bounds__(2 * D, 2) void walk_kernel(const WalkArgs a, const 
   else s.clear();
 
   const StateWeights<REVERSE> weights(lg, hh);
-  // Scores are taken in tiles of 32 x 32, 0: (0, 0), 1: the one off the diagonal, 2: (1, 1); a wave's tiles have the same distances (with two waves the first takes 0 and 2).
-  float near[16];
-#pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    const int j = 8 * (e >> 2) + 4 * hh + (e & 3), far = (REVERSE ? j - l32 : l32 - j) + (wave == 1 ? 32 : 0);
-    near[e] = far >= 0 ? power(lg, far) : 0.f;
+  // Scores are taken in tiles of 32 x 32, 0: (0, 0), 1: the one off the diagonal, 2: (1, 1).  Their weights, as a lane needs them, lie in LDS: on the diagonal, and off it.
+  for (int i = threadIdx.x; i < 2 * 16 * 64; i += 2 * D) {
+    const int l = i >> 2 & 63, j = 8 * (i >> 8 & 3) + 4 * (l >> 5) + (i & 3), far = (REVERSE ? j - (l & 31) : (l & 31) - j) + 32 * (i >> 10);
+    near[i] = far >= 0 ? power(lg, far) : 0.f;
   }
+  const int off = wave == 1 ? 1024 : 0;  // (with two waves the first takes tiles 0 and 2)
+  const int ti = REVERSE ? wave >> 1 : (wave + 1) >> 1, tj = REVERSE ? (wave + 1) >> 1 : wave >> 1;  // the wave's tile, if it has one
 
+  wait_all_but<0>();  // (else the compiler has the loop wait for all loads wherever it uses the state)
   f32x16 o[2];
   for (int n = 0; n < blocks; ++n) {
     for (int g = 0; g < group; ++g) {
@@ -357,50 +380,93 @@ __global__ __launch_bounds__(2 * D, 2) void walk_kernel(const WalkArgs a, const 
         now = step_of(last ? n + 1 : n, last ? 0 : g + 1);
         fetch(now);
       }
-      // scores, transposed (a lane: one row i, four columns j at a time), weighted, to LDS; only tiles with j <= i (backwards j >= i)
-      for (int tile = wave; tile < 3; tile += kWaves) {
-        const int ti = REVERSE ? tile >> 1 : (tile + 1) >> 1, tj = REVERSE ? (tile + 1) >> 1 : tile >> 1;
+      // Scores, transposed (a lane: one row i, four columns j at a time), only tiles with j <= i (backwards j >= i).  Operands are read two stages ahead, here and below.
+      constexpr int kSteps = D / 16, kAhead = 2;
+      auto scores = [&](int off, int ti, int tj) {
         f32x16 c{};
+        bf16x8 kf[kSteps], qf[kSteps];
+        auto read = [&](int st) {
+          kf[st] = row_operand<D>(ks, 32 * tj, st, lane);
+          qf[st] = row_operand<D>(qs, 32 * ti, st, lane);
+        };
 #pragma unroll
-        for (int st = 0; st < D / 16; ++st) c = mfma32(row_operand<D>(ks, 32 * tj, st, lane), row_operand<D>(qs, 32 * ti, st, lane), c);
+        for (int st = 0; st < kAhead; ++st) read(st);
+#pragma unroll
+        for (int st = 0; st < kSteps; ++st) {
+          if (st + kAhead < kSteps) read(st + kAhead);
+          __builtin_amdgcn_sched_barrier(0);
+          c = mfma32(kf[st], qf[st], c);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        f32x4 w[4];
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) w[q4] = lds_load4f(near + off + q4 * 256 + lane * 4);
 #pragma unroll
         for (int q4 = 0; q4 < 4; ++q4)
           *(__attribute__((address_space(3))) bf16x4*)(ps + (l32 * pitch(64) + 4 * hh) + (32 * ti * pitch(64) + 32 * tj + 8 * q4)) =
-              pack4(c[4 * q4] * near[4 * q4], c[4 * q4 + 1] * near[4 * q4 + 1], c[4 * q4 + 2] * near[4 * q4 + 2], c[4 * q4 + 3] * near[4 * q4 + 3]);
-      }
-      if (!REVERSE || g == 0) {  // what the state gives
-        o[0] = f32x16{};
-        o[1] = f32x16{};
+              pack4(c[4 * q4] * w[q4][0], c[4 * q4 + 1] * w[q4][1], c[4 * q4 + 2] * w[q4][2], c[4 * q4 + 3] * w[q4][3]);
+      };
+      if (wave < 3) scores(off, ti, tj);
+      if (kWaves == 2 && wave == 0) scores(0, 1, 1);
+      const bool from_state = !REVERSE || g == 0;
+      if (from_state) {
+        bf16x8 qf[kSteps][2];
+        auto read = [&](int st) {
+          qf[st][0] = row_operand<D>(qs, 0, st, lane);
+          qf[st][1] = row_operand<D>(qs, 32, st, lane);
+        };
+        o[0] = o[1] = f32x16{};
 #pragma unroll
-        for (int st = 0; st < D / 16; ++st) {
+        for (int st = 0; st < kAhead; ++st) read(st);
+#pragma unroll
+        for (int st = 0; st < kSteps; ++st) {
+          if (st + kAhead < kSteps) read(st + kAhead);
+          __builtin_amdgcn_sched_barrier(0);
           const bf16x8 sb = s.operand(st);
-#pragma unroll
-          for (int ti = 0; ti < 2; ++ti) o[ti] = mfma32(sb, row_operand<D>(qs, 32 * ti, st, lane), o[ti]);
+          o[0] = mfma32(sb, qf[st][0], o[0]);
+          o[1] = mfma32(sb, qf[st][1], o[1]);
+          __builtin_amdgcn_sched_barrier(0);
         }
+      }
+      if (from_state) {
 #pragma unroll
-        for (int ti = 0; ti < 2; ++ti) {
-          const int i = 32 * ti + l32 - x.empty;
+        for (int half = 0; half < 2; ++half) {
+          const int i = 32 * half + l32 - x.empty;
           const float by = power(lg, max(REVERSE ? x.rows - 1 - i : i + 1, 0));
 #pragma unroll
-          for (int e = 0; e < 16; ++e) o[ti][e] *= by;
+          for (int e = 0; e < 16; ++e) o[half][e] *= by;
         }
       }
       __syncthreads();
-      if (REVERSE ? g == 0 : last) s.scale(power(lg, x.rows));
+      bf16x8 vop[4];
+      {
+        bf16x8 pf[4][2];
+        auto read = [&](int st) {
+          vop[st] = column_operand<D, false>(vs, 16 * st, 32 * wave, lane);
 #pragma unroll
-      for (int st = 0; st < 4; ++st) {
-        const bf16x8 vop = column_operand<D, false>(vs, 16 * st, 32 * wave, lane);
+          for (int half = 0; half < 2; ++half)
+            if (REVERSE ? st >= 2 * half : st < 2 * half + 2) pf[st][half] = row_operand<64>(ps, 32 * half, st, lane);
+        };
+        read(0);
 #pragma unroll
-        for (int ti = 0; ti < 2; ++ti)
-          if (REVERSE ? st >= 2 * ti : st < 2 * ti + 2) o[ti] = mfma32(vop, row_operand<64>(ps, 32 * ti, st, lane), o[ti]);
-        if (REVERSE || last) s.add(ks, 16 * st, vop, weights.lead[st], weights.base, lane);
+        for (int st = 0; st < 4; ++st) {
+          if (st < 3) read(st + 1);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int half = 0; half < 2; ++half)
+            if (REVERSE ? st >= 2 * half : st < 2 * half + 2) o[half] = mfma32(vop[st], pf[st][half], o[half]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
       if (!REVERSE || last) {
+        const Rows out(a.o + x.row0 * q_stride + (h * q_group + (REVERSE ? 0 : g)) * D, 2 * (int)q_stride, x.rows, 2 * D);
 #pragma unroll
-        for (int ti = 0; ti < 2; ++ti) {
-          const int i = 32 * ti + l32 - x.empty;
-          store_row(a.o + (x.row0 + i) * q_stride + (h * q_group + (REVERSE ? 0 : g)) * D + 32 * wave, o[ti], a.scale, hh, i >= 0 && i < x.rows);
-        }
+        for (int half = 0; half < 2; ++half) store_row(out, 32 * half + l32 - x.empty, 64 * wave, o[half], a.scale, hh);
+      }
+      if (REVERSE ? g == 0 : last) s.scale(power(lg, x.rows));
+      if (REVERSE || last) {
+#pragma unroll
+        for (int st = 0; st < 4; ++st) s.template add<PARTS>(ks, 16 * st, vop[st], weights.lead[st], weights.base, lane);
       }
     }
   }
@@ -509,7 +575,7 @@ int validate_linear(const chunk_linear_desc* d) {
   if (!d || d->num_q_heads < 1 || d->num_kv_heads < 1 || d->total < 1 || d->num_segments < 1 || d->num_states < 0 || !d->segments || !finite_number(d->scale) ||
       d->scale <= 0.f)
     return CHUNK_ATTN_INVALID_ARG;
-  if (!head_dim_ok(d->head_dim) || d->num_q_heads % d->num_kv_heads != 0) return CHUNK_ATTN_UNSUPPORTED;
+  if (!head_dim_ok(d->head_dim) || d->num_q_heads % d->num_kv_heads != 0 || d->num_q_heads > CHUNK_LINEAR_MAX_HEADS) return CHUNK_ATTN_UNSUPPORTED;
   int64_t end = 0;
   for (int i = 0; i < d->num_segments; ++i) {
     const chunk_linear_seg& s = d->segments[i];
@@ -548,15 +614,15 @@ int check_slots(const chunk_linear_desc* d, bool in_once, bool in_place) {
   return CHUNK_ATTN_OK;
 }
 
-// Rows of a piece.  Sequences are cut where whole ones would leave compute units without work: as long as there are fewer than four walks for each.
+// Rows of a piece: a walk's even share when two walks run on each compute unit (one at head_dim 256).
 int piece_rows(const chunk_linear_desc* d) {
   int64_t rows = 0, longest = 0;
   for (int i = 0; i < d->num_segments; ++i) {
     rows += d->segments[i].len;
     longest = std::max<int64_t>(longest, d->segments[i].len);
   }
-  const int64_t wanted = rows * d->num_kv_heads / (4 * kCus);  // a walk's even share
-  const int64_t blocks = std::max<int64_t>(4, (wanted + kBlock - 1) / kBlock);
+  const int64_t share = rows * d->num_kv_heads / (d->head_dim > 128 ? kCus : 2 * kCus);
+  const int64_t blocks = std::max<int64_t>(1, (share + kBlock - 1) / kBlock);
   return (int)std::min<int64_t>(blocks, (longest + kBlock - 1) / kBlock) * kBlock;
 }
 int pieces_of(int len, int rows) { return (len - 1) / rows + 1; }
@@ -577,23 +643,23 @@ hipError_t by_dim(int d, F&& f) {
   return f(integral_constant<int, 256>{});
 }
 
-template <int D, bool REVERSE>
+template <int D, bool REVERSE, int PARTS>
 hipError_t launch_piece_states(const WalkArgs& a, const LinearSegs& segs, hipStream_t stream) {
   constexpr size_t smem = 2 * tile_bytes(D);
   static const hipError_t attr =
-      hipFuncSetAttribute(reinterpret_cast<const void*>(&piece_states_kernel<D, REVERSE>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+      hipFuncSetAttribute(reinterpret_cast<const void*>(&piece_states_kernel<D, REVERSE, PARTS>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (attr != hipSuccess) return attr;
-  hipLaunchKernelGGL((piece_states_kernel<D, REVERSE>), dim3((unsigned)(segs.num_pieces * a.heads)), dim3(2 * D), smem, stream, a, segs);
+  hipLaunchKernelGGL((piece_states_kernel<D, REVERSE, PARTS>), dim3((unsigned)(segs.num_pieces * a.heads)), dim3(2 * D), smem, stream, a, segs);
   hipLaunchKernelGGL((join_states_kernel<REVERSE>), dim3((D * D / 4 + 255) / 256, (unsigned)(segs.n * a.heads)), dim3(256), 0, stream, a, segs, D * D);
   return hipGetLastError();
 }
-template <int D, bool REVERSE, bool TRANSPOSED>
+template <int D, bool REVERSE, bool TRANSPOSED, int PARTS>
 hipError_t launch_walk(const WalkArgs& a, const LinearSegs& segs, hipStream_t stream) {
-  constexpr size_t smem = 3 * tile_bytes(D) + tile_bytes(kBlock);
+  constexpr size_t smem = 3 * tile_bytes(D) + tile_bytes(kBlock) + 2 * 16 * 64 * sizeof(float);
   static const hipError_t attr =
-      hipFuncSetAttribute(reinterpret_cast<const void*>(&walk_kernel<D, REVERSE, TRANSPOSED>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+      hipFuncSetAttribute(reinterpret_cast<const void*>(&walk_kernel<D, REVERSE, TRANSPOSED, PARTS>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (attr != hipSuccess) return attr;
-  hipLaunchKernelGGL((walk_kernel<D, REVERSE, TRANSPOSED>), dim3((unsigned)(segs.num_pieces * a.heads)), dim3(2 * D), smem, stream, a, segs);
+  hipLaunchKernelGGL((walk_kernel<D, REVERSE, TRANSPOSED, PARTS>), dim3((unsigned)(segs.num_pieces * a.heads)), dim3(2 * D), smem, stream, a, segs);
   return hipGetLastError();
 }
 
@@ -670,9 +736,12 @@ extern "C" int chunk_linear_fwd(const chunk_linear_desc* d, const void* q, const
   const hipError_t e = for_segments(d, rows, [&](const LinearSegs& segs, bool cut) {
     return by_dim(d->head_dim, [&](auto dim) {
       constexpr int D = decltype(dim)::value;
-      hipError_t e = hipSuccess;
-      if (cut) e = launch_piece_states<D, false>(a, segs, stream);
-      return e != hipSuccess ? e : launch_walk<D, false, false>(a, segs, stream);
+      auto with_parts = [&](auto parts) {
+        constexpr int kParts = decltype(parts)::value;
+        const hipError_t e = cut ? launch_piece_states<D, false, kParts>(a, segs, stream) : hipSuccess;
+        return e != hipSuccess ? e : launch_walk<D, false, false, kParts>(a, segs, stream);
+      };
+      return states_out ? with_parts(std::integral_constant<int, 3>{}) : with_parts(std::integral_constant<int, 2>{});
     });
   });
   return e == hipSuccess ? CHUNK_ATTN_OK : report_hip(e, "linear attention forward");
@@ -716,12 +785,12 @@ extern "C" int chunk_linear_bwd(const chunk_linear_desc* d, const void* q, const
       constexpr int D = decltype(dim)::value;
       hipError_t e = hipSuccess;
       if (cut) {
-        if ((e = launch_piece_states<D, false>(s_states, segs, stream)) != hipSuccess) return e;
-        if ((e = launch_piece_states<D, true>(r_states, segs, stream)) != hipSuccess) return e;
+        if ((e = launch_piece_states<D, false, 2>(s_states, segs, stream)) != hipSuccess) return e;
+        if ((e = d_states_in ? launch_piece_states<D, true, 3>(r_states, segs, stream) : launch_piece_states<D, true, 2>(r_states, segs, stream)) != hipSuccess) return e;
       }
-      if ((e = launch_walk<D, false, true>(to_q, segs, stream)) != hipSuccess) return e;
-      if ((e = launch_walk<D, true, true>(to_k, segs, stream)) != hipSuccess) return e;
-      return launch_walk<D, true, false>(to_v, segs, stream);
+      if ((e = launch_walk<D, false, true, 2>(to_q, segs, stream)) != hipSuccess) return e;
+      if ((e = launch_walk<D, true, true, 2>(to_k, segs, stream)) != hipSuccess) return e;
+      return d_states_in ? launch_walk<D, true, false, 3>(to_v, segs, stream) : launch_walk<D, true, false, 2>(to_v, segs, stream);
     });
   });
   return e == hipSuccess ? CHUNK_ATTN_OK : report_hip(e, "linear attention backward");
