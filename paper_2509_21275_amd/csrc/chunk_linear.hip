@@ -23,6 +23,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <initializer_list>
 #include <new>
 #include <utility>
@@ -40,9 +41,11 @@ constexpr int kBlock = 64;       // rows of a block
 constexpr int kLinearSegs = 144; // segments that travel with one launch
 
 struct LinearSegs {
-  int n, num_pieces, piece_rows;  // pieces of these segments; rows of a piece (a multiple of kBlock)
+  int n;                      // segments, those that leave most rows beside their full pieces first
+  int num_full, num_pieces;   // full pieces of these segments; all, the full ones first, then what is left of each segment that has something left
+  int piece_rows;             // rows of a full piece, a multiple of kBlock
   int start[kLinearSegs], len[kLinearSegs], in[kLinearSegs], out[kLinearSegs];
-  int piece0[kLinearSegs];  // first of its pieces among the launch's
+  int full0[kLinearSegs];   // full pieces of the segments before
   int place0[kLinearSegs];  // place of its first piece's state in the workspace, where it has several
 };
 struct WalkArgs {
@@ -62,16 +65,18 @@ struct Piece {
 };
 __device__ __forceinline__ Piece find_piece(const LinearSegs& s, int piece) {
   const int lane = threadIdx.x & 63;
-  int seg = -1;
-  for (int i = 0; i < s.n; i += 64) {
-    const int j = min(i + lane, s.n - 1);
-    seg += __popcll(__ballot(i + lane < s.n && s.piece0[j] <= piece));
-  }
   Piece p;
-  p.seg = __builtin_amdgcn_readfirstlane(seg);
+  if (piece < s.num_full) {
+    int seg = -1;  // the last segment whose full pieces begin at or before this one
+    for (int i = 0; i < s.n; i += 64) seg += __popcll(__ballot(i + lane < s.n && s.full0[min(i + lane, s.n - 1)] <= piece));
+    p.seg = __builtin_amdgcn_readfirstlane(seg);
+    p.index = piece - s.full0[p.seg];
+  } else {
+    p.seg = piece - s.num_full;
+    p.index = s.len[p.seg] / s.piece_rows;
+  }
   const int len = s.len[p.seg];
   p.pieces = (len + s.piece_rows - 1) / s.piece_rows;
-  p.index = piece - s.piece0[p.seg];
   p.row = s.start[p.seg] + p.index * s.piece_rows;
   p.rows = min(s.piece_rows, len - p.index * s.piece_rows);
   return p;
@@ -99,16 +104,16 @@ struct Rows {
 
 // A block's rows on their way to LDS, fetched ahead into registers.  Forwards a block of fewer rows stands at the end of its 64, behind `empty` rows of zeros: the weights of rows in the state are
 // then the same in every block.
-template <int D>
+template <int D, int THREADS = 2 * D>
 struct Tile {
-  static constexpr int kChunks = D / 8, kThreads = 2 * D, kEach = kBlock * kChunks / kThreads, kRowsApart = kThreads / kChunks;
+  static constexpr int kChunks = D / 8, kThreads = THREADS, kEach = kBlock * kChunks / kThreads, kRowsApart = kThreads / kChunks;
   u32x4 x[kEach];
   __device__ __forceinline__ void fetch(const Rows& from, int empty) {
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) x[i] = from.load((int)threadIdx.x / kChunks + i * kRowsApart - empty, (int)threadIdx.x % kChunks * 16);
+    for (int i = 0; i < kEach; ++i) x[i] = from.load((int)threadIdx.x % kThreads / kChunks + i * kRowsApart - empty, (int)threadIdx.x % kThreads % kChunks * 16);
   }
   __device__ __forceinline__ void store(lds_bf16* to) const {
-    lds_bf16* const at = to + (int)threadIdx.x / kChunks * pitch(D) + (int)threadIdx.x % kChunks * 8;
+    lds_bf16* const at = to + (int)threadIdx.x % kThreads / kChunks * pitch(D) + (int)threadIdx.x % kThreads % kChunks * 8;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) lds_store8(at + i * kRowsApart * pitch(D), __builtin_bit_cast(bf16x8, x[i]));
   }
@@ -231,7 +236,7 @@ __global__ __launch_bounds__(2 * D, 2) void piece_states_kernel(const WalkArgs a
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, hh = lane >> 5;
   const int h = blockIdx.x % a.heads;
   const Piece p = find_piece(segs, blockIdx.x / a.heads);
-  if (p.index == (REVERSE ? 0 : p.pieces - 1)) return;
+  if (p.index == (REVERSE ? 0 : p.pieces - 1)) return;  // (also where there is one piece)
   const float lg = log2_decay(a.log_decay, h);
   const int group = REVERSE ? a.group : 1;
   const int64_t stride = (int64_t)a.heads * group * D;
@@ -292,186 +297,335 @@ __global__ __launch_bounds__(256) void join_states_kernel(const WalkArgs a, cons
   }
 }
 
-// Four neighbouring elements of a row from either half of the wave (registers 4 g .. 4 g + 3 of an output tile are elements 8 g + 4 hh ..): stored as 16 bytes, the lower half
-// of the lanes takes those of an even g, the upper one those of the odd g behind it.
-__device__ __forceinline__ void store_row(const Rows& to, int row, int byte, const f32x16& o, float by, int hh) {
+// Four neighbouring elements of a row lie in either half of the wave (registers 4 g .. 4 g + 3 of an output tile are elements 8 g + 4 hh ..).  They are put together to 16 bytes of a lane, and then
+// moved between the lanes of rows r and r + 16, so that each store takes the wave's 64 bytes of sixteen rows (half of them of all rows took the address unit twice as long).
+__device__ __forceinline__ void store_rows(const Rows& to, int row0, int byte, const f32x16& o, int lane) {
+  u32x4 x[2];
 #pragma unroll
   for (int g = 0; g < 4; g += 2) {
     union {
       bf16x4 h;
       unsigned u[2];
     } even, odd;
-    even.h = pack4(o[4 * g] * by, o[4 * g + 1] * by, o[4 * g + 2] * by, o[4 * g + 3] * by);
-    odd.h = pack4(o[4 * g + 4] * by, o[4 * g + 5] * by, o[4 * g + 6] * by, o[4 * g + 7] * by);
-    const u32x2 x = __builtin_amdgcn_permlane32_swap(even.u[0], odd.u[0], false, false), y = __builtin_amdgcn_permlane32_swap(even.u[1], odd.u[1], false, false);
-    to.store(row, byte + 16 * (g + hh), u32x4{x[0], y[0], x[1], y[1]});
+    even.h = pack4(o[4 * g], o[4 * g + 1], o[4 * g + 2], o[4 * g + 3]);
+    odd.h = pack4(o[4 * g + 4], o[4 * g + 5], o[4 * g + 6], o[4 * g + 7]);
+    const u32x2 a = __builtin_amdgcn_permlane32_swap(even.u[0], odd.u[0], false, false), b = __builtin_amdgcn_permlane32_swap(even.u[1], odd.u[1], false, false);
+    x[g / 2] = u32x4{a[0], b[0], a[1], b[1]};  // lane (row l32, hh): bytes 32 (g / 2) + 16 hh of its row's 64
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const u32x2 y = __builtin_amdgcn_permlane16_swap(x[0][i], x[1][i], false, false);
+    x[0][i] = y[0];
+    x[1][i] = y[1];
+  }
+  // x[0]: rows row0 .. + 15, x[1]: the sixteen behind them; lanes 0 - 15: bytes 0, 16 - 31: 32, 32 - 47: 16, 48 - 63: 48
+  const int at = byte + (lane & 16) * 2 + (lane >> 5) * 16;
+  to.store(row0 + (lane & 15), at, x[0]);
+  to.store(row0 + 16 + (lane & 15), at, x[1]);
+}
+
+// ---- the three products of a step ----
+constexpr int kAhead = 2;  // stages that operands are read ahead of their products
+
+// Weights of scores, times the scale of outputs, as a lane needs them: of a tile on the diagonal of the block, and of the one off it ([2][quad of columns][lane][4]).
+constexpr int kNear = 2 * 16 * 64;
+template <bool REVERSE, int THREADS>
+__device__ __forceinline__ void score_weights(float lg, float scale, lds_f32* near) {
+  for (int i = threadIdx.x; i < kNear; i += THREADS) {
+    const int l = i >> 2 & 63, j = 8 * (i >> 8 & 3) + 4 * (l >> 5) + (i & 3), far = (REVERSE ? j - (l & 31) : (l & 31) - j) + 32 * (i >> 10);
+    near[i] = far >= 0 ? power(lg, far) * scale : 0.f;
+  }
+}
+// Scores of rows i of q with rows j of k, in tiles of 32 x 32, only those with j <= i (backwards j >= i): 0: (0, 0), 1: the one off the diagonal, 2: (1, 1).  Formed transposed (a lane holds one row i
+// and four columns j at a time), weighted, and written to LDS.
+template <int D, bool REVERSE>
+__device__ __forceinline__ void scores(int tile, const lds_bf16* qs, const lds_bf16* ks, const lds_f32* near, lds_bf16* ps, int lane) {
+  const int ti = REVERSE ? tile >> 1 : (tile + 1) >> 1, tj = REVERSE ? (tile + 1) >> 1 : tile >> 1;
+  constexpr int kSteps = D / 16;
+  f32x16 c{}, c1{};  // (two sums, so that a product need not wait for the one before)
+  bf16x8 kf[kSteps], qf[kSteps];
+  auto read = [&](int st) {
+    kf[st] = row_operand<D>(ks, 32 * tj, st, lane);
+    qf[st] = row_operand<D>(qs, 32 * ti, st, lane);
+  };
+#pragma unroll
+  for (int st = 0; st < kAhead; ++st) read(st);
+#pragma unroll
+  for (int st = 0; st < kSteps; ++st) {
+    if (st + kAhead < kSteps) read(st + kAhead);
+    __builtin_amdgcn_sched_barrier(0);
+    (st % 2 ? c1 : c) = mfma32(kf[st], qf[st], st % 2 ? c1 : c);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  c += c1;
+  f32x4 w[4];
+#pragma unroll
+  for (int q4 = 0; q4 < 4; ++q4) w[q4] = lds_load4f(near + (tile == 1 ? 1024 : 0) + q4 * 256 + lane * 4);
+  lds_bf16* const to = ps + ((lane & 31) * pitch(64) + 4 * (lane >> 5)) + (32 * ti * pitch(64) + 32 * tj);
+#pragma unroll
+  for (int q4 = 0; q4 < 4; ++q4)
+    *(__attribute__((address_space(3))) bf16x4*)(to + 8 * q4) = pack4(c[4 * q4] * w[q4][0], c[4 * q4 + 1] * w[q4][1], c[4 * q4 + 2] * w[q4][2], c[4 * q4 + 3] * w[q4][3]);
+}
+// What the state gives the wave's 32 columns, times each row's power of the decay and the scale of outputs.  Rows stand behind `empty` others.
+template <int D, bool REVERSE>
+__device__ __forceinline__ void state_outputs(const State<D>& s, const lds_bf16* qs, float lg, float scale, int rows, int empty, int lane, f32x16 (&o)[2]) {
+  constexpr int kSteps = D / 16;
+  bf16x8 qf[kSteps][2];
+  auto read = [&](int st) {
+    qf[st][0] = row_operand<D>(qs, 0, st, lane);
+    qf[st][1] = row_operand<D>(qs, 32, st, lane);
+  };
+  o[0] = o[1] = f32x16{};
+#pragma unroll
+  for (int st = 0; st < kAhead; ++st) read(st);
+#pragma unroll
+  for (int st = 0; st < kSteps; ++st) {
+    if (st + kAhead < kSteps) read(st + kAhead);
+    __builtin_amdgcn_sched_barrier(0);
+    const bf16x8 sb = s.operand(st);
+    o[0] = mfma32(sb, qf[st][0], o[0]);
+    o[1] = mfma32(sb, qf[st][1], o[1]);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    const int i = 32 * half + (lane & 31) - empty;
+    const float by = scale * power(lg, max(REVERSE ? rows - 1 - i : i + 1, 0));
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[half][e] *= by;
+  }
+}
+// Adds what the scores give; leaves v's operands.
+template <int D, bool REVERSE>
+__device__ __forceinline__ void score_outputs(const lds_bf16* ps, const lds_bf16* vs, int col0, int lane, f32x16 (&o)[2], bf16x8 (&vop)[4]) {
+  bf16x8 pf[4][2];
+  auto pair = [](int st, int half) { return REVERSE ? st >= 2 * half : st < 2 * half + 2; };
+  auto read = [&](int st) {
+    vop[st] = column_operand<D, false>(vs, 16 * st, col0, lane);
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+      if (pair(st, half)) pf[st][half] = row_operand<64>(ps, 32 * half, st, lane);
+  };
+#pragma unroll
+  for (int st = 0; st < kAhead; ++st) read(st);
+#pragma unroll
+  for (int st = 0; st < 4; ++st) {
+    if (st + kAhead < 4) read(st + kAhead);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+      if (pair(st, half)) o[half] = mfma32(vop[st], pf[st][half], o[half]);
+    __builtin_amdgcn_sched_barrier(0);
   }
 }
 
-// The walk.  Forwards a workgroup takes all query heads of its key/value head, one after the other in each block; backwards all of them stand in the roles of k and v.
-// The next step's rows are fetched while this one's products run; two workgroups share a compute unit (head_dim 128: 56 KB of LDS and at most 256 registers each).
-template <int D, bool REVERSE, bool TRANSPOSED, int PARTS>
+// The walk forwards: outputs, or dq.  A workgroup takes all query heads of its key/value head, one after the other in each block.  The next query head's rows are stored to LDS as soon as
+// all waves are through with this one's, in the middle of its step, and those of the one after next fetched from then on; k and v of the next block are fetched while this one's query
+// heads run.  Two workgroups share a compute unit (head_dim 128: 74 KB of LDS each).
+template <int D, bool TRANSPOSED, int PARTS>
 __global__ __launch_bounds__(2 * D, 2) void walk_kernel(const WalkArgs a, const LinearSegs segs) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
+  constexpr int kTile = kBlock * pitch(D), kWaves = D / 32;
   lds_bf16* const qs = (lds_bf16*)smem;
-  lds_bf16* const ks = qs + kBlock * pitch(D);
-  lds_bf16* const vs = ks + kBlock * pitch(D);
-  lds_bf16* const ps = vs + kBlock * pitch(D);  // weighted scores, 64 x 64
+  lds_bf16* const ks = qs + kTile;
+  lds_bf16* const vs = ks + kTile;
+  lds_bf16* const ps = vs + kTile;  // weighted scores, 64 x 64
   lds_f32* const near = (lds_f32*)(ps + kBlock * pitch(64));
-  constexpr int kWaves = D / 32;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, hh = lane >> 5, l32 = lane & 31;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, hh = lane >> 5;
   const int h = blockIdx.x % a.heads;
   const Piece p = find_piece(segs, blockIdx.x / a.heads);
   const float lg = log2_decay(a.log_decay, h);
-  const int group = a.group, q_group = REVERSE ? 1 : group, kv_group = REVERSE ? group : 1;
-  const int64_t q_stride = (int64_t)a.heads * q_group * D, kv_stride = (int64_t)a.heads * kv_group * D;
+  const int group = a.group;
+  const int64_t q_stride = (int64_t)a.heads * group * D, kv_stride = (int64_t)a.heads * D;
   const int blocks = (p.rows + kBlock - 1) / kBlock;
 
-  struct Step {  // one block and one query head
-    int g, rows, empty;
-    int64_t row0;
-  };
-  auto step_of = [&](int n, int g) {
-    const int b = REVERSE ? blocks - 1 - n : n, rows = min(kBlock, p.rows - b * kBlock);
-    return Step{g, rows, REVERSE ? 0 : kBlock - rows, (int64_t)p.row + b * kBlock};
+  auto rows_of = [&](int n) { return min(kBlock, p.rows - n * kBlock); };
+  auto q_rows = [&](const __bf16* t, int n, int g) {
+    return Rows(t + (int64_t)(p.row + n * kBlock) * q_stride + (h * group + g) * D, 2 * (int)q_stride, rows_of(n), 2 * D);
   };
   Tile<D> qt, kt, vt;
-  auto fetch = [&](const Step& x) {
-    if (!REVERSE || x.g == 0) qt.fetch(Rows(a.q + x.row0 * q_stride + (h * q_group + (REVERSE ? 0 : x.g)) * D, 2 * (int)q_stride, x.rows, 2 * D), x.empty);
-    if (REVERSE || x.g == 0) {
-      const int64_t at = x.row0 * kv_stride + (h * kv_group + (REVERSE ? x.g : 0)) * D;
-      kt.fetch(Rows(a.k + at, 2 * (int)kv_stride, x.rows, 2 * D), x.empty);
-      vt.fetch(Rows(a.v + at, 2 * (int)kv_stride, x.rows, 2 * D), x.empty);
-    }
+  auto fetch_q = [&](int n, int g) { qt.fetch(q_rows(a.q, n, g), kBlock - rows_of(n)); };
+  auto fetch_kv = [&](int n) {
+    const int64_t at = (int64_t)(p.row + n * kBlock) * kv_stride + h * D;
+    kt.fetch(Rows(a.k + at, 2 * (int)kv_stride, rows_of(n), 2 * D), kBlock - rows_of(n));
+    vt.fetch(Rows(a.v + at, 2 * (int)kv_stride, rows_of(n), 2 * D), kBlock - rows_of(n));
   };
-  Step now = step_of(0, 0);
-  fetch(now);
-
-  const int col = 32 * wave + l32;
+  // the query head `ahead` steps behind (n, g), if there is one
+  auto fetch_q_ahead = [&](int n, int g, int ahead) {
+    g += ahead;
+    n += g / group;
+    g %= group;
+    if (n < blocks) fetch_q(n, g);
+  };
+  fetch_q(0, 0);
+  fetch_kv(0);
+  const int col = 32 * wave + (lane & 31);
   State<D> s;
-  const int from = REVERSE ? segs.out[p.seg] : segs.in[p.seg];
+  const int from = segs.in[p.seg];
   if (p.pieces > 1) s.template load<TRANSPOSED>(a.inner + ((int64_t)(segs.place0[p.seg] + p.index) * a.heads + h) * D * D, col, hh, 1.f);
   else if (a.first && from >= 0) s.template load<TRANSPOSED>(a.first + ((int64_t)from * a.heads + h) * D * D, col, hh, a.first_scale);
   else s.clear();
-
-  const StateWeights<REVERSE> weights(lg, hh);
-  // Scores are taken in tiles of 32 x 32, 0: (0, 0), 1: the one off the diagonal, 2: (1, 1).  Their weights, as a lane needs them, lie in LDS: on the diagonal, and off it.
-  for (int i = threadIdx.x; i < 2 * 16 * 64; i += 2 * D) {
-    const int l = i >> 2 & 63, j = 8 * (i >> 8 & 3) + 4 * (l >> 5) + (i & 3), far = (REVERSE ? j - (l & 31) : (l & 31) - j) + 32 * (i >> 10);
-    near[i] = far >= 0 ? power(lg, far) : 0.f;
-  }
-  const int off = wave == 1 ? 1024 : 0;  // (with two waves the first takes tiles 0 and 2)
-  const int ti = REVERSE ? wave >> 1 : (wave + 1) >> 1, tj = REVERSE ? (wave + 1) >> 1 : wave >> 1;  // the wave's tile, if it has one
-
+  const StateWeights<false> weights(lg, hh);
+  score_weights<false, 2 * D>(lg, a.scale, near);
   wait_all_but<0>();  // (else the compiler has the loop wait for all loads wherever it uses the state)
-  f32x16 o[2];
+  qt.store(qs);
+  kt.store(ks);
+  vt.store(vs);
+  fetch_q_ahead(0, 0, 1);
+  if (blocks > 1) fetch_kv(1);
+  __syncthreads();
+
   for (int n = 0; n < blocks; ++n) {
+    const int rows = rows_of(n), empty = kBlock - rows;
     for (int g = 0; g < group; ++g) {
       const bool last = g == group - 1;
-      __syncthreads();
-      if (!REVERSE || g == 0) qt.store(qs);
-      if (REVERSE || g == 0) {
-        kt.store(ks);
-        vt.store(vs);
-      }
-      __syncthreads();
-      const Step x = now;
-      if (!last || n + 1 < blocks) {
-        now = step_of(last ? n + 1 : n, last ? 0 : g + 1);
-        fetch(now);
-      }
-      // Scores, transposed (a lane: one row i, four columns j at a time), only tiles with j <= i (backwards j >= i).  Operands are read two stages ahead, here and below.
-      constexpr int kSteps = D / 16, kAhead = 2;
-      auto scores = [&](int off, int ti, int tj) {
-        f32x16 c{};
-        bf16x8 kf[kSteps], qf[kSteps];
-        auto read = [&](int st) {
-          kf[st] = row_operand<D>(ks, 32 * tj, st, lane);
-          qf[st] = row_operand<D>(qs, 32 * ti, st, lane);
-        };
-#pragma unroll
-        for (int st = 0; st < kAhead; ++st) read(st);
-#pragma unroll
-        for (int st = 0; st < kSteps; ++st) {
-          if (st + kAhead < kSteps) read(st + kAhead);
-          __builtin_amdgcn_sched_barrier(0);
-          c = mfma32(kf[st], qf[st], c);
-          __builtin_amdgcn_sched_barrier(0);
-        }
-        f32x4 w[4];
-#pragma unroll
-        for (int q4 = 0; q4 < 4; ++q4) w[q4] = lds_load4f(near + off + q4 * 256 + lane * 4);
-#pragma unroll
-        for (int q4 = 0; q4 < 4; ++q4)
-          *(__attribute__((address_space(3))) bf16x4*)(ps + (l32 * pitch(64) + 4 * hh) + (32 * ti * pitch(64) + 32 * tj + 8 * q4)) =
-              pack4(c[4 * q4] * w[q4][0], c[4 * q4 + 1] * w[q4][1], c[4 * q4 + 2] * w[q4][2], c[4 * q4 + 3] * w[q4][3]);
-      };
-      if (wave < 3) scores(off, ti, tj);
-      if (kWaves == 2 && wave == 0) scores(0, 1, 1);
-      const bool from_state = !REVERSE || g == 0;
-      if (from_state) {
-        bf16x8 qf[kSteps][2];
-        auto read = [&](int st) {
-          qf[st][0] = row_operand<D>(qs, 0, st, lane);
-          qf[st][1] = row_operand<D>(qs, 32, st, lane);
-        };
-        o[0] = o[1] = f32x16{};
-#pragma unroll
-        for (int st = 0; st < kAhead; ++st) read(st);
-#pragma unroll
-        for (int st = 0; st < kSteps; ++st) {
-          if (st + kAhead < kSteps) read(st + kAhead);
-          __builtin_amdgcn_sched_barrier(0);
-          const bf16x8 sb = s.operand(st);
-          o[0] = mfma32(sb, qf[st][0], o[0]);
-          o[1] = mfma32(sb, qf[st][1], o[1]);
-          __builtin_amdgcn_sched_barrier(0);
-        }
-      }
-      if (from_state) {
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const int i = 32 * half + l32 - x.empty;
-          const float by = power(lg, max(REVERSE ? x.rows - 1 - i : i + 1, 0));
-#pragma unroll
-          for (int e = 0; e < 16; ++e) o[half][e] *= by;
-        }
-      }
-      __syncthreads();
+      f32x16 o[2];
       bf16x8 vop[4];
-      {
-        bf16x8 pf[4][2];
-        auto read = [&](int st) {
-          vop[st] = column_operand<D, false>(vs, 16 * st, 32 * wave, lane);
-#pragma unroll
-          for (int half = 0; half < 2; ++half)
-            if (REVERSE ? st >= 2 * half : st < 2 * half + 2) pf[st][half] = row_operand<64>(ps, 32 * half, st, lane);
-        };
-        read(0);
-#pragma unroll
-        for (int st = 0; st < 4; ++st) {
-          if (st < 3) read(st + 1);
-          __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-          for (int half = 0; half < 2; ++half)
-            if (REVERSE ? st >= 2 * half : st < 2 * half + 2) o[half] = mfma32(vop[st], pf[st][half], o[half]);
-          __builtin_amdgcn_sched_barrier(0);
-        }
+      for (int tile = wave; tile < 3; tile += kWaves) scores<D, false>(tile, qs, ks, near, ps, lane);
+      state_outputs<D, false>(s, qs, lg, a.scale, rows, empty, lane, o);
+      __syncthreads();
+      if (!last || n + 1 < blocks) {
+        qt.store(qs);
+        fetch_q_ahead(n, g, 2);
       }
-      if (!REVERSE || last) {
-        const Rows out(a.o + x.row0 * q_stride + (h * q_group + (REVERSE ? 0 : g)) * D, 2 * (int)q_stride, x.rows, 2 * D);
+      score_outputs<D, false>(ps, vs, 32 * wave, lane, o, vop);
+      const Rows out = q_rows(a.o, n, g);
 #pragma unroll
-        for (int half = 0; half < 2; ++half) store_row(out, 32 * half + l32 - x.empty, 64 * wave, o[half], a.scale, hh);
-      }
-      if (REVERSE ? g == 0 : last) s.scale(power(lg, x.rows));
-      if (REVERSE || last) {
+      for (int half = 0; half < 2; ++half) store_rows(out, 32 * half - empty, 64 * wave, o[half], lane);
+      if (last) {
+        s.scale(power(lg, rows));
 #pragma unroll
         for (int st = 0; st < 4; ++st) s.template add<PARTS>(ks, 16 * st, vop[st], weights.lead[st], weights.base, lane);
+        if (n + 1 < blocks) {
+          __syncthreads();
+          kt.store(ks);
+          vt.store(vs);
+          if (n + 2 < blocks) fetch_kv(n + 2);
+        }
       }
+      __syncthreads();
     }
   }
-  const int to = REVERSE ? segs.in[p.seg] : segs.out[p.seg];
-  if (a.last && to >= 0 && p.index == (REVERSE ? 0 : p.pieces - 1)) s.store(a.last + ((int64_t)to * a.heads + h) * D * D, col, hh, a.last_scale);
+  const int to = segs.out[p.seg];
+  if (a.last && to >= 0 && p.index == p.pieces - 1) s.store(a.last + ((int64_t)to * a.heads + h) * D * D, col, hh, a.last_scale);
+}
+
+// The walk backwards: dv (q's role: k; k, v: q, d_o; the state R) and dk (v; d_o, q; R^T), both from the same tiles of q and d_o, which half of the waves take in one role and half in the other
+// (PAIR; head_dim 256, where their states do not fit the registers of one compute unit: a workgroup for each).  What all query heads hand to the key/value head adds up in the accumulators.  With two buffers
+// (head_dim 96 and 128) the next query head's rows are stored while this one's are read.
+struct BackArgs {
+  const __bf16 *q, *k, *v, *d_o;
+  __bf16 *dk, *dv;
+  const float* log_decay;
+  const float* first;
+  float* last;
+  float* inner;
+  int heads, group;
+  float first_scale, last_scale, scale;
+};
+static_assert(sizeof(LinearSegs) + sizeof(BackArgs) <= 3900, "fits the kernel arguments");
+template <int D>
+struct Back {
+  static constexpr int kRoles = D == 256 ? 1 : 2, kThreads = 2 * D * kRoles, kBuffers = D == 96 || D == 128 ? 2 : 1;
+  static constexpr size_t smem = (kRoles + 2 * kBuffers) * tile_bytes(D) + kRoles * tile_bytes(64) + kNear * sizeof(float);
+};
+template <int D, int PARTS>
+__global__ __launch_bounds__(Back<D>::kThreads, 2) void walk_back_kernel(const BackArgs a, const LinearSegs segs) {
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  constexpr int kTile = kBlock * pitch(D), kWaves = D / 32, kRoles = Back<D>::kRoles, kBuffers = Back<D>::kBuffers, kThreads = Back<D>::kThreads;
+  const int lane = threadIdx.x & 63, hh = lane >> 5, wave = (threadIdx.x >> 6) % kWaves;
+  const int role = __builtin_amdgcn_readfirstlane(kRoles == 2 ? (int)(threadIdx.x >> 6) / kWaves : blockIdx.x % 2);  // 0: dv, 1: dk
+  const int index = kRoles == 2 ? blockIdx.x : blockIdx.x / 2, h = index % a.heads;
+  lds_bf16* const own = (lds_bf16*)smem + (kRoles == 2 ? role * kTile : 0);  // k or v
+  lds_bf16* const shared = (lds_bf16*)smem + kRoles * kTile;                 // q and d_o, by turns in two places
+  lds_bf16* const ps = shared + 2 * kBuffers * kTile + (kRoles == 2 ? role * kBlock * pitch(64) : 0);
+  lds_f32* const near = (lds_f32*)((lds_bf16*)smem + (kRoles + 2 * kBuffers) * kTile + kRoles * kBlock * pitch(64));
+  const Piece p = find_piece(segs, index / a.heads);
+  const float lg = log2_decay(a.log_decay, h);
+  const int group = a.group;
+  const int64_t q_stride = (int64_t)a.heads * group * D, kv_stride = (int64_t)a.heads * D;
+  const int blocks = (p.rows + kBlock - 1) / kBlock;
+
+  auto rows_of = [&](int n) { return min(kBlock, p.rows - (blocks - 1 - n) * kBlock); };
+  auto kv_rows = [&](const __bf16* t, int n) {
+    return Rows(t + (int64_t)(p.row + (blocks - 1 - n) * kBlock) * kv_stride + h * D, 2 * (int)kv_stride, rows_of(n), 2 * D);
+  };
+  Tile<D, 2 * D> owned;
+  Tile<D, kThreads> qt, dt;
+  auto fetch = [&](int n, int g, int ahead) {
+    g += ahead;
+    n += g / group;
+    g %= group;
+    if (n >= blocks) return;
+    const int64_t at = (int64_t)(p.row + (blocks - 1 - n) * kBlock) * q_stride + (h * group + g) * D;
+    qt.fetch(Rows(a.q + at, 2 * (int)q_stride, rows_of(n), 2 * D), 0);
+    dt.fetch(Rows(a.d_o + at, 2 * (int)q_stride, rows_of(n), 2 * D), 0);
+  };
+  fetch(0, 0, 0);
+  owned.fetch(kv_rows(role ? a.v : a.k, 0), 0);
+  const int col = 32 * wave + (lane & 31), from = segs.out[p.seg];
+  const bool given = a.first && from >= 0;
+  State<D> s;
+  if (p.pieces > 1 || given) {
+    const float* const at = p.pieces > 1 ? a.inner + ((int64_t)(segs.place0[p.seg] + p.index) * a.heads + h) * D * D : a.first + ((int64_t)from * a.heads + h) * D * D;
+    const float by = p.pieces > 1 ? 1.f : a.first_scale;
+    if (role) s.template load<true>(at, col, hh, by);
+    else s.template load<false>(at, col, hh, by);
+  } else {
+    s.clear();
+  }
+  const StateWeights<true> weights(lg, hh);
+  score_weights<true, kThreads>(lg, a.scale, near);
+  wait_all_but<0>();  // (as in the walk forwards)
+  qt.store(shared);
+  dt.store(shared + kTile);
+  owned.store(own);
+  fetch(0, 0, 1);
+  if (blocks > 1) owned.fetch(kv_rows(role ? a.v : a.k, 1), 0);
+  __syncthreads();
+
+  int turn = 0;
+  for (int n = 0; n < blocks; ++n) {
+    const int rows = rows_of(n);
+    f32x16 o[2];
+    for (int g = 0; g < group; ++g) {
+      const bool last = g == group - 1, more = !last || n + 1 < blocks;
+      const lds_bf16* const ks = shared + (2 * turn + role) * kTile;  // dv: q, dk: d_o
+      const lds_bf16* const vs = shared + (2 * turn + 1 - role) * kTile;
+      bf16x8 vop[4];
+      for (int tile = wave; tile < 3; tile += kWaves) scores<D, true>(tile, own, ks, near, ps, lane);
+      if (g == 0) state_outputs<D, true>(s, own, lg, a.scale, rows, 0, lane, o);
+      if (kBuffers == 2 && more) {
+        qt.store(shared + 2 * (turn ^ 1) * kTile);
+        dt.store(shared + (2 * (turn ^ 1) + 1) * kTile);
+        fetch(n, g, 2);
+      }
+      __syncthreads();
+      if (last && n + 1 < blocks) {
+        owned.store(own);
+        if (n + 2 < blocks) owned.fetch(kv_rows(role ? a.v : a.k, n + 2), 0);
+      }
+      score_outputs<D, true>(ps, vs, 32 * wave, lane, o, vop);
+      if (last) {
+        const Rows out = kv_rows(role ? a.dk : a.dv, n);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) store_rows(out, 32 * half, 64 * wave, o[half], lane);
+      }
+      if (g == 0) s.scale(power(lg, rows));
+#pragma unroll
+      for (int st = 0; st < 4; ++st) s.template add<PARTS>(ks, 16 * st, vop[st], weights.lead[st], weights.base, lane);
+      if (kBuffers == 1 && more) {
+        __syncthreads();
+        qt.store(shared);
+        dt.store(shared + kTile);
+        fetch(n, g, 2);
+      }
+      __syncthreads();
+      if (kBuffers == 2) turn ^= 1;
+    }
+  }
+  const int to = segs.in[p.seg];
+  if (role == 0 && a.last && to >= 0 && p.index == 0) s.store(a.last + ((int64_t)to * a.heads + h) * D * D, col, hh, a.last_scale);
 }
 
 // ---- one token ----
@@ -614,17 +768,6 @@ int check_slots(const chunk_linear_desc* d, bool in_once, bool in_place) {
   return CHUNK_ATTN_OK;
 }
 
-// Rows of a piece: a walk's even share when two walks run on each compute unit (one at head_dim 256).
-int piece_rows(const chunk_linear_desc* d) {
-  int64_t rows = 0, longest = 0;
-  for (int i = 0; i < d->num_segments; ++i) {
-    rows += d->segments[i].len;
-    longest = std::max<int64_t>(longest, d->segments[i].len);
-  }
-  const int64_t share = rows * d->num_kv_heads / (d->head_dim > 128 ? kCus : 2 * kCus);
-  const int64_t blocks = std::max<int64_t>(1, (share + kBlock - 1) / kBlock);
-  return (int)std::min<int64_t>(blocks, (longest + kBlock - 1) / kBlock) * kBlock;
-}
 int pieces_of(int len, int rows) { return (len - 1) / rows + 1; }
 int64_t count_places(const chunk_linear_desc* d, int rows) {
   int64_t n = 0;
@@ -633,6 +776,56 @@ int64_t count_places(const chunk_linear_desc* d, int rows) {
   return n;
 }
 size_t states_bytes(const chunk_linear_desc* d, int64_t n) { return (size_t)n * d->num_kv_heads * d->head_dim * d->head_dim * sizeof(float); }
+
+// What a walk and the sums of its pieces' states take, in us, measured at head_dim 128: a workgroup's start, from zeros or from a state; a block's products for one query head and those it
+// takes once, with few workgroups and with as many as the chip has places for (the memory is then the bound); a block in piece_states_kernel.
+struct WalkCost {
+  double start, start_cut, head[2], block[2], piece_block;
+  int few, places;
+};
+// Rows of a piece: the estimate of all of it that ends first.  Fewer rows: more walks at once, and ends that leave fewer compute units without work; but more states to write, join and read, and k and v
+// are read twice.  A launch takes as long as its work on the places it fills, or as the rounds of its full pieces.
+int piece_rows(const chunk_linear_desc* d, const WalkCost& c) {
+  int longest = 0;
+  int64_t blocks = 0;
+  for (int i = 0; i < d->num_segments; ++i) {
+    longest = std::max(longest, d->segments[i].len);
+    blocks += (d->segments[i].len + kBlock - 1) / kBlock;
+  }
+  const int group = d->num_q_heads / d->num_kv_heads, all = (longest + kBlock - 1) / kBlock;
+  const double heads = d->num_kv_heads;
+  int best = 0;
+  double best_us = 0;
+  for (int m = 1, next = 2;; m = next, next = m < 4 ? m + 1 : m % 3 == 0 ? m / 3 * 4 : m / 2 * 3) {  // 1, 2, 3, 4, 6, 8, 12, 16, 24, ...
+    m = std::min(m, all);
+    const int rows = m * kBlock;
+    int64_t full = 0, pieces = 0, places = 0, summed = 0;
+    for (int i = 0; i < d->num_segments; ++i) {
+      const int len = d->segments[i].len, n = pieces_of(len, rows);
+      full += len / rows;
+      pieces += n;
+      if (n > 1) {
+        places += n;
+        summed += (int64_t)(n - 1) * m;
+      }
+    }
+    const double filled = std::min<double>(pieces * heads, c.places), busy = std::min(1.0, std::max(0.0, (filled - c.few) / std::max(1, c.places - c.few)));
+    const double block = c.block[0] + busy * (c.block[1] - c.block[0]) + group * (c.head[0] + busy * (c.head[1] - c.head[0]));
+    const double start = places > 0 ? c.start_cut : c.start, piece = start + m * block;
+    double us = std::max(std::max(((pieces - places) * c.start + places * c.start_cut + blocks * block) * heads / filled, piece), std::ceil(full * heads / c.places) * piece);
+    if (places > 0) us += 12 + std::max(summed * heads / (2 * kCus), (double)m) * c.piece_block + states_bytes(d, places) * 2 / 5.5e6 + 0.06 * (all / m);
+    if (best == 0 || us < best_us) {
+      best = rows;
+      best_us = us;
+    }
+    if (m == all || blocks / m * heads < 16) break;
+  }
+  return best;
+}
+int forward_rows(const chunk_linear_desc* d) { return piece_rows(d, {3, 9, {2.1, 3.4}, {1.5, 2.0}, 3.0, kCus, d->head_dim > 128 ? kCus : 2 * kCus}); }
+int backward_rows(const chunk_linear_desc* d) {
+  return piece_rows(d, {3, 9, {3.4, 3.4}, {1.0, 1.0}, 3.0 * (d->num_q_heads / d->num_kv_heads), kCus, d->head_dim > 128 ? kCus / 2 : kCus});
+}
 
 template <class F>
 hipError_t by_dim(int d, F&& f) {
@@ -649,43 +842,64 @@ hipError_t launch_piece_states(const WalkArgs& a, const LinearSegs& segs, hipStr
   static const hipError_t attr =
       hipFuncSetAttribute(reinterpret_cast<const void*>(&piece_states_kernel<D, REVERSE, PARTS>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (attr != hipSuccess) return attr;
-  hipLaunchKernelGGL((piece_states_kernel<D, REVERSE, PARTS>), dim3((unsigned)(segs.num_pieces * a.heads)), dim3(2 * D), smem, stream, a, segs);
+  hipLaunchKernelGGL((piece_states_kernel<D, REVERSE, PARTS>), dim3((unsigned)((REVERSE ? segs.num_pieces : segs.num_full) * a.heads)), dim3(2 * D), smem, stream, a, segs);
   hipLaunchKernelGGL((join_states_kernel<REVERSE>), dim3((D * D / 4 + 255) / 256, (unsigned)(segs.n * a.heads)), dim3(256), 0, stream, a, segs, D * D);
   return hipGetLastError();
 }
-template <int D, bool REVERSE, bool TRANSPOSED, int PARTS>
+template <int D, bool TRANSPOSED, int PARTS>
 hipError_t launch_walk(const WalkArgs& a, const LinearSegs& segs, hipStream_t stream) {
-  constexpr size_t smem = 3 * tile_bytes(D) + tile_bytes(kBlock) + 2 * 16 * 64 * sizeof(float);
-  static const hipError_t attr =
-      hipFuncSetAttribute(reinterpret_cast<const void*>(&walk_kernel<D, REVERSE, TRANSPOSED, PARTS>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  constexpr size_t smem = 3 * tile_bytes(D) + tile_bytes(64) + kNear * sizeof(float);
+  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&walk_kernel<D, TRANSPOSED, PARTS>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (attr != hipSuccess) return attr;
-  hipLaunchKernelGGL((walk_kernel<D, REVERSE, TRANSPOSED, PARTS>), dim3((unsigned)(segs.num_pieces * a.heads)), dim3(2 * D), smem, stream, a, segs);
+  hipLaunchKernelGGL((walk_kernel<D, TRANSPOSED, PARTS>), dim3((unsigned)(segs.num_pieces * a.heads)), dim3(2 * D), smem, stream, a, segs);
+  return hipGetLastError();
+}
+template <int D, int PARTS>
+hipError_t launch_walk_back(const BackArgs& a, const LinearSegs& segs, hipStream_t stream) {
+  constexpr size_t smem = Back<D>::smem;
+  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&walk_back_kernel<D, PARTS>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (attr != hipSuccess) return attr;
+  hipLaunchKernelGGL((walk_back_kernel<D, PARTS>), dim3((unsigned)(segs.num_pieces * a.heads * (3 - Back<D>::kRoles))), dim3(Back<D>::kThreads), smem, stream, a, segs);
   return hipGetLastError();
 }
 
-// Goes through the segments, as many at a time as travel with a launch.
+// Goes through the segments, as many at a time as travel with a launch, with whether any of them is cut.  Full pieces start first, the others in falling size: what starts last is short.
 template <class F>
 hipError_t for_segments(const chunk_linear_desc* d, int rows, F&& f) {
+  std::vector<int> order;
+  try {
+    order.resize(d->num_segments);
+  } catch (const std::bad_alloc&) {
+    return hipErrorOutOfMemory;
+  }
+  for (int i = 0; i < d->num_segments; ++i) order[i] = i;
+  std::sort(order.begin(), order.end(), [&](int a, int b) {
+    const int x = d->segments[a].len % rows, y = d->segments[b].len % rows;
+    return x != y ? x > y : a < b;
+  });
   LinearSegs s;
   int64_t places = 0;
   for (int s0 = 0; s0 < d->num_segments; s0 += kLinearSegs) {
     s.n = std::min(kLinearSegs, d->num_segments - s0);
     s.piece_rows = rows;
-    s.num_pieces = 0;
+    s.num_full = s.num_pieces = 0;
     bool cut = false;
     for (int i = 0; i < s.n; ++i) {
-      const chunk_linear_seg& x = d->segments[s0 + i];
+      const chunk_linear_seg& x = d->segments[order[s0 + i]];
       s.start[i] = x.start;
       s.len[i] = x.len;
       s.in[i] = x.state_in;
       s.out[i] = x.state_out;
-      s.piece0[i] = s.num_pieces;
+      s.full0[i] = s.num_full;
       s.place0[i] = (int)places;
-      const int pieces = pieces_of(x.len, rows);
-      s.num_pieces += pieces;
-      if (pieces > 1) places += pieces;
-      cut |= pieces > 1;
+      s.num_full += x.len / rows;
+      s.num_pieces += x.len % rows != 0;
+      if (x.len > rows) {
+        places += pieces_of(x.len, rows);
+        cut = true;
+      }
     }
+    s.num_pieces += s.num_full;
     const hipError_t e = f(s, cut);
     if (e != hipSuccess) return e;
   }
@@ -710,8 +924,8 @@ extern "C" int chunk_linear_workspace_bytes(const chunk_linear_desc* d, size_t* 
   const int rc = chunk_linear_validate(d);
   if (rc != CHUNK_ATTN_OK) return rc;
   if (!fwd_bytes || !bwd_bytes) return CHUNK_ATTN_INVALID_ARG;
-  *fwd_bytes = states_bytes(d, count_places(d, piece_rows(d)));
-  *bwd_bytes = 2 * *fwd_bytes;
+  *fwd_bytes = states_bytes(d, count_places(d, forward_rows(d)));
+  *bwd_bytes = *fwd_bytes + states_bytes(d, count_places(d, backward_rows(d)));
   return CHUNK_ATTN_OK;
 }
 
@@ -724,7 +938,7 @@ extern "C" int chunk_linear_fwd(const chunk_linear_desc* d, const void* q, const
   for (int i = 0; i < d->num_segments; ++i)
     if ((d->segments[i].state_in >= 0 && !states_in) || (d->segments[i].state_out >= 0 && !states_out)) return CHUNK_ATTN_INVALID_ARG;
   if ((rc = check_slots(d, false, states_in == states_out)) != CHUNK_ATTN_OK) return rc;
-  const int rows = piece_rows(d);
+  const int rows = forward_rows(d);
   const size_t need = states_bytes(d, count_places(d, rows));
   if (need > 0) {
     if (!workspace || ((uintptr_t)workspace & 255) != 0) return CHUNK_ATTN_INVALID_ARG;
@@ -739,7 +953,7 @@ extern "C" int chunk_linear_fwd(const chunk_linear_desc* d, const void* q, const
       auto with_parts = [&](auto parts) {
         constexpr int kParts = decltype(parts)::value;
         const hipError_t e = cut ? launch_piece_states<D, false, kParts>(a, segs, stream) : hipSuccess;
-        return e != hipSuccess ? e : launch_walk<D, false, false, kParts>(a, segs, stream);
+        return e != hipSuccess ? e : launch_walk<D, false, kParts>(a, segs, stream);
       };
       return states_out ? with_parts(std::integral_constant<int, 3>{}) : with_parts(std::integral_constant<int, 2>{});
     });
@@ -760,37 +974,44 @@ extern "C" int chunk_linear_bwd(const chunk_linear_desc* d, const void* q, const
     if (d->segments[i].state_in >= 0 && !states_in) return CHUNK_ATTN_INVALID_ARG;
   // (the slots of the gradients: read by state_out, written by state_in)
   if ((rc = check_slots(d, d_states_in != nullptr, d_states_in != nullptr && d_states_in == d_states_out)) != CHUNK_ATTN_OK) return rc;
-  const int rows = piece_rows(d);
-  const size_t need = states_bytes(d, count_places(d, rows));
-  if (need > 0) {
+  const int rows_q = forward_rows(d), rows_kv = backward_rows(d);
+  const size_t need_q = states_bytes(d, count_places(d, rows_q)), need_kv = states_bytes(d, count_places(d, rows_kv));
+  if (need_q + need_kv > 0) {
     if (!workspace || ((uintptr_t)workspace & 255) != 0) return CHUNK_ATTN_INVALID_ARG;
-    if (workspace_bytes < 2 * need) return CHUNK_ATTN_WORKSPACE_TOO_SMALL;
+    if (workspace_bytes < need_q + need_kv) return CHUNK_ATTN_WORKSPACE_TOO_SMALL;
   }
   const __bf16 *bq = (const __bf16*)q, *bk = (const __bf16*)k, *bv = (const __bf16*)v, *bo = (const __bf16*)d_o;
   float* const inner_s = (float*)workspace;
-  float* const inner_r = need > 0 ? inner_s + need / sizeof(float) : nullptr;
+  float* const inner_r = need_kv > 0 ? inner_s + need_q / sizeof(float) : nullptr;
   const int heads = d->num_kv_heads, group = d->num_q_heads / heads;
   const float inv = 1.f / d->scale;
   // The walks' states backwards are the gradients' over `scale`, which all results are multiplied with.
   const WalkArgs s_states{nullptr, bk, bv, nullptr, log_decay, states_in, nullptr, inner_s, heads, group, 1.f, 1.f, d->scale};
   const WalkArgs r_states{nullptr, bq, bo, nullptr, log_decay, d_states_out, nullptr, inner_r, heads, group, inv, d->scale, d->scale};
-  WalkArgs to_q = s_states, to_k = r_states, to_v = r_states;
-  to_q.q = bo; to_q.k = bv; to_q.v = bk; to_q.o = (__bf16*)dq;
-  to_k.q = bv; to_k.k = bo; to_k.v = bq; to_k.o = (__bf16*)dk;
-  to_v.q = bk; to_v.k = bq; to_v.v = bo; to_v.o = (__bf16*)dv;
-  to_v.last = d_states_in;
+  WalkArgs to_q = s_states;
+  to_q.q = bo;
+  to_q.k = bv;
+  to_q.v = bk;
+  to_q.o = (__bf16*)dq;
+  const BackArgs to_kv{bq, bk, bv, bo, (__bf16*)dk, (__bf16*)dv, log_decay, d_states_out, d_states_in, inner_r, heads, group, inv, d->scale, d->scale};
   const hipStream_t stream = (hipStream_t)hip_stream;
-  const hipError_t e = for_segments(d, rows, [&](const LinearSegs& segs, bool cut) {
+  hipError_t e = for_segments(d, rows_q, [&](const LinearSegs& segs, bool cut) {
     return by_dim(d->head_dim, [&](auto dim) {
       constexpr int D = decltype(dim)::value;
-      hipError_t e = hipSuccess;
-      if (cut) {
-        if ((e = launch_piece_states<D, false, 2>(s_states, segs, stream)) != hipSuccess) return e;
-        if ((e = d_states_in ? launch_piece_states<D, true, 3>(r_states, segs, stream) : launch_piece_states<D, true, 2>(r_states, segs, stream)) != hipSuccess) return e;
-      }
-      if ((e = launch_walk<D, false, true, 2>(to_q, segs, stream)) != hipSuccess) return e;
-      if ((e = launch_walk<D, true, true, 2>(to_k, segs, stream)) != hipSuccess) return e;
-      return d_states_in ? launch_walk<D, true, false, 3>(to_v, segs, stream) : launch_walk<D, true, false, 2>(to_v, segs, stream);
+      const hipError_t e = cut ? launch_piece_states<D, false, 2>(s_states, segs, stream) : hipSuccess;
+      return e != hipSuccess ? e : launch_walk<D, true, 2>(to_q, segs, stream);
+    });
+  });
+  if (e != hipSuccess) return report_hip(e, "linear attention backward, dq");
+  e = for_segments(d, rows_kv, [&](const LinearSegs& segs, bool cut) {
+    return by_dim(d->head_dim, [&](auto dim) {
+      constexpr int D = decltype(dim)::value;
+      auto with_parts = [&](auto parts) {
+        constexpr int kParts = decltype(parts)::value;
+        const hipError_t e = cut ? launch_piece_states<D, true, kParts>(r_states, segs, stream) : hipSuccess;
+        return e != hipSuccess ? e : launch_walk_back<D, kParts>(to_kv, segs, stream);
+      };
+      return d_states_in ? with_parts(std::integral_constant<int, 3>{}) : with_parts(std::integral_constant<int, 2>{});
     });
   });
   return e == hipSuccess ? CHUNK_ATTN_OK : report_hip(e, "linear attention backward");

@@ -222,12 +222,19 @@ def test_slices_equal_the_whole_sequence():
             cl.chunk_linear_bwd(desc, q[r], k[r], v[r], lg, states, do[r], grads, dq[r], dk[r], dv[r], grads, ws)
         torch.cuda.synchronize()
         print(cuts, flush=True)
-        # (a slice's blocks begin at its first row: the sums that are rounded differ a little from the uncut sequence's)
-        grow = 1.25
-        close("o", o, want, grow * orc.rounding(q, k, v, lg, scale))
-        close("dq", dq, wants[0], grow * orc.rounding(do, v, k, lg, scale))
-        close("dk", dk, wants[1], grow * orc.rounding(v, do, q, lg, scale, backwards=True))
-        close("dv", dv, wants[2], grow * orc.rounding(k, q, do, lg, scale, backwards=True))
+        # What is rounded follows from the slices: blocks begin at a slice's first row, with the exact state before (behind) the slice.
+        before, behind = [None], [None]
+        for a, b in zip(cuts, cuts[1:]):
+            before.append(orc.forward(q[a:b], k[a:b], v[a:b], lg, scale, before[-1])[1])
+        for a, b in reversed(list(zip(cuts, cuts[1:]))):
+            behind.append(orc.backward(q[a:b], k[a:b], v[a:b], lg, scale, do[a:b], None, behind[-1])[3])
+        behind = behind[-2::-1]
+        for (a, b), S0, dS in zip(zip(cuts, cuts[1:]), before, behind):
+            r = slice(a, b)
+            close("o", o[r], want[r], orc.rounding(q[r], k[r], v[r], lg, scale, S0))
+            close("dq", dq[r], wants[0][r], orc.rounding(do[r], v[r], k[r], lg, scale, None if S0 is None else S0.transpose(1, 2)))
+            close("dk", dk[r], wants[1][r], orc.rounding(v[r], do[r], q[r], lg, scale, None if dS is None else dS.transpose(1, 2) / scale, backwards=True))
+            close("dv", dv[r], wants[2][r], orc.rounding(k[r], q[r], do[r], lg, scale, None if dS is None else dS / scale, backwards=True))
         close_state("state", states[-1], S, size)
         close_state("d_state", grads[0], wants[3], wants[4])
 
