@@ -281,14 +281,14 @@ __global__ __launch_bounds__(256) void join_states_kernel(const WalkArgs a, cons
   const float whole = power(lg, segs.piece_rows);
   f32x4* const x = reinterpret_cast<f32x4*>(a.inner + ((int64_t)segs.place0[seg] * a.heads + h) * elements + at);
   const int64_t apart = (int64_t)a.heads * elements / 4;
-  constexpr int kAhead = 8;  // states are loaded eight at a time: one after the other a sequence of 32 pieces took 20 us
-  for (int n0 = 0; n0 < pieces; n0 += kAhead) {
-    f32x4 own[kAhead];
+  constexpr int kTogether = 8;  // states are loaded eight at a time: one after the other a sequence of 32 pieces took 20 us
+  for (int n0 = 0; n0 < pieces; n0 += kTogether) {
+    f32x4 own[kTogether];
 #pragma unroll
-    for (int n = 0; n < kAhead; ++n)
+    for (int n = 0; n < kTogether; ++n)
       if (n0 + n < pieces - 1) own[n] = x[(REVERSE ? pieces - 1 - n0 - n : n0 + n) * apart];
 #pragma unroll
-    for (int n = 0; n < kAhead; ++n)
+    for (int n = 0; n < kTogether; ++n)
       if (n0 + n < pieces) {
         const int i = REVERSE ? pieces - 1 - n0 - n : n0 + n;
         x[i * apart] = sum;
@@ -325,7 +325,7 @@ __device__ __forceinline__ void store_rows(const Rows& to, int row0, int byte, c
 }
 
 // ---- the three products of a step ----
-constexpr int kAhead = 2;  // stages that operands are read ahead of their products
+constexpr int ahead(int d) { return d < 256 ? 2 : 1; }  // stages that operands are read ahead of their products (as far as there are registers)
 
 // Weights of scores, times the scale of outputs, as a lane needs them: of a tile on the diagonal of the block, and of the one off it ([2][quad of columns][lane][4]).
 constexpr int kNear = 2 * 16 * 64;
@@ -349,15 +349,16 @@ __device__ __forceinline__ void scores(int tile, const lds_bf16* qs, const lds_b
     qf[st] = row_operand<D>(qs, 32 * ti, st, lane);
   };
 #pragma unroll
-  for (int st = 0; st < kAhead; ++st) read(st);
+  for (int st = 0; st < ahead(D); ++st) read(st);
 #pragma unroll
   for (int st = 0; st < kSteps; ++st) {
-    if (st + kAhead < kSteps) read(st + kAhead);
+    if (st + ahead(D) < kSteps) read(st + ahead(D));
     __builtin_amdgcn_sched_barrier(0);
-    (st % 2 ? c1 : c) = mfma32(kf[st], qf[st], st % 2 ? c1 : c);
+    f32x16& sum = D < 256 && st % 2 ? c1 : c;
+    sum = mfma32(kf[st], qf[st], sum);
     __builtin_amdgcn_sched_barrier(0);
   }
-  c += c1;
+  if constexpr (D < 256) c += c1;
   f32x4 w[4];
 #pragma unroll
   for (int q4 = 0; q4 < 4; ++q4) w[q4] = lds_load4f(near + (tile == 1 ? 1024 : 0) + q4 * 256 + lane * 4);
@@ -377,10 +378,10 @@ __device__ __forceinline__ void state_outputs(const State<D>& s, const lds_bf16*
   };
   o[0] = o[1] = f32x16{};
 #pragma unroll
-  for (int st = 0; st < kAhead; ++st) read(st);
+  for (int st = 0; st < ahead(D); ++st) read(st);
 #pragma unroll
   for (int st = 0; st < kSteps; ++st) {
-    if (st + kAhead < kSteps) read(st + kAhead);
+    if (st + ahead(D) < kSteps) read(st + ahead(D));
     __builtin_amdgcn_sched_barrier(0);
     const bf16x8 sb = s.operand(st);
     o[0] = mfma32(sb, qf[st][0], o[0]);
@@ -407,10 +408,10 @@ __device__ __forceinline__ void score_outputs(const lds_bf16* ps, const lds_bf16
       if (pair(st, half)) pf[st][half] = row_operand<64>(ps, 32 * half, st, lane);
   };
 #pragma unroll
-  for (int st = 0; st < kAhead; ++st) read(st);
+  for (int st = 0; st < ahead(D); ++st) read(st);
 #pragma unroll
   for (int st = 0; st < 4; ++st) {
-    if (st + kAhead < 4) read(st + kAhead);
+    if (st + ahead(D) < 4) read(st + ahead(D));
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int half = 0; half < 2; ++half)
@@ -426,6 +427,7 @@ template <int D, bool TRANSPOSED, int PARTS>
 __global__ __launch_bounds__(2 * D, 2) void walk_kernel(const WalkArgs a, const LinearSegs segs) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   constexpr int kTile = kBlock * pitch(D), kWaves = D / 32;
+  constexpr bool kAheadOfBlock = D < 256;  // (at 256 the registers do not hold k and v of the next block as well)
   lds_bf16* const qs = (lds_bf16*)smem;
   lds_bf16* const ks = qs + kTile;
   lds_bf16* const vs = ks + kTile;
@@ -472,7 +474,7 @@ __global__ __launch_bounds__(2 * D, 2) void walk_kernel(const WalkArgs a, const 
   kt.store(ks);
   vt.store(vs);
   fetch_q_ahead(0, 0, 1);
-  if (blocks > 1) fetch_kv(1);
+  if (kAheadOfBlock && blocks > 1) fetch_kv(1);
   __syncthreads();
 
   for (int n = 0; n < blocks; ++n) {
@@ -495,12 +497,13 @@ __global__ __launch_bounds__(2 * D, 2) void walk_kernel(const WalkArgs a, const 
       if (last) {
         s.scale(power(lg, rows));
 #pragma unroll
-        for (int st = 0; st < 4; ++st) s.template add<PARTS>(ks, 16 * st, vop[st], weights.lead[st], weights.base, lane);
+        for (int st = 0; st < 4; ++st) s.template add<PARTS>(ks, 16 * st, D < 256 ? vop[st] : column_operand<D, false>(vs, 16 * st, 32 * wave, lane), weights.lead[st], weights.base, lane);
         if (n + 1 < blocks) {
           __syncthreads();
+          if (!kAheadOfBlock) fetch_kv(n + 1);
           kt.store(ks);
           vt.store(vs);
-          if (n + 2 < blocks) fetch_kv(n + 2);
+          if (kAheadOfBlock && n + 2 < blocks) fetch_kv(n + 2);
         }
       }
       __syncthreads();
@@ -580,8 +583,11 @@ __global__ __launch_bounds__(Back<D>::kThreads, 2) void walk_back_kernel(const B
   qt.store(shared);
   dt.store(shared + kTile);
   owned.store(own);
-  fetch(0, 0, 1);
-  if (blocks > 1) owned.fetch(kv_rows(role ? a.v : a.k, 1), 0);
+  constexpr bool kFetchAhead = D < 256;  // (at 256 the registers do not hold the next rows as well)
+  if (kFetchAhead) {
+    fetch(0, 0, 1);
+    if (blocks > 1) owned.fetch(kv_rows(role ? a.v : a.k, 1), 0);
+  }
   __syncthreads();
 
   int turn = 0;
@@ -602,8 +608,9 @@ __global__ __launch_bounds__(Back<D>::kThreads, 2) void walk_back_kernel(const B
       }
       __syncthreads();
       if (last && n + 1 < blocks) {
+        if (!kFetchAhead) owned.fetch(kv_rows(role ? a.v : a.k, n + 1), 0);
         owned.store(own);
-        if (n + 2 < blocks) owned.fetch(kv_rows(role ? a.v : a.k, n + 2), 0);
+        if (kFetchAhead && n + 2 < blocks) owned.fetch(kv_rows(role ? a.v : a.k, n + 2), 0);
       }
       score_outputs<D, true>(ps, vs, 32 * wave, lane, o, vop);
       if (last) {
@@ -613,12 +620,13 @@ __global__ __launch_bounds__(Back<D>::kThreads, 2) void walk_back_kernel(const B
       }
       if (g == 0) s.scale(power(lg, rows));
 #pragma unroll
-      for (int st = 0; st < 4; ++st) s.template add<PARTS>(ks, 16 * st, vop[st], weights.lead[st], weights.base, lane);
+      for (int st = 0; st < 4; ++st) s.template add<PARTS>(ks, 16 * st, D < 256 ? vop[st] : column_operand<D, false>(vs, 16 * st, 32 * wave, lane), weights.lead[st], weights.base, lane);
       if (kBuffers == 1 && more) {
         __syncthreads();
+        if (!kFetchAhead) fetch(n, g, 1);
         qt.store(shared);
         dt.store(shared + kTile);
-        fetch(n, g, 2);
+        if (kFetchAhead) fetch(n, g, 2);
       }
       __syncthreads();
       if (kBuffers == 2) turn ^= 1;
