@@ -9,6 +9,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "../../include/chunk_rope.h"
 #include "kernels.hpp"
@@ -19,6 +20,8 @@ namespace {
 
 constexpr int kRopeSegs = 192;  // segments that travel with one launch (kernel arguments are limited to 4 KB)
 constexpr int kMaxPairs = 128;
+// Calls that move more than the last-level cache (256 MiB) holds pass their rows by the caches.
+constexpr int64_t kStreamBytes = (int64_t)256 << 20;
 
 struct RopeTensor {
   const void* in;
@@ -41,41 +44,94 @@ struct RopeArgs {
 };
 static_assert(sizeof(RopeArgs) <= 3900, "fits the kernel arguments");
 
-// One token's heads of one tensor.  c, s: cosines and (signed) sines of the lane's pairs, times the magnitude.
-template <bool INTERLEAVED, class T>
+// Eight elements of 16-byte aligned bf16 or float32 rows, by the caches or past them.
+template <bool STREAM, class T>
+__device__ __forceinline__ void load_8(const T* p, float* x) {
+  if constexpr (sizeof(T) == 2) {
+    const bf16x8* const q = reinterpret_cast<const bf16x8*>(p);
+    const bf16x8 v = STREAM ? __builtin_nontemporal_load(q) : *q;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = (float)v[e];
+  } else {  // (two pieces that leave half a line to each other: kept)
+    const f32x4 v0 = reinterpret_cast<const f32x4*>(p)[0], v1 = reinterpret_cast<const f32x4*>(p)[1];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      x[e] = v0[e];
+      x[4 + e] = v1[e];
+    }
+  }
+}
+template <bool STREAM>
+__device__ __forceinline__ void store_8(__bf16* p, const float* x) {
+  bf16x8* const q = reinterpret_cast<bf16x8*>(p);
+  const bf16x8 v = pack8(x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]);
+  if constexpr (STREAM) __builtin_nontemporal_store(v, q);
+  else *q = v;
+}
+
+// How a lane's pieces of eight elements are accessed.  kLoose: some rows or halves of pairs are not 16-byte aligned, or the last piece is shorter.
+enum Access { kLoose, kKeep, kStream };
+template <Access A, class T>
+__device__ __forceinline__ void load_piece(const T* p, int n, float* x) {
+  if constexpr (A == kLoose) load_up_to_8(p, n, x);
+  else load_8<A == kStream>(p, x);
+}
+template <Access A>
+__device__ __forceinline__ void store_piece(__bf16* p, int n, const float* x) {
+  if constexpr (A == kLoose) store_up_to_8(p, n, x);
+  else store_8<A == kStream>(p, x);
+}
+
+// x c + y s, rounded in the same places however the pieces are accessed.
+__device__ __forceinline__ float turned(float x, float y, float c, float s) { return __builtin_fmaf(y, s, x * c); }
+
+// One token's heads of one tensor, as many at a time as are in flight together.  c, s: cosines and (signed) sines of the lane's pairs, times the magnitude.
+template <bool INTERLEAVED, Access A, class T>
 __device__ __forceinline__ void rotate_heads(const T* in, __bf16* out, int heads, int dim, int first_head, int head_step, bool rotates, int at, int n,
                                              int pairs, const float* c, const float* s) {
-  for (int h = first_head; h < heads; h += head_step) {
-    const T* const x = in + (int64_t)h * dim + at;
-    __bf16* const y = out + (int64_t)h * dim + at;
-    float a[8];
-    load_up_to_8(x, n, a);
-    if (rotates) {
+  constexpr int kTogether = 2;
+  const int second = !INTERLEAVED && rotates ? pairs : 0;  // how far the other half of the lane's pairs is; what it copies, it reads once
+  for (int h0 = first_head; h0 < heads; h0 += kTogether * head_step) {
+    float a[kTogether][8], b[kTogether][8];
+#pragma unroll
+    for (int k = 0; k < kTogether; ++k) {
+      const int h = h0 + k * head_step;
+      if (h < heads) {
+        const T* const x = in + (int64_t)h * dim + at;
+        load_piece<A>(x, n, a[k]);
+        if (second) load_piece<A>(x + second, n, b[k]);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kTogether; ++k) {
+      const int h = h0 + k * head_step;
+      if (h >= heads) continue;
+      __bf16* const y = out + (int64_t)h * dim + at;
+      if (!rotates) {
+        store_piece<A>(y, n, a[k]);
+        continue;
+      }
+      float r[8];
       if constexpr (INTERLEAVED) {
-        float r[8];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          r[2 * j] = a[2 * j] * c[j] - a[2 * j + 1] * s[j];
-          r[2 * j + 1] = a[2 * j + 1] * c[j] + a[2 * j] * s[j];
+          r[2 * j] = turned(a[k][2 * j], a[k][2 * j + 1], c[j], -s[j]);
+          r[2 * j + 1] = turned(a[k][2 * j + 1], a[k][2 * j], c[j], s[j]);
         }
-        store_up_to_8(y, n, r);
+        store_piece<A>(y, n, r);
       } else {
-        float b[8], r[8];
-        load_up_to_8(x + pairs, n, b);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) r[j] = a[j] * c[j] - b[j] * s[j];
-        store_up_to_8(y, n, r);
+        for (int j = 0; j < 8; ++j) r[j] = turned(a[k][j], b[k][j], c[j], -s[j]);
+        store_piece<A>(y, n, r);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) r[j] = b[j] * c[j] + a[j] * s[j];
-        store_up_to_8(y + pairs, n, r);
+        for (int j = 0; j < 8; ++j) r[j] = turned(b[k][j], a[k][j], c[j], s[j]);
+        store_piece<A>(y + pairs, n, r);
       }
-    } else {
-      store_up_to_8(y, n, a);
     }
   }
 }
 
-template <bool INTERLEAVED, class TK>
+template <bool INTERLEAVED, Access A, class TK>
 __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a) {
   const int lane = threadIdx.x & 63;
   const int unit = blockIdx.x * 4 + ((int)threadIdx.x >> 6);
@@ -94,10 +150,12 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a) {
   constexpr int kPairs = INTERLEAVED ? 4 : 8;
   float c[kPairs], s[kPairs];
   int at, n;  // the lane's first element of a head, and how many from there on
+  // The last piece of several begins eight elements before the end: what it shares with the one before, both lanes form alike (from the same loads, also in place, as one wave has the whole head).
   if (rotates) {
-    at = 8 * slot;
-    n = min(8, (INTERLEAVED ? 2 * a.pairs : a.pairs) - at);
-    const int first = kPairs * slot;
+    const int end = INTERLEAVED ? 2 * a.pairs : a.pairs;
+    at = max(0, min(8 * slot, end - 8));
+    n = min(8, end);
+    const int first = INTERLEAVED ? at / 2 : at;
 #pragma unroll
     for (int j = 0; j < kPairs; ++j) {
       double t = position * a.turns[first + j < a.pairs ? first + j : 0];
@@ -107,17 +165,25 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a) {
       s[j] *= a.keys_from_buffer ? -a.magnitude : a.magnitude;
     }
   } else {
-    at = 2 * a.pairs + 8 * (slot - a.pair_slots);
-    n = min(8, a.dim - at);
+    const int end = a.dim - 2 * a.pairs;
+    at = 2 * a.pairs + max(0, min(8 * (slot - a.pair_slots), end - 8));
+    n = min(8, end);
   }
   const int first_head = part * a.heads_per_wave + sub, step = a.waves_per_row * a.heads_per_wave;
   if (a.q.in)
-    rotate_heads<INTERLEAVED>((const __bf16*)a.q.in + row * a.q.in_stride, (__bf16*)a.q.out + row * a.q.out_stride, a.q.heads, a.dim, first_head, step, rotates, at, n,
-                              a.pairs, c, s);
+    rotate_heads<INTERLEAVED, A>((const __bf16*)a.q.in + row * a.q.in_stride, (__bf16*)a.q.out + row * a.q.out_stride, a.q.heads, a.dim, first_head, step, rotates, at, n,
+                                 a.pairs, c, s);
   if (a.k.in) {
     const int64_t from = a.keys_from_buffer ? key_row : row, to = a.keys_from_buffer ? row : key_row;
-    rotate_heads<INTERLEAVED>((const TK*)a.k.in + from * a.k.in_stride, (__bf16*)a.k.out + to * a.k.out_stride, a.k.heads, a.dim, first_head, step, rotates, at, n, a.pairs, c, s);
+    rotate_heads<INTERLEAVED, A>((const TK*)a.k.in + from * a.k.in_stride, (__bf16*)a.k.out + to * a.k.out_stride, a.k.heads, a.dim, first_head, step, rotates, at, n, a.pairs, c, s);
   }
+}
+
+template <bool INTERLEAVED, Access A>
+void launch_rope(const RopeArgs& a, bool k_f32, hipStream_t stream) {
+  const dim3 grid((unsigned)(((int64_t)a.rows * a.waves_per_row + 3) / 4));
+  if (k_f32) hipLaunchKernelGGL((rope_kernel<INTERLEAVED, A, float>), grid, dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL((rope_kernel<INTERLEAVED, A, __bf16>), grid, dim3(256), 0, stream, a);
 }
 
 int rope(const chunk_attn_desc* d, const chunk_rope_desc* r, RopeTensor q, RopeTensor k, bool backward, bool k_f32, hipStream_t stream) {
@@ -130,12 +196,16 @@ int rope(const chunk_attn_desc* d, const chunk_rope_desc* r, RopeTensor q, RopeT
   q.heads = d->num_q_heads;
   k.heads = d->num_kv_heads;
   bool copies = false;  // whether the elements behind the pairs have to be moved
+  bool loose = (r->interleaved ? r->rotary_dim : pairs) % 8 != 0;
+  int64_t bytes = 0;
   for (const RopeTensor* t : {&q, &k}) {
     if (!t->in != !t->out) return CHUNK_ATTN_INVALID_ARG;
     if (!t->in) continue;
     const bool f32 = t == &k && k_f32;
     const int64_t least = (int64_t)t->heads * d->head_dim;
     if (t->in_stride < least || t->out_stride < least || ((uintptr_t)t->in & (f32 ? 3 : 1)) != 0 || ((uintptr_t)t->out & 1) != 0) return CHUNK_ATTN_INVALID_ARG;
+    bytes += least * d->total_q * (f32 ? 6 : 4);
+    loose |= (((uintptr_t)t->in | (uintptr_t)t->out) & 15) != 0 || t->in_stride % (f32 ? 4 : 8) != 0 || t->out_stride % 8 != 0;
     if (t->in != t->out) copies = true;
     else if (f32 || t->in_stride != t->out_stride) return CHUNK_ATTN_INVALID_ARG;
   }
@@ -167,14 +237,14 @@ int rope(const chunk_attn_desc* d, const chunk_rope_desc* r, RopeTensor q, RopeT
     a.first_row = segs[0].q_start;
     a.rows = segs[a.num_segs - 1].q_start + segs[a.num_segs - 1].q_len - a.first_row;
     a.waves_per_row = a.rows < 4 * kCus ? 4 : 1;  // few tokens: a token's heads go to four waves
-    const dim3 grid((unsigned)(((int64_t)a.rows * a.waves_per_row + 3) / 4));
-    if (r->interleaved) {
-      if (k_f32) hipLaunchKernelGGL((rope_kernel<true, float>), grid, dim3(256), 0, stream, a);
-      else hipLaunchKernelGGL((rope_kernel<true, __bf16>), grid, dim3(256), 0, stream, a);
-    } else {
-      if (k_f32) hipLaunchKernelGGL((rope_kernel<false, float>), grid, dim3(256), 0, stream, a);
-      else hipLaunchKernelGGL((rope_kernel<false, __bf16>), grid, dim3(256), 0, stream, a);
-    }
+    auto launch = [&](auto access) {
+      constexpr Access A = decltype(access)::value;
+      if (r->interleaved) launch_rope<true, A>(a, k_f32, stream);
+      else launch_rope<false, A>(a, k_f32, stream);
+    };
+    if (loose) launch(std::integral_constant<Access, kLoose>{});
+    else if (bytes > kStreamBytes) launch(std::integral_constant<Access, kStream>{});
+    else launch(std::integral_constant<Access, kKeep>{});
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return report_hip(e, "rotary positions");
   }
