@@ -26,6 +26,7 @@
 #include <cmath>
 #include <initializer_list>
 #include <new>
+#include <type_traits>
 #include <utility>
 #include <vector>
 
@@ -648,21 +649,32 @@ struct StepArgs {
 };
 constexpr int step_groups(int d) { return d == 96 ? 8 : 1024 / d; }  // groups of D / 4 threads; a group takes every step_groups-th row of the state
 constexpr int step_threads(int d) { return d / 4 * step_groups(d); }
-constexpr int kStepHeads = 4;  // query heads at a time
-
-// A workgroup takes one row of the batch and one key/value head: a thread four columns of the state and every so many rows.  Bound by memory (the state, read and written).
-template <int D>
+// A workgroup takes one row of the batch and one key/value head: a thread four columns of the state and every so many rows, up to sixteen of them loaded at once, before anything else; HEADS query
+// heads at a time.  Bound by memory (the state, read and written).  STREAM: states larger than the last-level cache (256 MiB) pass it by.  us, kept / streamed: 128 sequences of 32 heads of 128 (541 MB)
+// 123 / 115, 64 of 16 of 256 (541 MB) 117 / 110; but 16 of 32 of 128 (68 MB) 15 / 21.
+constexpr int64_t kStreamBytes = (int64_t)256 << 20;
+template <int D, int HEADS, bool STREAM>
 __global__ __launch_bounds__(step_threads(D)) void step_kernel(const StepArgs a) {
-  constexpr int kGroups = step_groups(D), kThreads = step_threads(D), kRows = D / kGroups;
-  __shared__ float ks[D], qs[kStepHeads][D], sums[kStepHeads][kGroups][D];
+  constexpr int kGroups = step_groups(D), kThreads = step_threads(D), kRows = D / kGroups, kAtOnce = kRows < 16 ? kRows : 16;
+  __shared__ float ks[D], qs[HEADS][D], sums[HEADS][kGroups][D];
   __shared__ int next_row;
   const int h = blockIdx.x % a.heads, first = blockIdx.x / a.heads, slot = a.slots[first];
   if (slot < 0 || slot >= a.num_states) return;
   const int group = threadIdx.x / (D / 4), col = threadIdx.x % (D / 4) * 4;
-  const int64_t at = ((int64_t)slot * a.heads + h) * D * D;
-  const float decay = power(log2_decay(a.log_decay, h), 1);
+  const int64_t at = ((int64_t)slot * a.heads + h) * D * D + group * D + col;
   const float* from = a.states_in + at;
   float* const to = a.states_out + at;
+  auto load = [](const float* p) {
+    const f32x4* const q = reinterpret_cast<const f32x4*>(p);
+    return STREAM ? __builtin_nontemporal_load(q) : *q;
+  };
+  f32x4 x[kAtOnce];
+  auto load_rows = [&](const float* p, int n0) {
+#pragma unroll
+    for (int n = 0; n < kAtOnce; ++n) x[n] = load(p + (n0 + n) * kGroups * D);
+  };
+  load_rows(from, 0);
+  const float decay = power(log2_decay(a.log_decay, h), 1);
   int row = first;
   if (threadIdx.x == 0) next_row = a.batch;
   __syncthreads();
@@ -677,38 +689,39 @@ __global__ __launch_bounds__(step_threads(D)) void step_kernel(const StepArgs a)
   while (true) {
     const int64_t kv = ((int64_t)row * a.heads + h) * D;
     for (int i = threadIdx.x; i < D; i += kThreads) ks[i] = (float)a.k[kv + i];
-    float v[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = (float)a.v[kv + col + e];
-    for (int g0 = 0; g0 < a.group; g0 += kStepHeads) {
-      const int heads = min(kStepHeads, a.group - g0);
+    const bf16x4 v = *reinterpret_cast<const bf16x4*>(a.v + kv + col);
+    for (int g0 = 0; g0 < a.group; g0 += HEADS) {
+      const int heads = min(HEADS, a.group - g0);
       const int64_t q0 = (((int64_t)row * a.heads + h) * a.group + g0) * D;
       for (int i = threadIdx.x; i < heads * D; i += kThreads) qs[i / D][i % D] = (float)a.q[q0 + i];
       __syncthreads();
-      float acc[kStepHeads][4] = {};
-#pragma unroll 16
-      for (int n = 0; n < kRows; ++n) {
-        const int r = n * kGroups + group;
-        f32x4 x = *reinterpret_cast<const f32x4*>((g0 == 0 ? from : to) + (int64_t)r * D + col);
-        if (g0 == 0) {
-          const float kr = ks[r];
+      float acc[HEADS][4] = {};
+#pragma unroll 1
+      for (int n0 = 0; n0 < kRows; n0 += kAtOnce) {
+        if (n0 > 0 || g0 > 0 || row != first) load_rows(g0 == 0 ? from : to, n0);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) x[e] = x[e] * decay + kr * v[e];
-          *reinterpret_cast<f32x4*>(to + (int64_t)r * D + col) = x;
-        }
+        for (int n = 0; n < kAtOnce; ++n) {
+          const int r = (n0 + n) * kGroups + group;
+          if (g0 == 0) {
+            const float kr = ks[r];
 #pragma unroll
-        for (int g = 0; g < kStepHeads; ++g) {
-          if (g < heads) {
-            const float qr = qs[g][r];
+            for (int e = 0; e < 4; ++e) x[n][e] = x[n][e] * decay + kr * (float)v[e];
+            f32x4* const p = reinterpret_cast<f32x4*>(to + (n0 + n) * kGroups * D);
+            if (STREAM) __builtin_nontemporal_store(x[n], p);
+            else *p = x[n];
+          }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[g][e] += qr * x[e];
+          for (int g = 0; g < HEADS; ++g) {
+            if (HEADS == 1 || g < heads) {
+              const float qr = qs[g][r];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) acc[g][e] += qr * x[n][e];
+            }
           }
         }
       }
 #pragma unroll
-      for (int g = 0; g < kStepHeads; ++g)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sums[g][group][col + e] = acc[g][e];
+      for (int g = 0; g < HEADS; ++g) *reinterpret_cast<f32x4*>(&sums[g][group][col]) = f32x4{acc[g][0], acc[g][1], acc[g][2], acc[g][3]};
       __syncthreads();
       for (int i = threadIdx.x; i < heads * D; i += kThreads) {
         float sum = 0.f;
@@ -1039,7 +1052,16 @@ extern "C" int chunk_linear_step(int32_t batch, int32_t num_q_heads, int32_t num
                    num_q_heads / num_kv_heads, scale};
   const hipError_t e = by_dim(head_dim, [&](auto dim) {
     constexpr int D = decltype(dim)::value;
-    hipLaunchKernelGGL(step_kernel<D>, dim3((unsigned)(batch * num_kv_heads)), dim3(step_threads(D)), 0, (hipStream_t)hip_stream, a);
+    auto launch = [&](auto heads, auto stream) {
+      hipLaunchKernelGGL((step_kernel<D, decltype(heads)::value, decltype(stream)::value>), dim3((unsigned)(batch * num_kv_heads)), dim3(step_threads(D)), 0, (hipStream_t)hip_stream, a);
+    };
+    auto with_heads = [&](auto heads) {
+      if ((int64_t)batch * num_kv_heads * D * D * 8 > kStreamBytes) launch(heads, std::true_type{});
+      else launch(heads, std::false_type{});
+    };
+    if (a.group == 1) with_heads(std::integral_constant<int, 1>{});
+    else if (a.group <= 4) with_heads(std::integral_constant<int, 4>{});
+    else with_heads(std::integral_constant<int, 8>{});
     return hipGetLastError();
   });
   return e == hipSuccess ? CHUNK_ATTN_OK : report_hip(e, "linear attention step");
