@@ -678,7 +678,7 @@ extern "C" int fused_norm_bwd(const fused_norm_desc* d, const void* residual_out
   if (d_post_weight) a.post_parts = (float*)workspace;
   if (d_pre_weight) a.pre_parts = (float*)workspace + groups * d->cols;
   if (d->rows > 0) {
-    a.residual = residual_out;
+    a.residual = d->pre_weight ? residual_out : nullptr;  // (else not wanted)
     a.residual_stride = residual_out_stride;
     a.d_residual_out = d_residual_out;
     a.d_residual_out_stride = d_residual_out_stride;
