@@ -80,7 +80,8 @@ int chunk_linear_bwd(const chunk_linear_desc* desc, const void* q, const void* k
  * One token for each of `batch` sequences whose states lie in slots: q, o [batch][num_q_heads][head_dim], k, v [batch][num_kv_heads][head_dim]; slots
  * [batch] int32, DEVICE.  Reads state slots[i] from states_in, adds token i, writes the state to the same slot of states_out (which may be states_in) and the
  * output to row i of o.  Several rows with the same slot are consecutive tokens of that sequence, in the order of the rows.  A row whose slot is negative or >= num_states
- * is skipped: its row of o stays as it is.  Slots that no row names are not touched.  batch >= 0.
+ * is skipped: its row of o stays as it is.  Slots that no row names are not touched.  batch >= 0, batch * num_kv_heads < 2^24.  Each row looks for its slot in all of `slots`: with some 10^4 rows
+ * of few heads that takes longer than the states do.
  */
 int chunk_linear_step(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, const void* q, const void* k, const void* v,
                       const float* log_decay, const float* states_in, float* states_out, int32_t num_states, const int32_t* slots, void* o, float scale,

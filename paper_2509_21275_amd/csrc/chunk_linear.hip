@@ -1,13 +1,13 @@
 // Linear attention with a decay for each head over the sequences of a chunk (include/chunk_linear.h): forward, backward, and one token at a time.
 //
 // A sequence is taken in blocks of 64 rows.  With S the state before a block of L rows, row i of the block is
-//   o_i = l^(i+1) q_i S + sum_(j<=i) l^(i-j) (q_i . k_j) v_j        and the state behind it        S' = l^L S + sum_j l^(L-1-j) k_j^T v_j,
+//   o_i = scale (l^(i+1) q_i S + sum_(j<=i) l^(i-j) (q_i . k_j) v_j)        and the state behind it        S' = l^L S + sum_j l^(L-1-j) k_j^T v_j,
 // four products of matrices.  A workgroup walks the blocks of a piece of a sequence with S in its accumulators: wave w owns columns 32 w .. 32 w + 31 of S and of the
 // outputs.  All powers of l that occur have exponents >= 0, whatever the decay, and none of more than 64 rows' distance is formed inside a walk.
 //
 // The three gradients are the same walk with other tensors in the roles of q, k and v:
 //   dq: (d_o, v, k), state S^T;   dv: (k, q, d_o) and dk: (v, d_o, q) backwards, from the last row to the first, over rows j >= i; their state is the gradient of S, or its transpose.
-//   Backwards, R before a block (that is, behind its last row) gives   x_i = l^(L-1-i) q_i R + sum_(j>=i) l^(j-i) (q_i . k_j) v_j   and   R' = l^L R + sum_j l^(j+1) k_j^T v_j.
+//   Backwards, R before a block (that is, behind its last row) gives   x_i = l^(L-1-i) q_i R + scale sum_(j>=i) l^(j-i) (q_i . k_j) v_j   and   R' = l^L R + scale sum_j l^(j+1) k_j^T v_j.
 //
 // Long sequences are cut into pieces so that there are enough workgroups.  A first kernel forms each piece's own sum of k^T v, a second one adds them up along the sequence, and the
 // walks then start from there; states of pieces are float32 throughout.
@@ -57,7 +57,7 @@ struct WalkArgs {
   float* last;
   float* inner;              // states of the pieces of cut sequences, [place][kv head][D][D]
   int heads, group;          // key/value heads; query heads to each
-  float first_scale, last_scale, scale;
+  float scale;
 };
 static_assert(sizeof(LinearSegs) + sizeof(WalkArgs) <= 3900, "fits the kernel arguments");
 
@@ -149,7 +149,7 @@ struct State {
     for (int i = 0; i < D / 32; ++i) t[i] = f32x16{};
   }
   template <bool TRANSPOSED>
-  __device__ __forceinline__ void load(const float* from, int col, int hh, float by) {
+  __device__ __forceinline__ void load(const float* from, int col, int hh) {
 #pragma unroll
     for (int i = 0; i < D / 32; ++i)
 #pragma unroll
@@ -160,16 +160,16 @@ struct State {
         else
           for (int r = 0; r < 4; ++r) x[r] = from[(int64_t)(r0 + r) * D + col];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) t[i][4 * g + r] = x[r] * by;
+        for (int r = 0; r < 4; ++r) t[i][4 * g + r] = x[r];
       }
   }
-  __device__ __forceinline__ void store(float* to, int col, int hh, float by) const {
+  __device__ __forceinline__ void store(float* to, int col, int hh) const {
 #pragma unroll
     for (int i = 0; i < D / 32; ++i)
 #pragma unroll
       for (int g = 0; g < 4; ++g)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) to[(int64_t)(row(i, g, hh) + r) * D + col] = t[i][4 * g + r] * by;
+        for (int r = 0; r < 4; ++r) to[(int64_t)(row(i, g, hh) + r) * D + col] = t[i][4 * g + r];
   }
   __device__ __forceinline__ void scale(float by) {
 #pragma unroll
@@ -216,15 +216,15 @@ struct State {
   }
 };
 
-// Weights of a block's rows in its state, l^(63 - j) or backwards l^(j + 1) for row j = 16 s + 8 hh + e: lead[s] * base[e], both powers with exponents >= 0.
+// Weights of a block's rows in its state, l^(63 - j) or backwards (the gradient of S) scale * l^(j + 1) for row j = 16 s + 8 hh + e: lead[s] * base[e], both powers with exponents >= 0.
 template <bool REVERSE>
 struct StateWeights {
   float base[8], lead[4];
-  __device__ __forceinline__ StateWeights(float lg, int hh) {
+  __device__ __forceinline__ StateWeights(float lg, float scale, int hh) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) base[e] = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(power(lg, REVERSE ? e : 7 - e))));
 #pragma unroll
-    for (int s = 0; s < 4; ++s) lead[s] = power(lg, REVERSE ? 16 * s + 8 * hh + 1 : 56 - 16 * s - 8 * hh);
+    for (int s = 0; s < 4; ++s) lead[s] = REVERSE ? scale * power(lg, 16 * s + 8 * hh + 1) : power(lg, 56 - 16 * s - 8 * hh);
   }
 };
 
@@ -241,7 +241,7 @@ __global__ __launch_bounds__(2 * D, 2) void piece_states_kernel(const WalkArgs a
   const float lg = log2_decay(a.log_decay, h);
   const int group = REVERSE ? a.group : 1;
   const int64_t stride = (int64_t)a.heads * group * D;
-  const StateWeights<REVERSE> weights(lg, hh);
+  const StateWeights<REVERSE> weights(lg, a.scale, hh);
   State<D> s;
   s.clear();
   const int blocks = (p.rows + kBlock - 1) / kBlock, steps = blocks * group;
@@ -264,21 +264,21 @@ __global__ __launch_bounds__(2 * D, 2) void piece_states_kernel(const WalkArgs a
 #pragma unroll
     for (int st = 0; st < 4; ++st) s.template add<PARTS>(ks, 16 * st, column_operand<D, false>(vs, 16 * st, 32 * wave, lane), weights.lead[st], weights.base, lane);
   }
-  s.store(a.inner + ((int64_t)(segs.place0[p.seg] + p.index) * a.heads + h) * D * D, 32 * wave + (lane & 31), hh, 1.f);
+  s.store(a.inner + ((int64_t)(segs.place0[p.seg] + p.index) * a.heads + h) * D * D, 32 * wave + (lane & 31), hh);
 }
 
 // Adds them up along each sequence: in the place of each piece's own, the state that it starts from.  (The first one's, too: the slot it comes from may be the one that
 // the last piece's state goes to.)
 template <bool REVERSE>
 __global__ __launch_bounds__(256) void join_states_kernel(const WalkArgs a, const LinearSegs segs, int elements) {
-  const int seg = blockIdx.y / a.heads, h = blockIdx.y % a.heads;
-  const int at = (blockIdx.x * 256 + threadIdx.x) * 4;
+  const int seg = blockIdx.y, h = blockIdx.x % a.heads;
+  const int at = (int)(blockIdx.x / a.heads * 256 + threadIdx.x) * 4;
   const int len = segs.len[seg], pieces = (len + segs.piece_rows - 1) / segs.piece_rows;
   if (pieces == 1 || at >= elements) return;
   const float lg = log2_decay(a.log_decay, h);
   const int slot = REVERSE ? segs.out[seg] : segs.in[seg];
   f32x4 sum{};
-  if (a.first && slot >= 0) sum = *reinterpret_cast<const f32x4*>(a.first + ((int64_t)slot * a.heads + h) * elements + at) * a.first_scale;
+  if (a.first && slot >= 0) sum = *reinterpret_cast<const f32x4*>(a.first + ((int64_t)slot * a.heads + h) * elements + at);
   const float whole = power(lg, segs.piece_rows);
   f32x4* const x = reinterpret_cast<f32x4*>(a.inner + ((int64_t)segs.place0[seg] * a.heads + h) * elements + at);
   const int64_t apart = (int64_t)a.heads * elements / 4;
@@ -368,7 +368,7 @@ __device__ __forceinline__ void scores(int tile, const lds_bf16* qs, const lds_b
   for (int q4 = 0; q4 < 4; ++q4)
     *(__attribute__((address_space(3))) bf16x4*)(to + 8 * q4) = pack4(c[4 * q4] * w[q4][0], c[4 * q4 + 1] * w[q4][1], c[4 * q4 + 2] * w[q4][2], c[4 * q4 + 3] * w[q4][3]);
 }
-// What the state gives the wave's 32 columns, times each row's power of the decay and the scale of outputs.  Rows stand behind `empty` others.
+// What the state gives the wave's 32 columns, times each row's power of the decay and a scale.  Rows stand behind `empty` others.
 template <int D, bool REVERSE>
 __device__ __forceinline__ void state_outputs(const State<D>& s, const lds_bf16* qs, float lg, float scale, int rows, int empty, int lane, f32x16 (&o)[2]) {
   constexpr int kSteps = D / 16;
@@ -465,10 +465,10 @@ __global__ __launch_bounds__(2 * D, 2) void walk_kernel(const WalkArgs a, const 
   const int col = 32 * wave + (lane & 31);
   State<D> s;
   const int from = segs.in[p.seg];
-  if (p.pieces > 1) s.template load<TRANSPOSED>(a.inner + ((int64_t)(segs.place0[p.seg] + p.index) * a.heads + h) * D * D, col, hh, 1.f);
-  else if (a.first && from >= 0) s.template load<TRANSPOSED>(a.first + ((int64_t)from * a.heads + h) * D * D, col, hh, a.first_scale);
+  if (p.pieces > 1) s.template load<TRANSPOSED>(a.inner + ((int64_t)(segs.place0[p.seg] + p.index) * a.heads + h) * D * D, col, hh);
+  else if (a.first && from >= 0) s.template load<TRANSPOSED>(a.first + ((int64_t)from * a.heads + h) * D * D, col, hh);
   else s.clear();
-  const StateWeights<false> weights(lg, hh);
+  const StateWeights<false> weights(lg, 1.f, hh);
   score_weights<false, 2 * D>(lg, a.scale, near);
   wait_all_but<0>();  // (else the compiler has the loop wait for all loads wherever it uses the state)
   qt.store(qs);
@@ -511,7 +511,7 @@ __global__ __launch_bounds__(2 * D, 2) void walk_kernel(const WalkArgs a, const 
     }
   }
   const int to = segs.out[p.seg];
-  if (a.last && to >= 0 && p.index == p.pieces - 1) s.store(a.last + ((int64_t)to * a.heads + h) * D * D, col, hh, a.last_scale);
+  if (a.last && to >= 0 && p.index == p.pieces - 1) s.store(a.last + ((int64_t)to * a.heads + h) * D * D, col, hh);
 }
 
 // The walk backwards: dv (q's role: k; k, v: q, d_o; the state R) and dk (v; d_o, q; R^T), both from the same tiles of q and d_o, which half of the waves take in one role and half in the other
@@ -525,7 +525,7 @@ struct BackArgs {
   float* last;
   float* inner;
   int heads, group;
-  float first_scale, last_scale, scale;
+  float scale;
 };
 static_assert(sizeof(LinearSegs) + sizeof(BackArgs) <= 3900, "fits the kernel arguments");
 template <int D>
@@ -572,13 +572,12 @@ __global__ __launch_bounds__(Back<D>::kThreads, 2) void walk_back_kernel(const B
   State<D> s;
   if (p.pieces > 1 || given) {
     const float* const at = p.pieces > 1 ? a.inner + ((int64_t)(segs.place0[p.seg] + p.index) * a.heads + h) * D * D : a.first + ((int64_t)from * a.heads + h) * D * D;
-    const float by = p.pieces > 1 ? 1.f : a.first_scale;
-    if (role) s.template load<true>(at, col, hh, by);
-    else s.template load<false>(at, col, hh, by);
+    if (role) s.template load<true>(at, col, hh);
+    else s.template load<false>(at, col, hh);
   } else {
     s.clear();
   }
-  const StateWeights<true> weights(lg, hh);
+  const StateWeights<true> weights(lg, a.scale, hh);
   score_weights<true, kThreads>(lg, a.scale, near);
   wait_all_but<0>();  // (as in the walk forwards)
   qt.store(shared);
@@ -601,7 +600,7 @@ __global__ __launch_bounds__(Back<D>::kThreads, 2) void walk_back_kernel(const B
       const lds_bf16* const vs = shared + (2 * turn + 1 - role) * kTile;
       bf16x8 vop[4];
       for (int tile = wave; tile < 3; tile += kWaves) scores<D, true>(tile, own, ks, near, ps, lane);
-      if (g == 0) state_outputs<D, true>(s, own, lg, a.scale, rows, 0, lane, o);
+      if (g == 0) state_outputs<D, true>(s, own, lg, 1.f, rows, 0, lane, o);
       if (kBuffers == 2 && more) {
         qt.store(shared + 2 * (turn ^ 1) * kTile);
         dt.store(shared + (2 * (turn ^ 1) + 1) * kTile);
@@ -634,7 +633,7 @@ __global__ __launch_bounds__(Back<D>::kThreads, 2) void walk_back_kernel(const B
     }
   }
   const int to = segs.in[p.seg];
-  if (role == 0 && a.last && to >= 0 && p.index == 0) s.store(a.last + ((int64_t)to * a.heads + h) * D * D, col, hh, a.last_scale);
+  if (role == 0 && a.last && to >= 0 && p.index == 0) s.store(a.last + ((int64_t)to * a.heads + h) * D * D, col, hh);
 }
 
 // ---- one token ----
@@ -864,7 +863,7 @@ hipError_t launch_piece_states(const WalkArgs& a, const LinearSegs& segs, hipStr
       hipFuncSetAttribute(reinterpret_cast<const void*>(&piece_states_kernel<D, REVERSE, PARTS>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (attr != hipSuccess) return attr;
   hipLaunchKernelGGL((piece_states_kernel<D, REVERSE, PARTS>), dim3((unsigned)((REVERSE ? segs.num_pieces : segs.num_full) * a.heads)), dim3(2 * D), smem, stream, a, segs);
-  hipLaunchKernelGGL((join_states_kernel<REVERSE>), dim3((D * D / 4 + 255) / 256, (unsigned)(segs.n * a.heads)), dim3(256), 0, stream, a, segs, D * D);
+  hipLaunchKernelGGL((join_states_kernel<REVERSE>), dim3((unsigned)((D * D / 4 + 255) / 256 * a.heads), (unsigned)segs.n), dim3(256), 0, stream, a, segs, D * D);
   return hipGetLastError();
 }
 template <int D, bool TRANSPOSED, int PARTS>
@@ -966,7 +965,7 @@ extern "C" int chunk_linear_fwd(const chunk_linear_desc* d, const void* q, const
     if (workspace_bytes < need) return CHUNK_ATTN_WORKSPACE_TOO_SMALL;
   }
   WalkArgs a{(const __bf16*)q, (const __bf16*)k, (const __bf16*)v, (__bf16*)o, log_decay, states_in, states_out, (float*)workspace, d->num_kv_heads,
-             d->num_q_heads / d->num_kv_heads, 1.f, 1.f, d->scale};
+             d->num_q_heads / d->num_kv_heads, d->scale};
   const hipStream_t stream = (hipStream_t)hip_stream;
   const hipError_t e = for_segments(d, rows, [&](const LinearSegs& segs, bool cut) {
     return by_dim(d->head_dim, [&](auto dim) {
@@ -1005,16 +1004,14 @@ extern "C" int chunk_linear_bwd(const chunk_linear_desc* d, const void* q, const
   float* const inner_s = (float*)workspace;
   float* const inner_r = need_kv > 0 ? inner_s + need_q / sizeof(float) : nullptr;
   const int heads = d->num_kv_heads, group = d->num_q_heads / heads;
-  const float inv = 1.f / d->scale;
-  // The walks' states backwards are the gradients' over `scale`, which all results are multiplied with.
-  const WalkArgs s_states{nullptr, bk, bv, nullptr, log_decay, states_in, nullptr, inner_s, heads, group, 1.f, 1.f, d->scale};
-  const WalkArgs r_states{nullptr, bq, bo, nullptr, log_decay, d_states_out, nullptr, inner_r, heads, group, inv, d->scale, d->scale};
+  const WalkArgs s_states{nullptr, bk, bv, nullptr, log_decay, states_in, nullptr, inner_s, heads, group, d->scale};
+  const WalkArgs r_states{nullptr, bq, bo, nullptr, log_decay, d_states_out, nullptr, inner_r, heads, group, d->scale};
   WalkArgs to_q = s_states;
   to_q.q = bo;
   to_q.k = bv;
   to_q.v = bk;
   to_q.o = (__bf16*)dq;
-  const BackArgs to_kv{bq, bk, bv, bo, (__bf16*)dk, (__bf16*)dv, log_decay, d_states_out, d_states_in, inner_r, heads, group, inv, d->scale, d->scale};
+  const BackArgs to_kv{bq, bk, bv, bo, (__bf16*)dk, (__bf16*)dv, log_decay, d_states_out, d_states_in, inner_r, heads, group, d->scale};
   const hipStream_t stream = (hipStream_t)hip_stream;
   hipError_t e = for_segments(d, rows_q, [&](const LinearSegs& segs, bool cut) {
     return by_dim(d->head_dim, [&](auto dim) {
@@ -1046,7 +1043,7 @@ extern "C" int chunk_linear_step(int32_t batch, int32_t num_q_heads, int32_t num
   if (!head_dim_ok(head_dim) || num_q_heads % num_kv_heads != 0) return CHUNK_ATTN_UNSUPPORTED;
   if (batch == 0) return CHUNK_ATTN_OK;
   if (!q || !k || !v || !o || !log_decay || !slots || (num_states > 0 && (!states_in || !states_out)) || !aligned16({q, k, v, o, states_in, states_out}) ||
-      (((uintptr_t)log_decay | (uintptr_t)slots) & 3) != 0 || (int64_t)batch * num_kv_heads > INT32_MAX)
+      (((uintptr_t)log_decay | (uintptr_t)slots) & 3) != 0 || (int64_t)batch * num_kv_heads >= 1 << 24)  // (threads of a launch: below 2^32)
     return CHUNK_ATTN_INVALID_ARG;
   const StepArgs a{(const __bf16*)q, (const __bf16*)k, (const __bf16*)v, log_decay, states_in, states_out, slots, (__bf16*)o, batch, num_states, num_kv_heads,
                    num_q_heads / num_kv_heads, scale};

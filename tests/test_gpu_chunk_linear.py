@@ -127,6 +127,51 @@ def test_many_sequences():
     check(segs, 2, 2, 64, "weak", 300, at)
 
 
+def test_many_heads_and_sequences():
+    """More pairs of a segment and a head than 2^16, one of the sequences cut; some of the heads against the oracle."""
+    from paper_2509_21275_amd import chunk_linear as cl
+    n, more, H, d = 24576, 127, 513, 64
+    total, scale, some = n + more, d ** -0.5, [0, 255, 512]
+    generator = torch.Generator("cuda").manual_seed(3)
+    q, k, v = (torch.randn((total, H, d), generator=generator, device="cuda", dtype=torch.bfloat16) for _ in range(3))
+    o, lg = torch.empty_like(q), torch.full((H,), -0.002, device="cuda")
+    states = torch.full((2, H, d, d), 7.0, device="cuda")
+    states[0].zero_()
+    desc = cl.make_desc([(0, n, 0, 0)] + [(n + i, 1, -1, 1 if i == 9 else -1) for i in range(more)], H, H, d, total, 2, scale)
+    assert cl.chunk_linear_workspace_bytes(desc)[0] > 0  # (it is cut)
+    cl.chunk_linear_fwd(desc, q, k, v, lg, states, o, states, cl.alloc_workspace(desc))
+    torch.cuda.synchronize()
+    q, k, v, o, lg, states = q[:, some], k[:, some], v[:, some], o[:, some], lg[some], states[:, some]
+    want, S, size = orc.forward(q[:n], k[:n], v[:n], lg, scale)
+    close("o", o[:n], want, orc.rounding(q[:n], k[:n], v[:n], lg, scale))
+    close_state("state", states[0], S, size, n)
+    for i in range(n, total):
+        r = slice(i, i + 1)
+        want, S, size = orc.forward(q[r], k[r], v[r], lg, scale)
+        close("o", o[r], want, orc.rounding(q[r], k[r], v[r], lg, scale))
+        if i == n + 9:
+            close_state("state", states[1], S, size)
+
+
+def test_scale_of_no_normal_inverse():
+    """A scale whose inverse is not finite in float32: the gradients of what only the states carry are as they are with any other.  (What the scale multiplies is 2^-120 and less.)"""
+    from paper_2509_21275_amd import chunk_linear as cl
+    for n, d in ((100, 64), (1500, 128)):
+        H, scale = 2, 2.0 ** -130
+        q, k, v, do = (bf16((n, H, d), 30 + i) for i in range(4))
+        lg, ds = torch.full((H,), -0.004, device="cuda"), f32((1, H, d, d), 35)
+        desc = cl.make_desc([(0, n, -1, 0)], H, H, d, n, 1, scale)
+        dq, dk, dv = (torch.empty_like(q) for _ in range(3))
+        print(n, d, flush=True)
+        cl.chunk_linear_bwd(desc, q, k, v, lg, None, do, ds, dq, dk, dv, None, cl.alloc_workspace(desc))
+        torch.cuda.synchronize()
+        none = torch.zeros_like(q)
+        _, wk, wv, _, _ = orc.backward(q, k, v, lg, scale, do, None, ds[0])
+        assert float(dq.abs().max()) < 2.0 ** -100
+        close("dk", dk, wk, orc.rounding(v, none, none, lg, 1.0, ds[0].transpose(1, 2), backwards=True))
+        close("dv", dv, wv, orc.rounding(k, none, none, lg, 1.0, ds[0], backwards=True))
+
+
 def test_rows_past_4_gib():
     """A short sequence at the end of tensors of more than 2^32 bytes."""
     from paper_2509_21275_amd import chunk_linear as cl

@@ -138,7 +138,7 @@ def test_linear_refusals(ca):
     assert all(cl.chunk_linear_validate(desc(s)) == ca.OK for s in ok)
     for kw in (dict(H=0), dict(Hk=0), dict(total=0), dict(states=-1), dict(scale=0.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(segs=())):
         assert cl.chunk_linear_validate(desc(**kw)) == ca.INVALID_ARG, kw
-    for kw in (dict(d=80), dict(d=32), dict(H=3)):
+    for kw in (dict(d=80), dict(d=32), dict(H=3), dict(H=16386)):
         assert cl.chunk_linear_validate(desc(**kw)) == ca.UNSUPPORTED, kw
     for segs in (((0, 0, -1, -1),), ((0, 9, -1, -1),), ((-1, 3, -1, -1),), ((0, 4, -1, -1), (3, 2, -1, -1)), ((4, 2, -1, -1), (0, 2, -1, -1)), ((0, 8, 2, -1),),
                  ((0, 8, -2, -1),), ((0, 8, -1, 2),), ((0, 4, -1, 1), (4, 4, -1, 1)), ((1, 2**31 - 1, -1, -1),)):
@@ -153,7 +153,7 @@ def test_linear_refusals(ca):
 
     one, long = desc(((0, 8, 0, 1),)), desc(((0, 5000, 0, 1),), total=5000)
     f, b = cl.chunk_linear_workspace_bytes(long)
-    assert f > 0 and b == 2 * f and cl.chunk_linear_workspace_bytes(one) == (0, 0)
+    assert b >= f > 0 and cl.chunk_linear_workspace_bytes(one) == (0, 0)
     for kw in (dict(q=None), dict(q=P + 8), dict(lg=None), dict(lg=P + 2), dict(o=None), dict(s_in=None), dict(s_out=None), dict(s_in=P + 4)):
         assert fwd(one, **kw) == ca.INVALID_ARG, kw
     for kw in (dict(q=None), dict(dv=P + 2), dict(s_in=None), dict(ds_in=P + 8)):
