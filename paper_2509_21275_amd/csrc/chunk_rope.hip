@@ -19,6 +19,7 @@ namespace chunk_attn {
 namespace {
 
 constexpr int kRopeSegs = 192;  // segments that travel with one launch (kernel arguments are limited to 4 KB)
+constexpr int kRopeRows = 1 << 25;  // rows of a launch (its threads are limited to 2^32)
 constexpr int kMaxPairs = 128;
 // Calls that move more than the last-level cache (256 MiB) holds pass their rows by the caches.
 constexpr int64_t kStreamBytes = (int64_t)256 << 20;
@@ -234,19 +235,22 @@ int rope(const chunk_attn_desc* d, const chunk_rope_desc* r, RopeTensor q, RopeT
       a.to_position[i] = context - segs[i].q_start;
       a.to_key[i] = segs[i].kv_start + context - segs[i].q_start;
     }
-    a.first_row = segs[0].q_start;
-    a.rows = segs[a.num_segs - 1].q_start + segs[a.num_segs - 1].q_len - a.first_row;
-    a.waves_per_row = a.rows < 4 * kCus ? 4 : 1;  // few tokens: a token's heads go to four waves
-    auto launch = [&](auto access) {
-      constexpr Access A = decltype(access)::value;
-      if (r->interleaved) launch_rope<true, A>(a, k_f32, stream);
-      else launch_rope<false, A>(a, k_f32, stream);
-    };
-    if (loose) launch(std::integral_constant<Access, kLoose>{});
-    else if (bytes > kStreamBytes) launch(std::integral_constant<Access, kStream>{});
-    else launch(std::integral_constant<Access, kKeep>{});
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return report_hip(e, "rotary positions");
+    const int64_t end = (int64_t)segs[a.num_segs - 1].q_start + segs[a.num_segs - 1].q_len;
+    for (int64_t row = segs[0].q_start; row < end; row += kRopeRows) {
+      a.first_row = (int)row;
+      a.rows = (int)std::min<int64_t>(kRopeRows, end - row);
+      a.waves_per_row = a.rows < 4 * kCus ? 4 : 1;  // few tokens: a token's heads go to four waves
+      auto launch = [&](auto access) {
+        constexpr Access A = decltype(access)::value;
+        if (r->interleaved) launch_rope<true, A>(a, k_f32, stream);
+        else launch_rope<false, A>(a, k_f32, stream);
+      };
+      if (loose) launch(std::integral_constant<Access, kLoose>{});
+      else if (bytes > kStreamBytes) launch(std::integral_constant<Access, kStream>{});
+      else launch(std::integral_constant<Access, kKeep>{});
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return report_hip(e, "rotary positions");
+    }
   }
   return CHUNK_ATTN_OK;
 }

@@ -131,6 +131,21 @@ def test_far_positions():
     close(out, orc.rotate(x, orc.positions_and_key_rows(segs)[0], freq, False), orc.size(x, freq, False))
 
 
+def test_more_rows_than_a_launch_takes():
+    """2^26 + 77 tokens of one head (more than 2^32 bytes, several launches of one segment): rows at the ends of launches and the last ones, in place."""
+    import paper_2509_21275_amd as ca
+    from paper_2509_21275_amd import chunk_rope as cr
+    total = (1 << 26) + 77
+    desc = ca.make_desc([(0, total, 0, total)], 1, 1, 64, total, total, 0.1)
+    rope, freq = cr.make_rope(64), np.array(cr.rope_frequencies(64))
+    q = torch.randn((total, 1, 64), generator=torch.Generator("cuda").manual_seed(9), device="cuda", dtype=torch.bfloat16)
+    some = [0, 12345, (1 << 25) - 1, 1 << 25, (1 << 25) + 1, (1 << 26) - 1, 1 << 26, total - 1]
+    x = q[some].double().cpu().numpy()
+    cr.chunk_rope_fwd(desc, rope, q, None, q, None)
+    torch.cuda.synchronize()
+    close(q[some], orc.rotate(x, np.array(some), freq, False), orc.size(x, freq, False))
+
+
 def test_on_another_stream_and_in_a_graph():
     """Queued on a side stream, and captured (with a second table whose segments fill several launches) and replayed with eager work between."""
     import paper_2509_21275_amd as ca
