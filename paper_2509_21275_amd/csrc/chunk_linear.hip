@@ -556,16 +556,18 @@ __global__ __launch_bounds__(Back<D>::kThreads, 2) void walk_back_kernel(const B
   };
   Tile<D, 2 * D> owned;
   Tile<D, kThreads> qt, dt;
-  auto fetch = [&](int n, int g, int ahead) {
-    g += ahead;
-    n += g / group;
-    g %= group;
-    if (n >= blocks) return;
-    const int64_t at = (int64_t)(p.row + (blocks - 1 - n) * kBlock) * q_stride + (h * group + g) * D;
-    qt.fetch(Rows(a.q + at, 2 * (int)q_stride, rows_of(n), 2 * D), 0);
-    dt.fetch(Rows(a.d_o + at, 2 * (int)q_stride, rows_of(n), 2 * D), 0);
+  int next_block = 0, next_head = 0;  // what is fetched next
+  auto fetch = [&] {
+    if (next_block >= blocks) return;
+    const int64_t at = (int64_t)(p.row + (blocks - 1 - next_block) * kBlock) * q_stride + (h * group + next_head) * D;
+    qt.fetch(Rows(a.q + at, 2 * (int)q_stride, rows_of(next_block), 2 * D), 0);
+    dt.fetch(Rows(a.d_o + at, 2 * (int)q_stride, rows_of(next_block), 2 * D), 0);
+    if (++next_head == group) {
+      next_head = 0;
+      ++next_block;
+    }
   };
-  fetch(0, 0, 0);
+  fetch();
   owned.fetch(kv_rows(role ? a.v : a.k, 0), 0);
   const int col = 32 * wave + (lane & 31), from = segs.out[p.seg];
   const bool given = a.first && from >= 0;
@@ -585,7 +587,7 @@ __global__ __launch_bounds__(Back<D>::kThreads, 2) void walk_back_kernel(const B
   owned.store(own);
   constexpr bool kFetchAhead = D < 256;  // (at 256 the registers do not hold the next rows as well)
   if (kFetchAhead) {
-    fetch(0, 0, 1);
+    fetch();
     if (blocks > 1) owned.fetch(kv_rows(role ? a.v : a.k, 1), 0);
   }
   __syncthreads();
@@ -601,17 +603,18 @@ __global__ __launch_bounds__(Back<D>::kThreads, 2) void walk_back_kernel(const B
       bf16x8 vop[4];
       for (int tile = wave; tile < 3; tile += kWaves) scores<D, true>(tile, own, ks, near, ps, lane);
       if (g == 0) state_outputs<D, true>(s, own, lg, 1.f, rows, 0, lane, o);
-      if (kBuffers == 2 && more) {
+      auto store_next = [&] {
         qt.store(shared + 2 * (turn ^ 1) * kTile);
         dt.store(shared + (2 * (turn ^ 1) + 1) * kTile);
-        fetch(n, g, 2);
-      }
+        fetch();
+      };
       __syncthreads();
       if (last && n + 1 < blocks) {
         if (!kFetchAhead) owned.fetch(kv_rows(role ? a.v : a.k, n + 1), 0);
         owned.store(own);
         if (kFetchAhead && n + 2 < blocks) owned.fetch(kv_rows(role ? a.v : a.k, n + 2), 0);
       }
+      if (kBuffers == 2 && more && role == 0) store_next();  // (while the other half's products run, which stores when this half's run)
       score_outputs<D, true>(ps, vs, 32 * wave, lane, o, vop);
       if (last) {
         const Rows out = kv_rows(role ? a.dk : a.dv, n);
@@ -621,12 +624,13 @@ __global__ __launch_bounds__(Back<D>::kThreads, 2) void walk_back_kernel(const B
       if (g == 0) s.scale(power(lg, rows));
 #pragma unroll
       for (int st = 0; st < 4; ++st) s.template add<PARTS>(ks, 16 * st, D < 256 ? vop[st] : column_operand<D, false>(vs, 16 * st, 32 * wave, lane), weights.lead[st], weights.base, lane);
+      if (kBuffers == 2 && more && role == 1) store_next();
       if (kBuffers == 1 && more) {
         __syncthreads();
-        if (!kFetchAhead) fetch(n, g, 1);
+        if (!kFetchAhead) fetch();
         qt.store(shared);
         dt.store(shared + kTile);
-        if (kFetchAhead) fetch(n, g, 2);
+        if (kFetchAhead) fetch();
       }
       __syncthreads();
       if (kBuffers == 2) turn ^= 1;
