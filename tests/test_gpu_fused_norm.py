@@ -206,3 +206,25 @@ def test_no_rows_zero_rows_and_values_that_are_not_numbers():
         assert all(torch.equal(a[keep], b[keep]) for a, b in zip(got, want))
         assert all(bool(torch.isfinite(t[3]).all()) for t in got) and all(bool((t[3] == 0).all()) for t in got[:2])
         assert bool(torch.isnan(got[0][5]).all()) and bool(torch.isnan(got[1][5]).all())
+
+
+@pytest.mark.parametrize("cols", [80, 256, 1024, 8192, 16384])
+@pytest.mark.parametrize("wtype", [torch.bfloat16, torch.float32])
+def test_weights_at_any_address(cols, wtype):
+    """Weights that begin one element behind an aligned address (a row of a stacked parameter), and their gradients too: the bits of aligned ones."""
+    from paper_2509_21275_amd import fused_norm as fn
+    rows = 9
+    y, gate, residual, post, pre = case(rows, cols, {}, "silu", torch.bfloat16, wtype, 0, cols)
+    d_out, d_h, ws = make(rows, cols, 6), make(rows, cols, 7), fn.alloc_workspace(rows, cols)
+    results = []
+    for shift in (0, 1):
+        w = [torch.cat([t.new_full((shift,), float("nan")), t])[shift:] for t in (post, pre)]
+        assert all(t.data_ptr() % 16 == shift * t.element_size() for t in w)
+        out, h, dy, dg, dr = (torch.empty_like(y) for _ in range(5))
+        dw = [torch.full((cols + shift,), 7.0, device="cuda")[shift:] for _ in range(2)]
+        print(cols, wtype, shift, flush=True)
+        fn.fused_norm_fwd(y, gate, residual, *w, out, h, gate_kind="silu")
+        fn.fused_norm_bwd(y, gate, out, *w, d_out, d_h, dy, dg, dr, *dw, ws, gate_kind="silu")
+        torch.cuda.synchronize()
+        results.append((out, h, dy, dg, dr, *dw))
+    assert all(torch.equal(a, b) for a, b in zip(*results))
