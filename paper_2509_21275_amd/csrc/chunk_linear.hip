@@ -17,9 +17,16 @@
 // they are: transposed reads deliver column quads 0, 2, 1, 3.  Outputs are formed transposed (columns = tokens), so that the power of l a row is multiplied with is one
 // value of a lane, and four neighbouring elements of an output row lie in a lane.
 //
-// Precision: k_j^T (l^(L-1-j) v_j) has the weighted v_j as a bf16 operand.  Rounded once it would leave states with 2^-9 relative error, so it is split into three bf16 terms
-// (24 bits): the state is then as exact as float32 sums are, for three times its MFMAs (48 of 78 in a block at head_dim 128, where memory is the bound).  S and the weighted scores are
-// rounded to bf16 once where they are operands of an output's product.
+// Precision: k_j^T (l^(L-1-j) v_j) has the weighted v_j as a bf16 operand.  Rounded once it would leave states with up to 2^-8 of relative error, so it is split into PARTS bf16 terms: three (24 bits)
+// where the call leaves states or their gradients, which are then as exact as float32 sums are; two (2^-16) where they only pass on inside the call, to where they are rounded to an
+// operand (2^-8).  S and the weighted scores are rounded to bf16 once where they are operands of an output's product.  At head_dim 128 the terms are 48 (two: 32) of the 76 (60)
+// products of a wave in a block.
+//
+// Measured (us; head_dim 128 unless said).  Forward, 65536 tokens in 20 sequences, 32/8 heads: 391, of that the walk 320 (1.34 GB, 4.2 TB/s), the pieces' sums 75 and 12; 8192 tokens of 32/32
+// 96 (walk 55 of 268 MB, sums 30 and 11), with states left 113.  Bound by memory while all places are filled; starts (9 of a piece's 30 - 60) and unequal ends are what is above it.
+// Backward, 16384 tokens of 32/8 in 8 sequences: 330 - 360 by the box, walk_back 160, dq's walk 81, sums 68 + 23 and 16 + 13.  walk_back's 103 GFLOP (terms counted) run at 0.65 PFLOP/s, in
+// its loops at 0.9, where a large product of matrices reaches 1.1: the clock that the chip's power leaves (1.8 GHz) bounds it, not the chain of a step (a sixth fewer cycles
+// per step left the time where it was).  head_dim 256: 8192 tokens of 16/16, forward 163, backward 430 - 455; its walks spill (36 and 73 registers).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -808,7 +815,8 @@ struct WalkCost {
   int few, places;
 };
 // Rows of a piece: the estimate of all of it that ends first.  Fewer rows: more walks at once, and ends that leave fewer compute units without work; but more states to write, join and read, and k and v
-// are read twice.  A launch takes as long as its work on the places it fills, or as the rounds of its full pieces.
+// are read twice.  A launch takes as long as its work on the places it fills, or as the rounds of its full pieces.  us by rows of a piece (* chosen): 8192 tokens of 32/32 of 128, forward, 256: 120, *512: 96,
+// 1024: 101, uncut: 343; 16384 in 8 sequences of 32/8, backward, 128: 389, *256: 341, 1024: 427, uncut: 2146; 32 sequences of 2000 of 32/8, backward, 512: 1044, *uncut: 741.
 int piece_rows(const chunk_linear_desc* d, const WalkCost& c) {
   int longest = 0;
   int64_t blocks = 0;

@@ -21,7 +21,8 @@ namespace {
 constexpr int kRopeSegs = 192;  // segments that travel with one launch (kernel arguments are limited to 4 KB)
 constexpr int kRopeRows = 1 << 25;  // rows of a launch (its threads are limited to 2^32)
 constexpr int kMaxPairs = 128;
-// Calls that move more than the last-level cache (256 MiB) holds pass their rows by the caches.
+// Calls that move more than the last-level cache (256 MiB) holds pass their rows by the caches.  us, kept / streamed, 32/8 heads of 128: 4096 tokens (84 MB) 16.2 / 17.6; 16384 (336 MB) 65 / 62, 5.4 TB/s;
+// 65536 (1.34 GB) 246 / 221, 6.1 TB/s; backward of 65536 with float32 dk (1.48 GB) 267 / 253.  Loose pieces are kept: 65536 tokens with rotary_dim 126 397, 3.4 TB/s, 38 of 96 192, 5.2.
 constexpr int64_t kStreamBytes = (int64_t)256 << 20;
 
 struct RopeTensor {

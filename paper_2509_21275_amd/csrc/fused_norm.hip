@@ -3,7 +3,10 @@
 // Bound by memory: every given tensor is read or written once.  A group of TPR lanes holds a row in registers, eight neighbouring elements to a lane
 // and chunk (16 bytes of bf16), NCH chunks, so that the statistics cost no second read: the forward forms the mean square of y, then that of r'; the backward forms in one
 // sum over the row all that t needs, and in a second one what dy needs.  Groups walk the rows with a grid stride and keep their weights and the sums of the
-// weights' gradients in registers; the latter go to the workspace, one row of sums for each workgroup, and a second kernel adds those in a fixed order.
+// weights' gradients in registers (long rows: the sums in LDS, see NormBack); the latter go to the workspace, one row of sums for each workgroup, and a second kernel adds those in a fixed order.
+//
+// Measured: 16384 rows of 4096, forward with a gate (671 MB) 130 us, 5.2 TB/s; 8191 of 8192, backward with float32 residuals (1.21 GB) 233 us, 5.2; 524288 of 128, backward (671 MB) 126 us, 5.3;
+// 64 rows 9 us, which is the host's part.  Loose rows take an access for each element: 1.7 - 2.9 TB/s (16384 of 4095, backward, 231 us).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
