@@ -10,7 +10,7 @@
 //   Backwards, R before a block (that is, behind its last row) gives   x_i = l^(L-1-i) q_i R + scale sum_(j>=i) l^(j-i) (q_i . k_j) v_j   and   R' = l^L R + scale sum_j l^(j+1) k_j^T v_j.
 //
 // Long sequences are cut into pieces so that there are enough workgroups.  A first kernel forms each piece's own sum of k^T v, a second one adds them up along the sequence, and the
-// walks then start from there; states of pieces are float32 throughout.
+// walks then start from there (forwards, with few pieces and small states, the walks add them up themselves: kDirect); states of pieces are float32 throughout.
 //
 // Accumulators as operands: an accumulator tile holds S[row][column = lane % 32], and the eight values of a lane in one half of it are what an MFMA operand wants of 16 rows, if
 // only the rows are named accordingly (device_common.hpp, "C-order").  Here the rows of K^T are fed to the state's product in the order that makes the names come out as
@@ -65,6 +65,7 @@ struct WalkArgs {
   float* inner;              // states of the pieces of cut sequences, [place][kv head][D][D]
   int heads, group;          // key/value heads; query heads to each
   float scale;
+  int direct;                // whether walks add up the sums of the pieces before theirs themselves
 };
 static_assert(sizeof(LinearSegs) + sizeof(WalkArgs) <= 3900, "fits the kernel arguments");
 
@@ -178,6 +179,38 @@ struct State {
 #pragma unroll
         for (int r = 0; r < 4; ++r) to[(int64_t)(row(i, g, hh) + r) * D + col] = t[i][4 * g + r];
   }
+  // As the waves hold it, [wave][tile][quad of rows][lane][4]: 16 bytes to a lane, next to its neighbours'.
+  static __device__ __forceinline__ f32x4* own(float* state, int wave, int lane) { return reinterpret_cast<f32x4*>(state) + wave * (D / 8) * 64 + lane; }
+  __device__ __forceinline__ void load_own(float* state, int wave, int lane) {
+    const f32x4* const from = own(state, wave, lane);
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 x = from[(4 * i + g) * 64];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) t[i][4 * g + r] = x[r];
+      }
+  }
+  __device__ __forceinline__ void store_own(float* state, int wave, int lane) const {
+    f32x4* const to = own(state, wave, lane);
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) to[(4 * i + g) * 64] = f32x4{t[i][4 * g], t[i][4 * g + 1], t[i][4 * g + 2], t[i][4 * g + 3]};
+  }
+  // by times it, and another one
+  __device__ __forceinline__ void scale_and_add_own(float by, float* state, int wave, int lane) {
+    const f32x4* const from = own(state, wave, lane);
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 x = from[(4 * i + g) * 64];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) t[i][4 * g + r] = t[i][4 * g + r] * by + x[r];
+      }
+  }
   __device__ __forceinline__ void scale(float by) {
 #pragma unroll
     for (int i = 0; i < D / 32; ++i)
@@ -236,7 +269,7 @@ struct StateWeights {
 };
 
 // Each piece's own k^T v into its place in the workspace, but for the one at the far end of its sequence, whose nobody needs, and for sequences of one piece.
-template <int D, bool REVERSE, int PARTS>
+template <int D, bool REVERSE, bool TRANSPOSED, int PARTS>
 __global__ __launch_bounds__(2 * D, 2) void piece_states_kernel(const WalkArgs a, const LinearSegs segs) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   lds_bf16* const ks = (lds_bf16*)smem;
@@ -249,8 +282,17 @@ __global__ __launch_bounds__(2 * D, 2) void piece_states_kernel(const WalkArgs a
   const int group = REVERSE ? a.group : 1;
   const int64_t stride = (int64_t)a.heads * group * D;
   const StateWeights<REVERSE> weights(lg, a.scale, hh);
+  float* const place = a.inner + ((int64_t)(segs.place0[p.seg] + p.index) * a.heads + h) * D * D;
+  const int col = 32 * wave + (lane & 31);
   State<D> s;
-  s.clear();
+  const int from = REVERSE ? -1 : segs.in[p.seg];
+  if (!REVERSE && D < 256 && a.direct && p.index == 0 && a.first && from >= 0) {
+    // The state before the sequence goes into the first piece's sum, and into the last place, which no sum takes, for the first piece's walk (the slot may be where the last one's walk leaves its own).
+    s.template load<TRANSPOSED>(a.first + ((int64_t)from * a.heads + h) * D * D, col, hh);
+    s.store_own(place + (int64_t)(p.pieces - 1) * a.heads * D * D, wave, lane);
+  } else {
+    s.clear();
+  }
   const int blocks = (p.rows + kBlock - 1) / kBlock, steps = blocks * group;
   Tile<D> kt, vt;
   auto fetch = [&](int step) {
@@ -271,13 +313,15 @@ __global__ __launch_bounds__(2 * D, 2) void piece_states_kernel(const WalkArgs a
 #pragma unroll
     for (int st = 0; st < 4; ++st) s.template add<PARTS>(ks, 16 * st, column_operand<D, false>(vs, 16 * st, 32 * wave, lane), weights.lead[st], weights.base, lane);
   }
-  s.store(a.inner + ((int64_t)(segs.place0[p.seg] + p.index) * a.heads + h) * D * D, 32 * wave + (lane & 31), hh);
+  if constexpr (REVERSE) s.store(place, col, hh);
+  else s.store_own(place, wave, lane);
 }
 
 // Adds them up along each sequence: in the place of each piece's own, the state that it starts from.  (The first one's, too: the slot it comes from may be the one that
 // the last piece's state goes to.)
-template <bool REVERSE>
-__global__ __launch_bounds__(256) void join_states_kernel(const WalkArgs a, const LinearSegs segs, int elements) {
+template <int D, bool REVERSE, bool TRANSPOSED>
+__global__ __launch_bounds__(256) void join_states_kernel(const WalkArgs a, const LinearSegs segs) {
+  constexpr int elements = D * D;
   const int seg = blockIdx.y, h = blockIdx.x % a.heads;
   const int at = (int)(blockIdx.x / a.heads * 256 + threadIdx.x) * 4;
   const int len = segs.len[seg], pieces = (len + segs.piece_rows - 1) / segs.piece_rows;
@@ -285,22 +329,35 @@ __global__ __launch_bounds__(256) void join_states_kernel(const WalkArgs a, cons
   const float lg = log2_decay(a.log_decay, h);
   const int slot = REVERSE ? segs.out[seg] : segs.in[seg];
   f32x4 sum{};
-  if (a.first && slot >= 0) sum = *reinterpret_cast<const f32x4*>(a.first + ((int64_t)slot * a.heads + h) * elements + at);
-  const float whole = power(lg, segs.piece_rows);
-  f32x4* const x = reinterpret_cast<f32x4*>(a.inner + ((int64_t)segs.place0[seg] * a.heads + h) * elements + at);
-  const int64_t apart = (int64_t)a.heads * elements / 4;
+  if (a.first && slot >= 0) {
+    const float* const from = a.first + ((int64_t)slot * a.heads + h) * elements;
+    if constexpr (REVERSE) {
+      sum = *reinterpret_cast<const f32x4*>(from + at);
+    } else {  // (forward places are in the waves' order)
+      const int lane = at / 4 % 64, g = at / 256 % 4, i = at / 1024 % (D / 32), wave = at / (32 * D);
+      const int col = 32 * wave + lane % 32, row = State<D>::row(i, g, lane / 32);
+      if constexpr (TRANSPOSED) {
+        sum = *reinterpret_cast<const f32x4*>(from + col * D + row);
+      } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sum[r] = from[(row + r) * D + col];
+      }
+    }
+  }
+  const float whole = power(lg, segs.piece_rows), first = REVERSE ? power(lg, len - (pieces - 1) * segs.piece_rows) : whole;
+  const int64_t apart = (int64_t)a.heads * elements / 4 * (REVERSE ? -1 : 1);
+  f32x4* x = reinterpret_cast<f32x4*>(a.inner + ((int64_t)segs.place0[seg] * a.heads + h) * elements + at) - (REVERSE ? (pieces - 1) * apart : 0);
   constexpr int kTogether = 8;  // states are loaded eight at a time: one after the other a sequence of 32 pieces took 20 us
-  for (int n0 = 0; n0 < pieces; n0 += kTogether) {
+  for (int n0 = 0; n0 < pieces; n0 += kTogether, x += kTogether * apart) {
     f32x4 own[kTogether];
 #pragma unroll
     for (int n = 0; n < kTogether; ++n)
-      if (n0 + n < pieces - 1) own[n] = x[(REVERSE ? pieces - 1 - n0 - n : n0 + n) * apart];
+      if (n0 + n < pieces - 1) own[n] = x[n * apart];
 #pragma unroll
     for (int n = 0; n < kTogether; ++n)
       if (n0 + n < pieces) {
-        const int i = REVERSE ? pieces - 1 - n0 - n : n0 + n;
-        x[i * apart] = sum;
-        if (n0 + n < pieces - 1) sum = sum * (i == pieces - 1 ? power(lg, len - i * segs.piece_rows) : whole) + own[n];
+        x[n * apart] = sum;
+        if (n0 + n < pieces - 1) sum = sum * (n0 + n == 0 ? first : whole) + own[n];
       }
   }
 }
@@ -472,8 +529,16 @@ __global__ __launch_bounds__(2 * D, 2) void walk_kernel(const WalkArgs a, const 
   const int col = 32 * wave + (lane & 31);
   State<D> s;
   const int from = segs.in[p.seg];
-  if (p.pieces > 1) s.template load<TRANSPOSED>(a.inner + ((int64_t)(segs.place0[p.seg] + p.index) * a.heads + h) * D * D, col, hh);
-  else if (a.first && from >= 0) s.template load<TRANSPOSED>(a.first + ((int64_t)from * a.heads + h) * D * D, col, hh);
+  const bool direct = D < 256 && a.direct;
+  if (p.pieces > 1 && (!direct || p.index > 0 || (a.first && from >= 0))) {
+    const int64_t apart = (int64_t)a.heads * D * D;
+    float* const sums = a.inner + segs.place0[p.seg] * apart + (int64_t)h * D * D;
+    s.load_own(sums + (!direct ? p.index : p.index > 0 ? 0 : p.pieces - 1) * apart, wave, lane);
+    if (direct) {
+      const float whole = power(lg, segs.piece_rows);
+      for (int i = 1; i < p.index; ++i) s.scale_and_add_own(whole, sums + i * apart, wave, lane);
+    }
+  } else if (p.pieces == 1 && a.first && from >= 0) s.template load<TRANSPOSED>(a.first + ((int64_t)from * a.heads + h) * D * D, col, hh);
   else s.clear();
   const StateWeights<false> weights(lg, 1.f, hh);
   score_weights<false, 2 * D>(lg, a.scale, near);
@@ -859,6 +924,11 @@ int backward_rows(const chunk_linear_desc* d) {
   return piece_rows(d, {3, 9, {3.4, 3.4}, {1.0, 1.0}, 3.0 * (d->num_q_heads / d->num_kv_heads), kCus, d->head_dim > 128 ? kCus / 2 : kCus});
 }
 
+// Up to this many elements of sums before a piece its walk adds them up itself, which saves a launch.  us, added up by join_states_kernel / by the walks: four sequences of 128 - 512 tokens, 8 heads of 64
+// (up to 8 pieces), 16.4 / 13.2; 8 of 2000, 8 heads of 64, 33.1 / 30.2; 16384 tokens, 32 heads of 64, 84 / 81; but 4096 tokens, 8 heads of 64 in 64 pieces 21.4 / 25.6, 16384 of 32/8 of 128
+// in 64 121 / 141.  Not at head_dim 256, whose walks have no registers for it.
+constexpr int kDirect = 5 * 128 * 128;
+
 template <class F>
 hipError_t by_dim(int d, F&& f) {
   using std::integral_constant;
@@ -868,14 +938,15 @@ hipError_t by_dim(int d, F&& f) {
   return f(integral_constant<int, 256>{});
 }
 
-template <int D, bool REVERSE, int PARTS>
+template <int D, bool REVERSE, bool TRANSPOSED, int PARTS>
 hipError_t launch_piece_states(const WalkArgs& a, const LinearSegs& segs, hipStream_t stream) {
   constexpr size_t smem = 2 * tile_bytes(D);
   static const hipError_t attr =
-      hipFuncSetAttribute(reinterpret_cast<const void*>(&piece_states_kernel<D, REVERSE, PARTS>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+      hipFuncSetAttribute(reinterpret_cast<const void*>(&piece_states_kernel<D, REVERSE, TRANSPOSED, PARTS>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (attr != hipSuccess) return attr;
-  hipLaunchKernelGGL((piece_states_kernel<D, REVERSE, PARTS>), dim3((unsigned)((REVERSE ? segs.num_pieces : segs.num_full) * a.heads)), dim3(2 * D), smem, stream, a, segs);
-  hipLaunchKernelGGL((join_states_kernel<REVERSE>), dim3((unsigned)((D * D / 4 + 255) / 256 * a.heads), (unsigned)segs.n), dim3(256), 0, stream, a, segs, D * D);
+  hipLaunchKernelGGL((piece_states_kernel<D, REVERSE, TRANSPOSED, PARTS>), dim3((unsigned)((REVERSE ? segs.num_pieces : segs.num_full) * a.heads)), dim3(2 * D), smem, stream, a, segs);
+  if (!a.direct)
+    hipLaunchKernelGGL((join_states_kernel<D, REVERSE, TRANSPOSED>), dim3((unsigned)(D * D / 1024 * a.heads), (unsigned)segs.n), dim3(256), 0, stream, a, segs);
   return hipGetLastError();
 }
 template <int D, bool TRANSPOSED, int PARTS>
@@ -886,6 +957,13 @@ hipError_t launch_walk(const WalkArgs& a, const LinearSegs& segs, hipStream_t st
   hipLaunchKernelGGL((walk_kernel<D, TRANSPOSED, PARTS>), dim3((unsigned)(segs.num_pieces * a.heads)), dim3(2 * D), smem, stream, a, segs);
   return hipGetLastError();
 }
+// Forward sums and walks, of segments in at most `pieces` pieces.
+template <int D, bool TRANSPOSED, int PARTS>
+hipError_t launch_forward(WalkArgs a, const LinearSegs& segs, int pieces, hipStream_t stream) {
+  a.direct = D < 256 && (pieces - 1) * D * D <= kDirect;
+  const hipError_t e = pieces > 1 ? launch_piece_states<D, false, TRANSPOSED, PARTS>(a, segs, stream) : hipSuccess;
+  return e != hipSuccess ? e : launch_walk<D, TRANSPOSED, PARTS>(a, segs, stream);
+}
 template <int D, int PARTS>
 hipError_t launch_walk_back(const BackArgs& a, const LinearSegs& segs, hipStream_t stream) {
   constexpr size_t smem = Back<D>::smem;
@@ -895,7 +973,7 @@ hipError_t launch_walk_back(const BackArgs& a, const LinearSegs& segs, hipStream
   return hipGetLastError();
 }
 
-// Goes through the segments, as many at a time as travel with a launch, with whether any of them is cut.  Full pieces start first, the others in falling size: what starts last is short.
+// Goes through the segments, as many at a time as travel with a launch, with how many pieces any of them has.  Full pieces start first, the others in falling size: what starts last is short.
 template <class F>
 hipError_t for_segments(const chunk_linear_desc* d, int rows, F&& f) {
   std::vector<int> order;
@@ -915,7 +993,7 @@ hipError_t for_segments(const chunk_linear_desc* d, int rows, F&& f) {
     s.n = std::min(kLinearSegs, d->num_segments - s0);
     s.piece_rows = rows;
     s.num_full = s.num_pieces = 0;
-    bool cut = false;
+    int most = 1;
     for (int i = 0; i < s.n; ++i) {
       const chunk_linear_seg& x = d->segments[order[s0 + i]];
       s.start[i] = x.start;
@@ -928,11 +1006,11 @@ hipError_t for_segments(const chunk_linear_desc* d, int rows, F&& f) {
       s.num_pieces += x.len % rows != 0;
       if (x.len > rows) {
         places += pieces_of(x.len, rows);
-        cut = true;
+        most = std::max(most, pieces_of(x.len, rows));
       }
     }
     s.num_pieces += s.num_full;
-    const hipError_t e = f(s, cut);
+    const hipError_t e = f(s, most);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
@@ -979,13 +1057,12 @@ extern "C" int chunk_linear_fwd(const chunk_linear_desc* d, const void* q, const
   WalkArgs a{(const __bf16*)q, (const __bf16*)k, (const __bf16*)v, (__bf16*)o, log_decay, states_in, states_out, (float*)workspace, d->num_kv_heads,
              d->num_q_heads / d->num_kv_heads, d->scale};
   const hipStream_t stream = (hipStream_t)hip_stream;
-  const hipError_t e = for_segments(d, rows, [&](const LinearSegs& segs, bool cut) {
+  const hipError_t e = for_segments(d, rows, [&](const LinearSegs& segs, int pieces) {
     return by_dim(d->head_dim, [&](auto dim) {
       constexpr int D = decltype(dim)::value;
       auto with_parts = [&](auto parts) {
         constexpr int kParts = decltype(parts)::value;
-        const hipError_t e = cut ? launch_piece_states<D, false, kParts>(a, segs, stream) : hipSuccess;
-        return e != hipSuccess ? e : launch_walk<D, false, kParts>(a, segs, stream);
+        return launch_forward<D, false, kParts>(a, segs, pieces, stream);
       };
       return states_out ? with_parts(std::integral_constant<int, 3>{}) : with_parts(std::integral_constant<int, 2>{});
     });
@@ -1016,29 +1093,23 @@ extern "C" int chunk_linear_bwd(const chunk_linear_desc* d, const void* q, const
   float* const inner_s = (float*)workspace;
   float* const inner_r = need_kv > 0 ? inner_s + need_q / sizeof(float) : nullptr;
   const int heads = d->num_kv_heads, group = d->num_q_heads / heads;
-  const WalkArgs s_states{nullptr, bk, bv, nullptr, log_decay, states_in, nullptr, inner_s, heads, group, d->scale};
+  const WalkArgs to_q{bo, bv, bk, (__bf16*)dq, log_decay, states_in, nullptr, inner_s, heads, group, d->scale};
   const WalkArgs r_states{nullptr, bq, bo, nullptr, log_decay, d_states_out, nullptr, inner_r, heads, group, d->scale};
-  WalkArgs to_q = s_states;
-  to_q.q = bo;
-  to_q.k = bv;
-  to_q.v = bk;
-  to_q.o = (__bf16*)dq;
   const BackArgs to_kv{bq, bk, bv, bo, (__bf16*)dk, (__bf16*)dv, log_decay, d_states_out, d_states_in, inner_r, heads, group, d->scale};
   const hipStream_t stream = (hipStream_t)hip_stream;
-  hipError_t e = for_segments(d, rows_q, [&](const LinearSegs& segs, bool cut) {
+  hipError_t e = for_segments(d, rows_q, [&](const LinearSegs& segs, int pieces) {
     return by_dim(d->head_dim, [&](auto dim) {
       constexpr int D = decltype(dim)::value;
-      const hipError_t e = cut ? launch_piece_states<D, false, 2>(s_states, segs, stream) : hipSuccess;
-      return e != hipSuccess ? e : launch_walk<D, true, 2>(to_q, segs, stream);
+      return launch_forward<D, true, 2>(to_q, segs, pieces, stream);
     });
   });
   if (e != hipSuccess) return report_hip(e, "linear attention backward, dq");
-  e = for_segments(d, rows_kv, [&](const LinearSegs& segs, bool cut) {
+  e = for_segments(d, rows_kv, [&](const LinearSegs& segs, int pieces) {
     return by_dim(d->head_dim, [&](auto dim) {
       constexpr int D = decltype(dim)::value;
       auto with_parts = [&](auto parts) {
         constexpr int kParts = decltype(parts)::value;
-        const hipError_t e = cut ? launch_piece_states<D, true, kParts>(r_states, segs, stream) : hipSuccess;
+        const hipError_t e = pieces > 1 ? launch_piece_states<D, true, false, kParts>(r_states, segs, stream) : hipSuccess;
         return e != hipSuccess ? e : launch_walk_back<D, kParts>(to_kv, segs, stream);
       };
       return d_states_in ? with_parts(std::integral_constant<int, 3>{}) : with_parts(std::integral_constant<int, 2>{});

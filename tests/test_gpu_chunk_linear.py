@@ -116,6 +116,18 @@ def test_states_in_place():
         check(segs, H, Hk, d, "weak", len(lens) + 1, at, in_place=True)
 
 
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("lens,H,Hk,d", [([640, 3], 3, 1, 64), ([2500], 2, 2, 64), ([400, 129], 2, 1, 96), ([1500], 2, 2, 96), ([300, 200], 2, 2, 128), ([700], 2, 1, 128), ([500], 1, 1, 256)])
+def test_pieces_and_states(lens, H, Hk, d, in_place):
+    """Few and many pieces of a sequence (sums added up by the walks, or before them), each sequence from a state and to one."""
+    segs, at = [], 0
+    for i, n in enumerate(lens):
+        segs.append((at, n, i, i if in_place else len(lens) - i))
+        at += n
+    print(lens, H, Hk, d, in_place, flush=True)
+    check(segs, H, Hk, d, "weak", len(lens) + 1, at, seed=7, in_place=in_place)
+
+
 def test_many_sequences():
     """More segments than travel with one launch, some of them cut."""
     lens = [1 + (i * 37) % 90 for i in range(300)]
