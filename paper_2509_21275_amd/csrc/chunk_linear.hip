@@ -18,15 +18,15 @@
 // value of a lane, and four neighbouring elements of an output row lie in a lane.
 //
 // Precision: k_j^T (l^(L-1-j) v_j) has the weighted v_j as a bf16 operand.  Rounded once it would leave states with up to 2^-8 of relative error, so it is split into PARTS bf16 terms: three (24 bits)
-// where the call leaves states or their gradients, which are then as exact as float32 sums are; two (2^-16) where they only pass on inside the call, to where they are rounded to an
-// operand (2^-8).  S and the weighted scores are rounded to bf16 once where they are operands of an output's product.  At head_dim 128 the terms are 48 (two: 32) of the 76 (60)
+// in sums and walks that go into a state or a state's gradient that is left, which is then as exact as float32 sums are; two (2^-16) where the sum only becomes an
+// operand, rounded to 2^-8 (16384 tokens of 32/8 heads of 128, backward with one gradient of a state left: three everywhere 355 us, so 333).  S and the weighted scores are rounded to bf16 once where they are operands of an output's product.  At head_dim 128 the terms are 48 (two: 32) of the 76 (60)
 // products of a wave in a block.
 //
-// Measured (us; head_dim 128 unless said).  Forward, 65536 tokens in 20 sequences, 32/8 heads: 391, of that the walk 320 (1.34 GB, 4.2 TB/s), the pieces' sums 75 and 12; 8192 tokens of 32/32
-// 96 (walk 55 of 268 MB, sums 30 and 11), with states left 113.  Bound by memory while all places are filled; starts (9 of a piece's 30 - 60) and unequal ends are what is above it.
-// Backward, 16384 tokens of 32/8 in 8 sequences: 330 - 360 by the box, walk_back 160, dq's walk 81, sums 68 + 23 and 16 + 13.  walk_back's 103 GFLOP (terms counted) run at 0.65 PFLOP/s, in
+// Measured (us; head_dim 128 unless said).  Forward, 65536 tokens in 20 sequences, 32/8 heads: 389, of that the walk 320 (1.34 GB, 4.2 TB/s), the pieces' sums 75 and 12; 8192 tokens of 32/32
+// 96 (walk 55 of 268 MB, sums 30 and 11), with a state left 113.  Bound by memory while all places are filled; starts (9 of a piece's 30 - 60) and unequal ends are what is above it.
+// Backward, 16384 tokens of 32/8 in 8 sequences: 333, walk_back 160, dq's walk 81, sums 65 + 23 and 16 + 13.  walk_back's 103 GFLOP (terms counted) run at 0.65 PFLOP/s, in
 // its loops at 0.9, where a large product of matrices reaches 1.1: the clock that the chip's power leaves (1.8 GHz) bounds it, not the chain of a step (a sixth fewer cycles
-// per step left the time where it was).  head_dim 256: 8192 tokens of 16/16, forward 163, backward 430 - 455; its walks spill (36 and 73 registers).
+// per step left the time where it was).  head_dim 256: 8192 tokens of 16/16, forward 163, backward 447; its walks spill registers (24 - 154).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -270,14 +270,12 @@ struct StateWeights {
 
 // Each piece's own k^T v into its place in the workspace, but for the one at the far end of its sequence, whose nobody needs, and for sequences of one piece.
 template <int D, bool REVERSE, bool TRANSPOSED, int PARTS>
-__global__ __launch_bounds__(2 * D, 2) void piece_states_kernel(const WalkArgs a, const LinearSegs segs) {
+__device__ __forceinline__ void piece_states(const WalkArgs& a, const LinearSegs& segs, const Piece& p) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   lds_bf16* const ks = (lds_bf16*)smem;
   lds_bf16* const vs = ks + kBlock * pitch(D);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, hh = lane >> 5;
   const int h = blockIdx.x % a.heads;
-  const Piece p = find_piece(segs, blockIdx.x / a.heads);
-  if (p.index == (REVERSE ? 0 : p.pieces - 1)) return;  // (also where there is one piece)
   const float lg = log2_decay(a.log_decay, h);
   const int group = REVERSE ? a.group : 1;
   const int64_t stride = (int64_t)a.heads * group * D;
@@ -315,6 +313,14 @@ __global__ __launch_bounds__(2 * D, 2) void piece_states_kernel(const WalkArgs a
   }
   if constexpr (REVERSE) s.store(place, col, hh);
   else s.store_own(place, wave, lane);
+}
+
+template <int D, bool REVERSE, bool TRANSPOSED>
+__global__ __launch_bounds__(2 * D, D < 256 ? 3 : 2) void piece_states_kernel(const WalkArgs a, const LinearSegs segs) {
+  const Piece p = find_piece(segs, blockIdx.x / a.heads);
+  if (p.index == (REVERSE ? 0 : p.pieces - 1)) return;  // (also where there is one piece)
+  if (a.last && (REVERSE ? segs.in : segs.out)[p.seg] >= 0) piece_states<D, REVERSE, TRANSPOSED, 3>(a, segs, p);  // (the sum goes into a state that is left)
+  else piece_states<D, REVERSE, TRANSPOSED, 2>(a, segs, p);
 }
 
 // Adds them up along each sequence: in the place of each piece's own, the state that it starts from.  (The first one's, too: the slot it comes from may be the one that
@@ -489,7 +495,7 @@ __device__ __forceinline__ void score_outputs(const lds_bf16* ps, const lds_bf16
 // all waves are through with this one's, in the middle of its step, and those of the one after next fetched from then on; k and v of the next block are fetched while this one's query
 // heads run.  Two workgroups share a compute unit (head_dim 128: 74 KB of LDS each).
 template <int D, bool TRANSPOSED, int PARTS>
-__global__ __launch_bounds__(2 * D, 2) void walk_kernel(const WalkArgs a, const LinearSegs segs) {
+__device__ __forceinline__ void walk(const WalkArgs& a, const LinearSegs& segs, const Piece& p) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   constexpr int kTile = kBlock * pitch(D), kWaves = D / 32;
   constexpr bool kAheadOfBlock = D < 256;  // (at 256 the registers do not hold k and v of the next block as well)
@@ -500,7 +506,6 @@ __global__ __launch_bounds__(2 * D, 2) void walk_kernel(const WalkArgs a, const 
   lds_f32* const near = (lds_f32*)(ps + kBlock * pitch(64));
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, hh = lane >> 5;
   const int h = blockIdx.x % a.heads;
-  const Piece p = find_piece(segs, blockIdx.x / a.heads);
   const float lg = log2_decay(a.log_decay, h);
   const int group = a.group;
   const int64_t q_stride = (int64_t)a.heads * group * D, kv_stride = (int64_t)a.heads * D;
@@ -582,8 +587,15 @@ __global__ __launch_bounds__(2 * D, 2) void walk_kernel(const WalkArgs a, const 
       __syncthreads();
     }
   }
-  const int to = segs.out[p.seg];
-  if (a.last && to >= 0 && p.index == p.pieces - 1) s.store(a.last + ((int64_t)to * a.heads + h) * D * D, col, hh);
+  if constexpr (PARTS == 3) s.store(a.last + ((int64_t)segs.out[p.seg] * a.heads + h) * D * D, col, hh);
+}
+template <int D, bool TRANSPOSED>
+__global__ __launch_bounds__(2 * D, 2) void walk_kernel(const WalkArgs a, const LinearSegs segs) {
+  const Piece p = find_piece(segs, blockIdx.x / a.heads);
+  if constexpr (!TRANSPOSED) {  // (those leave none)
+    if (a.last && segs.out[p.seg] >= 0 && p.index == p.pieces - 1) return walk<D, TRANSPOSED, 3>(a, segs, p);  // leaves its state
+  }
+  walk<D, TRANSPOSED, 2>(a, segs, p);
 }
 
 // The walk backwards: dv (q's role: k; k, v: q, d_o; the state R) and dk (v; d_o, q; R^T), both from the same tiles of q and d_o, which half of the waves take in one role and half in the other
@@ -606,17 +618,15 @@ struct Back {
   static constexpr size_t smem = (kRoles + 2 * kBuffers) * tile_bytes(D) + kRoles * tile_bytes(64) + kNear * sizeof(float);
 };
 template <int D, int PARTS>
-__global__ __launch_bounds__(Back<D>::kThreads, 2) void walk_back_kernel(const BackArgs a, const LinearSegs segs) {
+__device__ __forceinline__ void walk_back(const BackArgs& a, const LinearSegs& segs, const Piece& p, int h) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   constexpr int kTile = kBlock * pitch(D), kWaves = D / 32, kRoles = Back<D>::kRoles, kBuffers = Back<D>::kBuffers, kThreads = Back<D>::kThreads;
   const int lane = threadIdx.x & 63, hh = lane >> 5, wave = (threadIdx.x >> 6) % kWaves;
   const int role = __builtin_amdgcn_readfirstlane(kRoles == 2 ? (int)(threadIdx.x >> 6) / kWaves : blockIdx.x % 2);  // 0: dv, 1: dk
-  const int index = kRoles == 2 ? blockIdx.x : blockIdx.x / 2, h = index % a.heads;
   lds_bf16* const own = (lds_bf16*)smem + (kRoles == 2 ? role * kTile : 0);  // k or v
   lds_bf16* const shared = (lds_bf16*)smem + kRoles * kTile;                 // q and d_o, by turns in two places
   lds_bf16* const ps = shared + 2 * kBuffers * kTile + (kRoles == 2 ? role * kBlock * pitch(64) : 0);
   lds_f32* const near = (lds_f32*)((lds_bf16*)smem + (kRoles + 2 * kBuffers) * kTile + kRoles * kBlock * pitch(64));
-  const Piece p = find_piece(segs, index / a.heads);
   const float lg = log2_decay(a.log_decay, h);
   const int group = a.group;
   const int64_t q_stride = (int64_t)a.heads * group * D, kv_stride = (int64_t)a.heads * D;
@@ -708,8 +718,14 @@ __global__ __launch_bounds__(Back<D>::kThreads, 2) void walk_back_kernel(const B
       if (kBuffers == 2) turn ^= 1;
     }
   }
-  const int to = segs.in[p.seg];
-  if (role == 0 && a.last && to >= 0 && p.index == 0) s.store(a.last + ((int64_t)to * a.heads + h) * D * D, col, hh);
+  if (PARTS == 3 && role == 0) s.store(a.last + ((int64_t)segs.in[p.seg] * a.heads + h) * D * D, col, hh);
+}
+template <int D>
+__global__ __launch_bounds__(Back<D>::kThreads, 2) void walk_back_kernel(const BackArgs a, const LinearSegs segs) {
+  const int index = Back<D>::kRoles == 2 ? blockIdx.x : blockIdx.x / 2;
+  const Piece p = find_piece(segs, index / a.heads);
+  if (a.last && segs.in[p.seg] >= 0 && p.index == 0) walk_back<D, 3>(a, segs, p, index % a.heads);  // leaves the gradient of a state
+  else walk_back<D, 2>(a, segs, p, index % a.heads);
 }
 
 // ---- one token ----
@@ -938,38 +954,38 @@ hipError_t by_dim(int d, F&& f) {
   return f(integral_constant<int, 256>{});
 }
 
-template <int D, bool REVERSE, bool TRANSPOSED, int PARTS>
+template <int D, bool REVERSE, bool TRANSPOSED>
 hipError_t launch_piece_states(const WalkArgs& a, const LinearSegs& segs, hipStream_t stream) {
   constexpr size_t smem = 2 * tile_bytes(D);
   static const hipError_t attr =
-      hipFuncSetAttribute(reinterpret_cast<const void*>(&piece_states_kernel<D, REVERSE, TRANSPOSED, PARTS>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+      hipFuncSetAttribute(reinterpret_cast<const void*>(&piece_states_kernel<D, REVERSE, TRANSPOSED>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (attr != hipSuccess) return attr;
-  hipLaunchKernelGGL((piece_states_kernel<D, REVERSE, TRANSPOSED, PARTS>), dim3((unsigned)((REVERSE ? segs.num_pieces : segs.num_full) * a.heads)), dim3(2 * D), smem, stream, a, segs);
+  hipLaunchKernelGGL((piece_states_kernel<D, REVERSE, TRANSPOSED>), dim3((unsigned)((REVERSE ? segs.num_pieces : segs.num_full) * a.heads)), dim3(2 * D), smem, stream, a, segs);
   if (!a.direct)
     hipLaunchKernelGGL((join_states_kernel<D, REVERSE, TRANSPOSED>), dim3((unsigned)(D * D / 1024 * a.heads), (unsigned)segs.n), dim3(256), 0, stream, a, segs);
   return hipGetLastError();
 }
-template <int D, bool TRANSPOSED, int PARTS>
+template <int D, bool TRANSPOSED>
 hipError_t launch_walk(const WalkArgs& a, const LinearSegs& segs, hipStream_t stream) {
   constexpr size_t smem = 3 * tile_bytes(D) + tile_bytes(64) + kNear * sizeof(float);
-  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&walk_kernel<D, TRANSPOSED, PARTS>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&walk_kernel<D, TRANSPOSED>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (attr != hipSuccess) return attr;
-  hipLaunchKernelGGL((walk_kernel<D, TRANSPOSED, PARTS>), dim3((unsigned)(segs.num_pieces * a.heads)), dim3(2 * D), smem, stream, a, segs);
+  hipLaunchKernelGGL((walk_kernel<D, TRANSPOSED>), dim3((unsigned)(segs.num_pieces * a.heads)), dim3(2 * D), smem, stream, a, segs);
   return hipGetLastError();
 }
 // Forward sums and walks, of segments in at most `pieces` pieces.
-template <int D, bool TRANSPOSED, int PARTS>
+template <int D, bool TRANSPOSED>
 hipError_t launch_forward(WalkArgs a, const LinearSegs& segs, int pieces, hipStream_t stream) {
   a.direct = D < 256 && (pieces - 1) * D * D <= kDirect;
-  const hipError_t e = pieces > 1 ? launch_piece_states<D, false, TRANSPOSED, PARTS>(a, segs, stream) : hipSuccess;
-  return e != hipSuccess ? e : launch_walk<D, TRANSPOSED, PARTS>(a, segs, stream);
+  const hipError_t e = pieces > 1 ? launch_piece_states<D, false, TRANSPOSED>(a, segs, stream) : hipSuccess;
+  return e != hipSuccess ? e : launch_walk<D, TRANSPOSED>(a, segs, stream);
 }
-template <int D, int PARTS>
+template <int D>
 hipError_t launch_walk_back(const BackArgs& a, const LinearSegs& segs, hipStream_t stream) {
   constexpr size_t smem = Back<D>::smem;
-  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&walk_back_kernel<D, PARTS>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&walk_back_kernel<D>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (attr != hipSuccess) return attr;
-  hipLaunchKernelGGL((walk_back_kernel<D, PARTS>), dim3((unsigned)(segs.num_pieces * a.heads * (3 - Back<D>::kRoles))), dim3(Back<D>::kThreads), smem, stream, a, segs);
+  hipLaunchKernelGGL((walk_back_kernel<D>), dim3((unsigned)(segs.num_pieces * a.heads * (3 - Back<D>::kRoles))), dim3(Back<D>::kThreads), smem, stream, a, segs);
   return hipGetLastError();
 }
 
@@ -1060,11 +1076,7 @@ extern "C" int chunk_linear_fwd(const chunk_linear_desc* d, const void* q, const
   const hipError_t e = for_segments(d, rows, [&](const LinearSegs& segs, int pieces) {
     return by_dim(d->head_dim, [&](auto dim) {
       constexpr int D = decltype(dim)::value;
-      auto with_parts = [&](auto parts) {
-        constexpr int kParts = decltype(parts)::value;
-        return launch_forward<D, false, kParts>(a, segs, pieces, stream);
-      };
-      return states_out ? with_parts(std::integral_constant<int, 3>{}) : with_parts(std::integral_constant<int, 2>{});
+      return launch_forward<D, false>(a, segs, pieces, stream);
     });
   });
   return e == hipSuccess ? CHUNK_ATTN_OK : report_hip(e, "linear attention forward");
@@ -1094,25 +1106,21 @@ extern "C" int chunk_linear_bwd(const chunk_linear_desc* d, const void* q, const
   float* const inner_r = need_kv > 0 ? inner_s + need_q / sizeof(float) : nullptr;
   const int heads = d->num_kv_heads, group = d->num_q_heads / heads;
   const WalkArgs to_q{bo, bv, bk, (__bf16*)dq, log_decay, states_in, nullptr, inner_s, heads, group, d->scale};
-  const WalkArgs r_states{nullptr, bq, bo, nullptr, log_decay, d_states_out, nullptr, inner_r, heads, group, d->scale};
+  const WalkArgs r_states{nullptr, bq, bo, nullptr, log_decay, d_states_out, d_states_in, inner_r, heads, group, d->scale};
   const BackArgs to_kv{bq, bk, bv, bo, (__bf16*)dk, (__bf16*)dv, log_decay, d_states_out, d_states_in, inner_r, heads, group, d->scale};
   const hipStream_t stream = (hipStream_t)hip_stream;
   hipError_t e = for_segments(d, rows_q, [&](const LinearSegs& segs, int pieces) {
     return by_dim(d->head_dim, [&](auto dim) {
       constexpr int D = decltype(dim)::value;
-      return launch_forward<D, true, 2>(to_q, segs, pieces, stream);
+      return launch_forward<D, true>(to_q, segs, pieces, stream);
     });
   });
   if (e != hipSuccess) return report_hip(e, "linear attention backward, dq");
   e = for_segments(d, rows_kv, [&](const LinearSegs& segs, int pieces) {
     return by_dim(d->head_dim, [&](auto dim) {
       constexpr int D = decltype(dim)::value;
-      auto with_parts = [&](auto parts) {
-        constexpr int kParts = decltype(parts)::value;
-        const hipError_t e = pieces > 1 ? launch_piece_states<D, true, false, kParts>(r_states, segs, stream) : hipSuccess;
-        return e != hipSuccess ? e : launch_walk_back<D, kParts>(to_kv, segs, stream);
-      };
-      return d_states_in ? with_parts(std::integral_constant<int, 3>{}) : with_parts(std::integral_constant<int, 2>{});
+      const hipError_t e = pieces > 1 ? launch_piece_states<D, true, false>(r_states, segs, stream) : hipSuccess;
+      return e != hipSuccess ? e : launch_walk_back<D>(to_kv, segs, stream);
     });
   });
   return e == hipSuccess ? CHUNK_ATTN_OK : report_hip(e, "linear attention backward");
