@@ -17,8 +17,8 @@
  *                   larger one is taken as it is).  A constant: it has no gradient here.
  *   states        : [num_states][num_kv_heads][head_dim of k][head_dim of v] float32, 16-byte aligned
  * Rows of no segment stay as they are.  States (and their gradients) that a call leaves are summed up in float32, from products that are as good as float32's; the products with bf16 operands
- * that form outputs take the state and the weighted scores (l^(t-s) q.k) rounded to bf16, and the result is rounded once more.  A forward without states_out, and a backward without
- * d_states_in, sum the states inside the call from products good to 2^-16.  A value that is not finite
+ * that form outputs take the state and the weighted scores (l^(t-s) q.k) rounded to bf16, and the result is rounded once more.  Sums inside the call that go into no state
+ * that it leaves take products good to 2^-16.  A value that is not finite
  * in a token makes what its sequence has in the same 64 rows (counted from the sequence's start) not finite, and all that follows it.
  *
  * The calls are asynchronous on `hip_stream`, keep nothing, allocate nothing and may be captured into a graph.  The segment table is HOST memory, read during the call; it
