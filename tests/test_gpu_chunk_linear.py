@@ -38,6 +38,8 @@ def close_state(name, got, want, size, terms=1):
 def decays(Hk, kind):
     if kind == "weak":
         return -torch.exp2(-torch.linspace(3.0, 10.0, Hk)).cuda()
+    if kind == "growing":
+        return torch.linspace(0.02, 0.001, Hk).cuda()
     return torch.tensor([0.0, -0.7, -30.0, float("-inf"), -3.0, -0.05, -88.0, -0.001][:Hk], device="cuda")
 
 
@@ -126,6 +128,14 @@ def test_pieces_and_states(lens, H, Hk, d, in_place):
         at += n
     print(lens, H, Hk, d, in_place, flush=True)
     check(segs, H, Hk, d, "weak", len(lens) + 1, at, seed=7, in_place=in_place)
+
+
+def test_states_that_grow():
+    """Decays above 1 are taken as they are."""
+    for lens, H, Hk, d in (([70, 500, 1], 4, 2, 64), ([330], 2, 2, 128), ([200], 1, 1, 256)):
+        segs, total, slots = packed(lens, gap=2)
+        print(lens, H, Hk, d, flush=True)
+        check(segs, H, Hk, d, "growing", slots, total, seed=11)
 
 
 def test_many_sequences():
