@@ -599,7 +599,7 @@ __global__ __launch_bounds__(2 * D, 2) void walk_kernel(const WalkArgs a, const 
 }
 
 // The walk backwards: dv (q's role: k; k, v: q, d_o; the state R) and dk (v; d_o, q; R^T), both from the same tiles of q and d_o, which half of the waves take in one role and half in the other
-// (PAIR; head_dim 256, where their states do not fit the registers of one compute unit: a workgroup for each).  What all query heads hand to the key/value head adds up in the accumulators.  With two buffers
+// (head_dim 256, where their states do not fit the registers of one compute unit: a workgroup for each).  What all query heads hand to the key/value head adds up in the accumulators.  With two buffers
 // (head_dim 96 and 128) the next query head's rows are stored while this one's are read.
 struct BackArgs {
   const __bf16 *q, *k, *v, *d_o;
@@ -610,6 +610,7 @@ struct BackArgs {
   float* inner;
   int heads, group;
   float scale;
+  int only;  // where a workgroup has one role: the role of all of this launch, or -1: the two by turns
 };
 static_assert(sizeof(LinearSegs) + sizeof(BackArgs) <= 3900, "fits the kernel arguments");
 template <int D>
@@ -618,11 +619,11 @@ struct Back {
   static constexpr size_t smem = (kRoles + 2 * kBuffers) * tile_bytes(D) + kRoles * tile_bytes(64) + kNear * sizeof(float);
 };
 template <int D, int PARTS>
-__device__ __forceinline__ void walk_back(const BackArgs& a, const LinearSegs& segs, const Piece& p, int h) {
+__device__ __forceinline__ void walk_back(const BackArgs& a, const LinearSegs& segs, const Piece& p, int h, int workgroup_role) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   constexpr int kTile = kBlock * pitch(D), kWaves = D / 32, kRoles = Back<D>::kRoles, kBuffers = Back<D>::kBuffers, kThreads = Back<D>::kThreads;
   const int lane = threadIdx.x & 63, hh = lane >> 5, wave = (threadIdx.x >> 6) % kWaves;
-  const int role = __builtin_amdgcn_readfirstlane(kRoles == 2 ? (int)(threadIdx.x >> 6) / kWaves : blockIdx.x % 2);  // 0: dv, 1: dk
+  const int role = __builtin_amdgcn_readfirstlane(kRoles == 2 ? (int)(threadIdx.x >> 6) / kWaves : workgroup_role);  // 0: dv, 1: dk
   lds_bf16* const own = (lds_bf16*)smem + (kRoles == 2 ? role * kTile : 0);  // k or v
   lds_bf16* const shared = (lds_bf16*)smem + kRoles * kTile;                 // q and d_o, by turns in two places
   lds_bf16* const ps = shared + 2 * kBuffers * kTile + (kRoles == 2 ? role * kBlock * pitch(64) : 0);
@@ -722,10 +723,11 @@ __device__ __forceinline__ void walk_back(const BackArgs& a, const LinearSegs& s
 }
 template <int D>
 __global__ __launch_bounds__(Back<D>::kThreads, 2) void walk_back_kernel(const BackArgs a, const LinearSegs segs) {
-  const int index = Back<D>::kRoles == 2 ? blockIdx.x : blockIdx.x / 2;
+  const bool turns = Back<D>::kRoles == 1 && a.only < 0;
+  const int index = turns ? blockIdx.x / 2 : blockIdx.x, role = turns ? blockIdx.x % 2 : a.only;
   const Piece p = find_piece(segs, index / a.heads);
-  if (a.last && segs.in[p.seg] >= 0 && p.index == 0) walk_back<D, 3>(a, segs, p, index % a.heads);  // leaves the gradient of a state
-  else walk_back<D, 2>(a, segs, p, index % a.heads);
+  if (a.last && segs.in[p.seg] >= 0 && p.index == 0) walk_back<D, 3>(a, segs, p, index % a.heads, role);  // leaves the gradient of a state
+  else walk_back<D, 2>(a, segs, p, index % a.heads, role);
 }
 
 // ---- one token ----
@@ -980,13 +982,31 @@ hipError_t launch_forward(WalkArgs a, const LinearSegs& segs, int pieces, hipStr
   const hipError_t e = pieces > 1 ? launch_piece_states<D, false, TRANSPOSED>(a, segs, stream) : hipSuccess;
   return e != hipSuccess ? e : launch_walk<D, TRANSPOSED>(a, segs, stream);
 }
+// Whether the gradient of some state is read and written in one place by the walks themselves.  (Cut sequences start from a copy in the workspace.)
+bool in_place_uncut(const BackArgs& a, const LinearSegs& segs) {
+  if (!a.last || a.last != a.first) return false;
+  for (int i = 0; i < segs.n; ++i)
+    if (segs.len[i] <= segs.piece_rows && segs.in[i] >= 0 && segs.in[i] == segs.out[i]) return true;
+  return false;
+}
 template <int D>
-hipError_t launch_walk_back(const BackArgs& a, const LinearSegs& segs, hipStream_t stream) {
+hipError_t launch_walk_back(BackArgs a, const LinearSegs& segs, hipStream_t stream) {
   constexpr size_t smem = Back<D>::smem;
   static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&walk_back_kernel<D>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (attr != hipSuccess) return attr;
-  hipLaunchKernelGGL((walk_back_kernel<D>), dim3((unsigned)(segs.num_pieces * a.heads * (3 - Back<D>::kRoles))), dim3(Back<D>::kThreads), smem, stream, a, segs);
-  return hipGetLastError();
+  auto launch = [&](int roles, int only) {
+    a.only = only;
+    hipLaunchKernelGGL((walk_back_kernel<D>), dim3((unsigned)(segs.num_pieces * a.heads * roles)), dim3(Back<D>::kThreads), smem, stream, a, segs);
+    return hipGetLastError();
+  };
+  if constexpr (Back<D>::kRoles == 1) {
+    if (in_place_uncut(a, segs)) {  // dk's workgroups start from a gradient that dv's replace, and nothing says which of them run first: dk in a launch before
+      const hipError_t e = launch(1, 1);
+      return e != hipSuccess ? e : launch(1, 0);
+    }
+    return launch(2, -1);
+  }
+  return launch(1, -1);
 }
 
 // Goes through the segments, as many at a time as travel with a launch, with how many pieces any of them has.  Full pieces start first, the others in falling size: what starts last is short.
@@ -1107,7 +1127,7 @@ extern "C" int chunk_linear_bwd(const chunk_linear_desc* d, const void* q, const
   const int heads = d->num_kv_heads, group = d->num_q_heads / heads;
   const WalkArgs to_q{bo, bv, bk, (__bf16*)dq, log_decay, states_in, nullptr, inner_s, heads, group, d->scale};
   const WalkArgs r_states{nullptr, bq, bo, nullptr, log_decay, d_states_out, d_states_in, inner_r, heads, group, d->scale};
-  const BackArgs to_kv{bq, bk, bv, bo, (__bf16*)dk, (__bf16*)dv, log_decay, d_states_out, d_states_in, inner_r, heads, group, d->scale};
+  const BackArgs to_kv{bq, bk, bv, bo, (__bf16*)dk, (__bf16*)dv, log_decay, d_states_out, d_states_in, inner_r, heads, group, d->scale, -1};
   const hipStream_t stream = (hipStream_t)hip_stream;
   hipError_t e = for_segments(d, rows_q, [&](const LinearSegs& segs, int pieces) {
     return by_dim(d->head_dim, [&](auto dim) {
