@@ -16,9 +16,8 @@
  *   log_decay     : [num_kv_heads] float32, natural logarithm of the decay, normally <= 0 (0: nothing decays, -inf: only the token itself counts; a
  *                   larger one is taken as it is).  A constant: it has no gradient here.
  *   states        : [num_states][num_kv_heads][head_dim of k][head_dim of v] float32, 16-byte aligned
- * Rows of no segment stay as they are.  States (and their gradients) that a call leaves are summed up in float32, from products that are as good as float32's; the products with bf16 operands
- * that form outputs take the state and the weighted scores (l^(t-s) q.k) rounded to bf16, and the result is rounded once more.  Sums inside the call that go into no state
- * that it leaves take products good to 2^-16.  A value that is not finite
+ * Rows of no segment stay as they are.  States (and their gradients) that a call leaves are summed up in float32, from products that are as good as float32's; products
+ * that form outputs, and sums inside the call that go into no state that it leaves, are good to 2^-16 and summed up in float32.  A result is rounded once.  A value that is not finite
  * in a token makes what its sequence has in the same 64 rows (counted from the sequence's start) not finite, and all that follows it.
  *
  * The calls are asynchronous on `hip_stream`, keep nothing, allocate nothing and may be captured into a graph.  The segment table is HOST memory, read during the call; it

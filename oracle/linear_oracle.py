@@ -44,7 +44,7 @@ def backward(q, k, v, log_decay, scale, d_o, state=None, d_final=None):
 
 
 def rounding(q, k, v, log_decay, scale, state=None, backwards=False, block=64):
-    """Root of the sum of squares of what the kernels round to bf16 on the way to an output [tokens, heads of q, d]: the weighted scores inside a block of
+    """Root of the sum of squares of what the kernels hand on in bf16 terms on the way to an output [tokens, heads of q, d]: the weighted scores inside a block of
     rows times v, and the state before the block times q.  q has either all query heads (k, v shared by them) or only the key/value heads (k, v of all
     query heads added up)."""
     n, H = q.shape[0], max(q.shape[1], k.shape[1])

@@ -17,10 +17,10 @@
 // they are: transposed reads deliver column quads 0, 2, 1, 3.  Outputs are formed transposed (columns = tokens), so that the power of l a row is multiplied with is one
 // value of a lane, and four neighbouring elements of an output row lie in a lane.
 //
-// Precision: k_j^T (l^(L-1-j) v_j) has the weighted v_j as a bf16 operand.  Rounded once it would leave states with up to 2^-8 of relative error, so it is split into PARTS bf16 terms: three (24 bits)
-// in sums and walks that go into a state or a state's gradient that is left, which is then as exact as float32 sums are; two (2^-16) where the sum only becomes an
-// operand, rounded to 2^-8 (16384 tokens of 32/8 heads of 128, backward with one gradient of a state left: three everywhere 355 us, so 333).  S and the weighted scores are rounded to bf16 once where they are operands of an output's product.  At head_dim 128 the terms are 48 (two: 32) of the 76 (60)
-// products of a wave in a block.
+// Precision: an operand in bf16 that is not an input would be off by 2^-8, as much as the one rounding of a result, so it is a sum of bf16 terms, each a product of its own.  Two terms (2^-16) for the state and the
+// weighted scores in an output's products (one each: root mean square error 2.3e-3 of the result where a single rounding leaves 1.7e-3, 11 - 13 % less time at head_dim 128: 8192 tokens of 32/32 with a state left
+// 115 -> 131 us, 65536 packed of 32/8 389 -> 441, backward of 16384 326 -> 370) and for the weighted v_j in sums k_j^T (l^(L-1-j) v_j) that only become such an operand; three (24 bits) in sums and walks that go into a state or a
+// state's gradient that is left, which is then as exact as float32 sums are.  At head_dim 128 the terms past the first are half of the 82 products of a wave in a block of one query head.
 //
 // Measured (us; head_dim 128 unless said).  Forward, 65536 tokens in 20 sequences, 32/8 heads: 389, of that the walk 320 (1.34 GB, 4.2 TB/s), the pieces' sums 75 and 12; 8192 tokens of 32/32
 // 96 (walk 55 of 268 MB, sums 30 and 11), with a state left 113.  Bound by memory while all places are filled; starts (9 of a piece's 30 - 60) and unequal ends are what is above it.
@@ -146,6 +146,18 @@ __device__ __forceinline__ bf16x8 column_operand(const lds_bf16* tile, int row0,
   return u.all;
 }
 
+// x as a sum of bf16 terms, each the rounded rest of those before: two are good to 2^-16, three to float32.
+template <int PARTS>
+__device__ __forceinline__ void split(float (&x)[8], bf16x8 (&term)[PARTS]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p) {
+      term[p][e] = (__bf16)x[e];
+      x[e] -= (float)term[p][e];
+    }
+}
+
 // The state of a wave: D rows x 32 columns.
 template <int D>
 struct State {
@@ -217,29 +229,25 @@ struct State {
 #pragma unroll
       for (int e = 0; e < 16; ++e) t[i][e] *= by;
   }
-  // operand of rows 16 step .. 16 step + 15 as the contraction
-  __device__ __forceinline__ bf16x8 operand(int step) const {
-    const f32x16& a = t[step >> 1];
-    const int o = 8 * (step & 1);
-    return pack8(a[o], a[o + 1], a[o + 2], a[o + 3], a[o + 4], a[o + 5], a[o + 6], a[o + 7]);
+  // operands of rows 16 step .. 16 step + 15 as the contraction: two bf16 terms
+  __device__ __forceinline__ void operands(int step, bf16x8 (&term)[2]) const {
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = t[step >> 1][8 * (step & 1) + e];
+    split(x, term);
   }
   // adds k^T (w v) of 16 rows from row0 on: v's operand as it was read; element e's row weighs lead * base[e]
   template <int PARTS>
   __device__ __forceinline__ void add(const lds_bf16* k_tile, int row0, bf16x8 v, float lead, const float (&base)[8], int lane) {
     constexpr int kTiles = D / 32, kHalf = (kTiles + 1) / 2;
     bf16x8 kt[kTiles], part[PARTS];
+    float x[8];
 #pragma unroll
     for (int i = 0; i < kHalf; ++i) kt[i] = column_operand<D, true>(k_tile, row0, 32 * i, lane);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      float x = (float)v[e] * (lead * base[e]);
-#pragma unroll
-      for (int p = 0; p < PARTS; ++p) {
-        part[p][e] = (__bf16)x;
-        x -= (float)part[p][e];
-      }
-    }
+    for (int e = 0; e < 8; ++e) x[e] = (float)v[e] * (lead * base[e]);
+    split(x, part);
 #pragma unroll
     for (int i = kHalf; i < kTiles; ++i) kt[i] = column_operand<D, true>(k_tile, row0, 32 * i, lane);
     __builtin_amdgcn_sched_barrier(0);
@@ -408,7 +416,9 @@ __device__ __forceinline__ void score_weights(float lg, float scale, lds_f32* ne
   }
 }
 // Scores of rows i of q with rows j of k, in tiles of 32 x 32, only those with j <= i (backwards j >= i): 0: (0, 0), 1: the one off the diagonal, 2: (1, 1).  Formed transposed (a lane holds one row i
-// and four columns j at a time), weighted, and written to LDS.
+// and four columns j at a time), weighted, and written to LDS in two bf16 terms, the second ones' three tiles behind the first ones'.
+constexpr int kScoreTile = 32 * pitch(32);
+constexpr size_t kScoreBytes = 2 * 3 * kScoreTile * 2;
 template <int D, bool REVERSE>
 __device__ __forceinline__ void scores(int tile, const lds_bf16* qs, const lds_bf16* ks, const lds_f32* near, lds_bf16* ps, int lane) {
   const int ti = REVERSE ? tile >> 1 : (tile + 1) >> 1, tj = REVERSE ? (tile + 1) >> 1 : tile >> 1;
@@ -433,10 +443,20 @@ __device__ __forceinline__ void scores(int tile, const lds_bf16* qs, const lds_b
   f32x4 w[4];
 #pragma unroll
   for (int q4 = 0; q4 < 4; ++q4) w[q4] = lds_load4f(near + (tile == 1 ? 1024 : 0) + q4 * 256 + lane * 4);
-  lds_bf16* const to = ps + ((lane & 31) * pitch(64) + 4 * (lane >> 5)) + (32 * ti * pitch(64) + 32 * tj);
+  lds_bf16* const to = ps + ((lane & 31) * pitch(32) + 4 * (lane >> 5)) + tile * kScoreTile;
 #pragma unroll
-  for (int q4 = 0; q4 < 4; ++q4)
-    *(__attribute__((address_space(3))) bf16x4*)(to + 8 * q4) = pack4(c[4 * q4] * w[q4][0], c[4 * q4 + 1] * w[q4][1], c[4 * q4 + 2] * w[q4][2], c[4 * q4 + 3] * w[q4][3]);
+  for (int q4 = 0; q4 < 4; q4 += 2) {
+    float x[8];
+    bf16x8 term[2];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = c[4 * q4 + e] * w[q4 + e / 4][e % 4];
+    split(x, term);
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      *(__attribute__((address_space(3))) bf16x4*)(to + 3 * p * kScoreTile + 8 * q4) = __builtin_shufflevector(term[p], term[p], 0, 1, 2, 3);
+      *(__attribute__((address_space(3))) bf16x4*)(to + 3 * p * kScoreTile + 8 * q4 + 8) = __builtin_shufflevector(term[p], term[p], 4, 5, 6, 7);
+    }
+  }
 }
 // What the state gives the wave's 32 columns, times each row's power of the decay and a scale.  Rows stand behind `empty` others.
 template <int D, bool REVERSE>
@@ -454,9 +474,13 @@ __device__ __forceinline__ void state_outputs(const State<D>& s, const lds_bf16*
   for (int st = 0; st < kSteps; ++st) {
     if (st + ahead(D) < kSteps) read(st + ahead(D));
     __builtin_amdgcn_sched_barrier(0);
-    const bf16x8 sb = s.operand(st);
-    o[0] = mfma32(sb, qf[st][0], o[0]);
-    o[1] = mfma32(sb, qf[st][1], o[1]);
+    bf16x8 sb[2];
+    s.operands(st, sb);
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      o[0] = mfma32(sb[p], qf[st][0], o[0]);
+      o[1] = mfma32(sb[p], qf[st][1], o[1]);
+    }
     __builtin_amdgcn_sched_barrier(0);
   }
 #pragma unroll
@@ -470,23 +494,29 @@ __device__ __forceinline__ void state_outputs(const State<D>& s, const lds_bf16*
 // Adds what the scores give; leaves v's operands.
 template <int D, bool REVERSE>
 __device__ __forceinline__ void score_outputs(const lds_bf16* ps, const lds_bf16* vs, int col0, int lane, f32x16 (&o)[2], bf16x8 (&vop)[4]) {
-  bf16x8 pf[4][2];
+  constexpr int kAhead = D < 128 ? 2 : 1;  // (two at 128 spill 36 registers: 65536 packed tokens 441 -> 455 us)
+  bf16x8 pf[4][2][2];
   auto pair = [](int st, int half) { return REVERSE ? st >= 2 * half : st < 2 * half + 2; };
   auto read = [&](int st) {
     vop[st] = column_operand<D, false>(vs, 16 * st, col0, lane);
 #pragma unroll
     for (int half = 0; half < 2; ++half)
-      if (pair(st, half)) pf[st][half] = row_operand<64>(ps, 32 * half, st, lane);
+      if (pair(st, half))
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+          pf[st][half][p] = row_operand<32>(ps + (half + (st >> 1) + 3 * p) * kScoreTile, 0, st & 1, lane);
   };
 #pragma unroll
-  for (int st = 0; st < ahead(D); ++st) read(st);
+  for (int st = 0; st < kAhead; ++st) read(st);
 #pragma unroll
   for (int st = 0; st < 4; ++st) {
-    if (st + ahead(D) < 4) read(st + ahead(D));
+    if (st + kAhead < 4) read(st + kAhead);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int half = 0; half < 2; ++half)
-      if (pair(st, half)) o[half] = mfma32(vop[st], pf[st][half], o[half]);
+    for (int p = 0; p < 2; ++p)
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+        if (pair(st, half)) o[half] = mfma32(vop[st], pf[st][half][p], o[half]);
     __builtin_amdgcn_sched_barrier(0);
   }
 }
@@ -502,8 +532,8 @@ __device__ __forceinline__ void walk(const WalkArgs& a, const LinearSegs& segs, 
   lds_bf16* const qs = (lds_bf16*)smem;
   lds_bf16* const ks = qs + kTile;
   lds_bf16* const vs = ks + kTile;
-  lds_bf16* const ps = vs + kTile;  // weighted scores, 64 x 64
-  lds_f32* const near = (lds_f32*)(ps + kBlock * pitch(64));
+  lds_bf16* const ps = vs + kTile;  // weighted scores
+  lds_f32* const near = (lds_f32*)(ps + kScoreBytes / 2);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, hh = lane >> 5;
   const int h = blockIdx.x % a.heads;
   const float lg = log2_decay(a.log_decay, h);
@@ -616,7 +646,7 @@ static_assert(sizeof(LinearSegs) + sizeof(BackArgs) <= 3900, "fits the kernel ar
 template <int D>
 struct Back {
   static constexpr int kRoles = D == 256 ? 1 : 2, kThreads = 2 * D * kRoles, kBuffers = D == 96 || D == 128 ? 2 : 1;
-  static constexpr size_t smem = (kRoles + 2 * kBuffers) * tile_bytes(D) + kRoles * tile_bytes(64) + kNear * sizeof(float);
+  static constexpr size_t smem = (kRoles + 2 * kBuffers) * tile_bytes(D) + kRoles * kScoreBytes + kNear * sizeof(float);
 };
 template <int D, int PARTS>
 __device__ __forceinline__ void walk_back(const BackArgs& a, const LinearSegs& segs, const Piece& p, int h, int workgroup_role) {
@@ -626,8 +656,8 @@ __device__ __forceinline__ void walk_back(const BackArgs& a, const LinearSegs& s
   const int role = __builtin_amdgcn_readfirstlane(kRoles == 2 ? (int)(threadIdx.x >> 6) / kWaves : workgroup_role);  // 0: dv, 1: dk
   lds_bf16* const own = (lds_bf16*)smem + (kRoles == 2 ? role * kTile : 0);  // k or v
   lds_bf16* const shared = (lds_bf16*)smem + kRoles * kTile;                 // q and d_o, by turns in two places
-  lds_bf16* const ps = shared + 2 * kBuffers * kTile + (kRoles == 2 ? role * kBlock * pitch(64) : 0);
-  lds_f32* const near = (lds_f32*)((lds_bf16*)smem + (kRoles + 2 * kBuffers) * kTile + kRoles * kBlock * pitch(64));
+  lds_bf16* const ps = shared + 2 * kBuffers * kTile + (kRoles == 2 ? role * (int)kScoreBytes / 2 : 0);
+  lds_f32* const near = (lds_f32*)((lds_bf16*)smem + (kRoles + 2 * kBuffers) * kTile + kRoles * (int)kScoreBytes / 2);
   const float lg = log2_decay(a.log_decay, h);
   const int group = a.group;
   const int64_t q_stride = (int64_t)a.heads * group * D, kv_stride = (int64_t)a.heads * D;
@@ -969,7 +999,7 @@ hipError_t launch_piece_states(const WalkArgs& a, const LinearSegs& segs, hipStr
 }
 template <int D, bool TRANSPOSED>
 hipError_t launch_walk(const WalkArgs& a, const LinearSegs& segs, hipStream_t stream) {
-  constexpr size_t smem = 3 * tile_bytes(D) + tile_bytes(64) + kNear * sizeof(float);
+  constexpr size_t smem = 3 * tile_bytes(D) + kScoreBytes + kNear * sizeof(float);
   static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&walk_kernel<D, TRANSPOSED>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (attr != hipSuccess) return attr;
   hipLaunchKernelGGL((walk_kernel<D, TRANSPOSED>), dim3((unsigned)(segs.num_pieces * a.heads)), dim3(2 * D), smem, stream, a, segs);

@@ -1,6 +1,12 @@
-"""Linear attention at the edges of what a call may be: gradients of states in place where no sequence is cut."""
+"""Linear attention at the edges of what a call may be: gradients of states in place where no sequence is cut; outputs that are rounded to bf16 once.
+
+Tolerance of outputs: half a step of bf16 for the result, 2^-8 of its value.  Before that, what is an operand of a product (weighted scores, the state, the weighted rows in the sums that become the state) is the
+sum of two bf16 terms, off by at most 2^-8 * 2^-8 = 2^-16 of its value, 2^-16 / sqrt(3) in root mean square.  With the oracle's root of the sum of squares of what scores and states contribute (the sums' own
+products contribute as much as the state at most, so sqrt(2) of it), six standard deviations are 6 sqrt(2) 2^-16 / sqrt(3) < 5 * 2^-16 of it.  Float32 sums: 2^-18 of the tensor's largest value."""
 import pytest
 import torch
+
+from oracle import linear_oracle as orc
 
 pytestmark = pytest.mark.gpu
 
@@ -37,3 +43,37 @@ def test_gradients_of_states_in_place_uncut(d, H, Hk):
     both = given.clone()
     for a, b in zip(run(both, both), want):
         assert torch.equal(a, b)
+
+
+def rounded_once(name, got, want, sigma):
+    assert bool(torch.isfinite(got).all()), name
+    over = (got.double() - want).abs() - (2.0 ** -8 * want.abs() + 5 * 2.0 ** -16 * sigma + 2.0 ** -18 * want.abs().max())
+    assert float(over.max()) <= 0, (name, float(over.max()), int((over > 0).sum()), over.numel())
+
+
+@pytest.mark.parametrize("lens,H,Hk,d", [([1, 33, 64, 130], 4, 2, 64), ([700], 2, 2, 64), ([200, 65], 3, 1, 96), ([100, 500], 4, 2, 128), ([1500], 2, 2, 128), ([90, 300], 2, 1, 256)])
+def test_outputs_are_rounded_once(lens, H, Hk, d):
+    """From states and from none, uncut and in pieces, all query heads of a key/value head."""
+    from paper_2509_21275_amd import chunk_linear as cl
+    total, scale = sum(lens), d ** -0.5
+    segs, at = [], 0
+    for i, n in enumerate(lens):
+        segs.append((at, n, i if i % 2 == 0 else -1, i))
+        at += n
+    q, k, v, do = (normal((total, h, d), 20 + i) for i, h in enumerate((H, Hk, Hk, H)))
+    lg = -torch.exp2(-torch.linspace(2.0, 9.0, Hk)).cuda()
+    states, grads = normal((len(lens), Hk, d, d), 30, torch.float32, 3.0), normal((len(lens), Hk, d, d), 31, torch.float32)
+    desc = cl.make_desc(segs, H, Hk, d, total, len(lens), scale)
+    ws, left, first = cl.alloc_workspace(desc), torch.empty_like(states), torch.empty_like(states)
+    o, dq, dk, dv = (torch.empty_like(t) for t in (q, q, k, v))
+    print(lens, H, Hk, d, flush=True)
+    cl.chunk_linear_fwd(desc, q, k, v, lg, states, o, left, ws)
+    cl.chunk_linear_bwd(desc, q, k, v, lg, states, do, grads, dq, dk, dv, first, ws)
+    torch.cuda.synchronize()
+    for start, n, a, b in segs:
+        r, S0, dS = slice(start, start + n), states[a] if a >= 0 else None, grads[b]
+        rounded_once("o", o[r], orc.forward(q[r], k[r], v[r], lg, scale, S0)[0], orc.rounding(q[r], k[r], v[r], lg, scale, S0))
+        wq, wk, wv, _, _ = orc.backward(q[r], k[r], v[r], lg, scale, do[r], S0, dS)
+        rounded_once("dq", dq[r], wq, orc.rounding(do[r], v[r], k[r], lg, scale, None if S0 is None else S0.transpose(1, 2)))
+        rounded_once("dk", dk[r], wk, orc.rounding(v[r], do[r], q[r], lg, scale, dS.transpose(1, 2) / scale, backwards=True))
+        rounded_once("dv", dv[r], wv, orc.rounding(k[r], q[r], do[r], lg, scale, dS / scale, backwards=True))
