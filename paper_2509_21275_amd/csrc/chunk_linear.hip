@@ -20,7 +20,7 @@
 // Precision: an operand in bf16 that is not an input would be off by 2^-8, as much as the one rounding of a result, so it is a sum of bf16 terms, each a product of its own.  Two terms (2^-16) for the state and the
 // weighted scores in an output's products (one each: root mean square error 2.3e-3 of the result where a single rounding leaves 1.7e-3, 11 - 13 % less time at head_dim 128: 8192 tokens of 32/32 with a state left
 // 115 -> 131 us, 65536 packed of 32/8 389 -> 441, backward of 16384 326 -> 370) and for the weighted v_j in sums k_j^T (l^(L-1-j) v_j) that only become such an operand; three (24 bits) in sums and walks that go into a state or a
-// state's gradient that is left, which is then as exact as float32 sums are.  At head_dim 128 the terms past the first are half of the 82 products of a wave in a block of one query head.
+// state's gradient that is left, which is then as exact as float32 sums are.  At head_dim 128 the terms past the first are 38 of the 82 products of a wave in a block of one query head.
 //
 // Measured (us; head_dim 128 unless said).  Forward, 65536 tokens in 20 sequences, 32/8 heads: 389, of that the walk 320 (1.34 GB, 4.2 TB/s), the pieces' sums 75 and 12; 8192 tokens of 32/32
 // 96 (walk 55 of 268 MB, sums 30 and 11), with a state left 113.  Bound by memory while all places are filled; starts (9 of a piece's 30 - 60) and unequal ends are what is above it.
@@ -265,14 +265,18 @@ struct State {
 };
 
 // Weights of a block's rows in its state, l^(63 - j) or backwards (the gradient of S) scale * l^(j + 1) for row j = 16 s + 8 hh + e: lead[s] * base[e], both powers with exponents >= 0.
+// Eights of rows that are not there in any block of a piece of fewer than 64 weigh nothing: a decay above 1 may have no float32 number for a power that no row needs, and that times a row of zeros is no zero.
 template <bool REVERSE>
 struct StateWeights {
   float base[8], lead[4];
-  __device__ __forceinline__ StateWeights(float lg, float scale, int hh) {
+  __device__ __forceinline__ StateWeights(float lg, float scale, int hh, int piece_rows) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) base[e] = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(power(lg, REVERSE ? e : 7 - e))));
 #pragma unroll
-    for (int s = 0; s < 4; ++s) lead[s] = REVERSE ? scale * power(lg, 16 * s + 8 * hh + 1) : power(lg, 56 - 16 * s - 8 * hh);
+    for (int s = 0; s < 4; ++s) {
+      const int eight = REVERSE ? 16 * s + 8 * hh : 56 - 16 * s - 8 * hh;  // the least power of its rows, or one less
+      lead[s] = eight >= piece_rows ? 0.f : REVERSE ? scale * power(lg, eight + 1) : power(lg, eight);
+    }
   }
 };
 
@@ -287,7 +291,7 @@ __device__ __forceinline__ void piece_states(const WalkArgs& a, const LinearSegs
   const float lg = log2_decay(a.log_decay, h);
   const int group = REVERSE ? a.group : 1;
   const int64_t stride = (int64_t)a.heads * group * D;
-  const StateWeights<REVERSE> weights(lg, a.scale, hh);
+  const StateWeights<REVERSE> weights(lg, a.scale, hh, p.rows);
   float* const place = a.inner + ((int64_t)(segs.place0[p.seg] + p.index) * a.heads + h) * D * D;
   const int col = 32 * wave + (lane & 31);
   State<D> s;
@@ -406,13 +410,14 @@ __device__ __forceinline__ void store_rows(const Rows& to, int row0, int byte, c
 // ---- the three products of a step ----
 constexpr int ahead(int d) { return d < 256 ? 2 : 1; }  // stages that operands are read ahead of their products (as far as there are registers)
 
-// Weights of scores, times the scale of outputs, as a lane needs them: of a tile on the diagonal of the block, and of the one off it ([2][quad of columns][lane][4]).
+// Weights of scores, times the scale of outputs, as a lane needs them: of a tile on the diagonal of the block, and of the one off it ([2][quad of columns][lane][4]);
+// no weight for rows further apart than any two of the piece's.
 constexpr int kNear = 2 * 16 * 64;
 template <bool REVERSE, int THREADS>
-__device__ __forceinline__ void score_weights(float lg, float scale, lds_f32* near) {
+__device__ __forceinline__ void score_weights(float lg, float scale, int piece_rows, lds_f32* near) {
   for (int i = threadIdx.x; i < kNear; i += THREADS) {
     const int l = i >> 2 & 63, j = 8 * (i >> 8 & 3) + 4 * (l >> 5) + (i & 3), far = (REVERSE ? j - (l & 31) : (l & 31) - j) + 32 * (i >> 10);
-    near[i] = far >= 0 ? power(lg, far) * scale : 0.f;
+    near[i] = far >= 0 && far < piece_rows ? power(lg, far) * scale : 0.f;
   }
 }
 // Scores of rows i of q with rows j of k, in tiles of 32 x 32, only those with j <= i (backwards j >= i): 0: (0, 0), 1: the one off the diagonal, 2: (1, 1).  Formed transposed (a lane holds one row i
@@ -575,8 +580,8 @@ __device__ __forceinline__ void walk(const WalkArgs& a, const LinearSegs& segs, 
     }
   } else if (p.pieces == 1 && a.first && from >= 0) s.template load<TRANSPOSED>(a.first + ((int64_t)from * a.heads + h) * D * D, col, hh);
   else s.clear();
-  const StateWeights<false> weights(lg, 1.f, hh);
-  score_weights<false, 2 * D>(lg, a.scale, near);
+  const StateWeights<false> weights(lg, 1.f, hh, p.rows);
+  score_weights<false, 2 * D>(lg, a.scale, p.rows, near);
   wait_all_but<0>();  // (else the compiler has the loop wait for all loads wherever it uses the state)
   qt.store(qs);
   kt.store(ks);
@@ -692,8 +697,8 @@ __device__ __forceinline__ void walk_back(const BackArgs& a, const LinearSegs& s
   } else {
     s.clear();
   }
-  const StateWeights<true> weights(lg, a.scale, hh);
-  score_weights<true, kThreads>(lg, a.scale, near);
+  const StateWeights<true> weights(lg, a.scale, hh, p.rows);
+  score_weights<true, kThreads>(lg, a.scale, p.rows, near);
   wait_all_but<0>();  // (as in the walk forwards)
   qt.store(shared);
   dt.store(shared + kTile);

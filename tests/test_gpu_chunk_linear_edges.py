@@ -1,4 +1,5 @@
-"""Linear attention at the edges of what a call may be: gradients of states in place where no sequence is cut; outputs that are rounded to bf16 once.
+"""Linear attention at the edges of what a call may be: gradients of states in place where no sequence is cut; outputs that are rounded to bf16 once;
+decays above 1 whose powers leave float32 soon behind the last token.
 
 Tolerance of outputs: half a step of bf16 for the result, 2^-8 of its value.  Before that, what is an operand of a product (weighted scores, the state, the weighted rows in the sums that become the state) is the
 sum of two bf16 terms, off by at most 2^-8 * 2^-8 = 2^-16 of its value, 2^-16 / sqrt(3) in root mean square.  With the oracle's root of the sum of squares of what scores and states contribute (the sums' own
@@ -77,3 +78,32 @@ def test_outputs_are_rounded_once(lens, H, Hk, d):
         rounded_once("dq", dq[r], wq, orc.rounding(do[r], v[r], k[r], lg, scale, None if S0 is None else S0.transpose(1, 2)))
         rounded_once("dk", dk[r], wk, orc.rounding(v[r], do[r], q[r], lg, scale, dS.transpose(1, 2) / scale, backwards=True))
         rounded_once("dv", dv[r], wv, orc.rounding(k[r], q[r], do[r], lg, scale, dS / scale, backwards=True))
+
+
+@pytest.mark.parametrize("n,log_decay", [(1, 10.0), (5, 10.0), (8, 10.0), (9, 5.0), (10, 2.0), (24, 3.4), (33, 2.0), (40, 2.0), (63, 1.3), (64, 1.3), (65, 1.15), (150, 0.5)])
+@pytest.mark.parametrize("given", [False, True])
+def test_decays_far_above_one(n, log_decay, given):
+    """Powers of the decay that no token needs may be past float32's largest number (exp(88.7)): what is finite by definition is right.  Every product and sum is of float32 quality or 2^-16 of a term, in sums
+    of less than 2^8 terms: 2^-14 of the sum of the terms' magnitudes (the oracle's result of the magnitudes), and half a step of bf16 for the result."""
+    from paper_2509_21275_amd import chunk_linear as cl
+    for d, H, Hk in ((64, 2, 1), (96, 1, 1), (128, 2, 2), (256, 1, 1)):
+        q, k, v, do = (normal((n, h, d), 40 + i) for i, h in enumerate((H, Hk, Hk, H)))
+        lg, scale = torch.full((Hk,), log_decay, device="cuda"), d ** -0.5
+        states, grads = normal((1, Hk, d, d), 45, torch.float32), normal((1, Hk, d, d), 46, torch.float32)
+        desc = cl.make_desc([(0, n, 0 if given else -1, 0)], H, Hk, d, n, 1, scale)
+        ws, left, first = cl.alloc_workspace(desc), torch.empty_like(states), torch.zeros_like(states)
+        o, dq, dk, dv = (torch.empty_like(t) for t in (q, q, k, v))
+        print(n, log_decay, given, d, flush=True)
+        cl.chunk_linear_fwd(desc, q, k, v, lg, states, o, left, ws)
+        cl.chunk_linear_bwd(desc, q, k, v, lg, states, do, grads if given else None, dq, dk, dv, first if given else None, ws)
+        torch.cuda.synchronize()
+        S0, dS = (states[0], grads[0]) if given else (None, None)
+        args, sizes = (q, k, v), [t.double().abs() for t in (q, k, v)]
+        want = [*orc.forward(*args, lg, scale, S0)[:2], *orc.backward(*args, lg, scale, do, S0, dS)[:4]]
+        S0, dS = (None if t is None else t.double().abs() for t in (S0, dS))
+        size = [*orc.forward(*sizes, lg, scale, S0)[:2], *orc.backward(*sizes, lg, scale, do.double().abs(), S0, dS)[:4]]
+        got = [o, left[0], dq, dk, dv, first[0]]
+        for name, g, w, z in list(zip(("o", "state", "dq", "dk", "dv", "d_state"), got, want, size))[:6 if given else 5]:
+            assert bool(torch.isfinite(g).all()), name
+            over = (g.double() - w).abs() - (2.0 ** -8 * w.abs() * (g.dtype == torch.bfloat16) + 2.0 ** -14 * z)
+            assert float(over.max()) <= 0, (name, float(over.max()))
