@@ -15,7 +15,7 @@
  *   k, v, dk, dv  : [total][num_kv_heads][head_dim]
  *   log_decay     : [num_kv_heads] float32, natural logarithm of the decay, normally <= 0 (0: nothing decays, -inf: only the token itself counts; a
  *                   larger one is taken as it is, as long as float32 has the powers of l up to the sequence's length, rounded up to a multiple of 8: past that
- *                   results may be infinite or NaN).  A constant: it has no gradient here.
+ *                   results may be infinite or NaN; a NaN makes all results of its head NaN).  A constant: it has no gradient here.
  *   states        : [num_states][num_kv_heads][head_dim of k][head_dim of v] float32, 16-byte aligned
  * Rows of no segment stay as they are.  States (and their gradients) that a call leaves are summed up in float32, from products that are as good as float32's; products
  * that form outputs, and sums inside the call that go into no state that it leaves, are good to 2^-16 and summed up in float32.  A result is rounded once.  A value that is not finite

@@ -90,8 +90,11 @@ __device__ __forceinline__ Piece find_piece(const LinearSegs& s, int piece) {
   p.rows = min(s.piece_rows, len - p.index * s.piece_rows);
   return p;
 }
-// log2 of a head's decay.  The bound stands for -inf: l^0 is 1 and every other power 0.
-__device__ __forceinline__ float log2_decay(const float* log_decay, int h) { return fmaxf((float)((double)log_decay[h] * 1.4426950408889634), -1000.f); }
+// log2 of a head's decay.  The bound stands for -inf: l^0 is 1 and every other power 0.  A NaN stays one (told by its bits: a comparison, or the maximum alone, would lose it).
+__device__ __forceinline__ float log2_decay(const float* log_decay, int h) {
+  const float x = log_decay[h];
+  return (__float_as_uint(x) & 0x7fffffffu) > 0x7f800000u ? x : fmaxf((float)((double)x * 1.4426950408889634), -1000.f);
+}
 __device__ __forceinline__ float power(float lg, int n) { return __builtin_amdgcn_exp2f(lg * (float)n); }
 
 // Tiles in LDS are rows of D elements and a few more, so that an element's place is linear in its row and column (one address per lane and kind of read, the rest are constants) and neither 16-byte

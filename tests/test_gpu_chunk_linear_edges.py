@@ -1,5 +1,5 @@
 """Linear attention at the edges of what a call may be: gradients of states in place where no sequence is cut; outputs that are rounded to bf16 once;
-decays above 1 whose powers leave float32 soon behind the last token.
+decays above 1 whose powers leave float32 soon behind the last token, and decays that are no numbers.
 
 Tolerance of outputs: half a step of bf16 for the result, 2^-8 of its value.  Before that, what is an operand of a product (weighted scores, the state, the weighted rows in the sums that become the state) is the
 sum of two bf16 terms, off by at most 2^-8 * 2^-8 = 2^-16 of its value, 2^-16 / sqrt(3) in root mean square.  With the oracle's root of the sum of squares of what scores and states contribute (the sums' own
@@ -107,3 +107,36 @@ def test_decays_far_above_one(n, log_decay, given):
             assert bool(torch.isfinite(g).all()), name
             over = (g.double() - w).abs() - (2.0 ** -8 * w.abs() * (g.dtype == torch.bfloat16) + 2.0 ** -14 * z)
             assert float(over.max()) <= 0, (name, float(over.max()))
+
+
+@pytest.mark.parametrize("d", [64, 96, 128, 256])
+def test_a_decay_that_is_no_number_shows(d):
+    """A NaN in log_decay: nothing of that head comes out finite, and the other heads' results have the bits that they have without it."""
+    from paper_2509_21275_amd import chunk_linear as cl
+    H, Hk, lens = 6, 3, [1, 30, 64, 700]
+    total, scale, segs, at = sum(lens), d ** -0.5, [], 0
+    for i, n in enumerate(lens):
+        segs.append((at, n, i if i % 2 else -1, i))
+        at += n
+    q, k, v, do = (normal((total, h, d), 50 + i) for i, h in enumerate((H, Hk, Hk, H)))
+    states, grads = (normal((len(lens), Hk, d, d), 55 + i, torch.float32) for i in range(2))
+    desc = cl.make_desc(segs, H, Hk, d, total, len(lens), scale)
+    ws, slots = cl.alloc_workspace(desc), torch.arange(len(lens), dtype=torch.int32, device="cuda")
+    print(d, flush=True)
+
+    def run(lg):
+        o, dq, dk, dv, left, first, stepped = (torch.zeros_like(t) for t in (q, q, k, v, states, states, states))
+        cl.chunk_linear_fwd(desc, q, k, v, lg, states, o, left, ws)
+        cl.chunk_linear_bwd(desc, q, k, v, lg, states, do, grads, dq, dk, dv, first, ws)
+        single = torch.zeros_like(q[:len(lens)])
+        cl.chunk_linear_step(q[:len(lens)], k[:len(lens)], v[:len(lens)], lg, states, stepped, slots, single, scale)
+        torch.cuda.synchronize()
+        return o, dq, dk, dv, left, first[1::2], single, stepped
+
+    lg = torch.tensor([-0.1, -0.02, -0.005], device="cuda")
+    want = run(lg)
+    lg[1] = float("nan")
+    for got, w in zip(run(lg), want):
+        n = got.shape[1] // Hk
+        assert torch.equal(got[:, :n], w[:, :n]) and torch.equal(got[:, 2 * n:], w[:, 2 * n:])
+        assert not bool(torch.isfinite(got[:, n:2 * n]).any())
