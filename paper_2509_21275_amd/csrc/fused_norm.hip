@@ -53,9 +53,11 @@ __device__ __forceinline__ void gate_and_slope(float g, int kind, float& act, fl
     slope = 1.f;
     return;
   }
-  const float p = sigmoid_of(g);
+  // p = sigmoid(g) and q = sigmoid(-g), both from exp(-|g|): 1 - p has no digits left where the gate is wide open (none at all from g = 17 on)
+  const float e = __expf(-fabsf(g)), larger = __builtin_amdgcn_rcpf(1.f + e), smaller = e * larger;
+  const float p = g < 0.f ? smaller : larger, q = g < 0.f ? larger : smaller;
   act = kind == FUSED_NORM_GATE_SIGMOID ? p : g * p;
-  slope = kind == FUSED_NORM_GATE_SIGMOID ? p * (1.f - p) : p * (1.f + g * (1.f - p));
+  slope = kind == FUSED_NORM_GATE_SIGMOID ? p * q : p * (1.f + g * q);
 }
 
 template <int TPR>
