@@ -11,7 +11,7 @@
  *
  * The backward starts from what the forward has left in residual_out, forming the row's statistics again while it has the row in registers:
  *
- *   t  = d_residual_out + gradient of N at r' applied to d_h             (either may be null; one has to be there)
+ *   t  = d_residual_out + gradient of N at r' applied to d_h             (d_h is there where w_pre is, and only there; d_residual_out may be null beside it)
  *   d_residual = residual_scale * t,   d_gate = block_scale * t * N(y; w_post) * a'(g),   dy = gradient of N at y applied to block_scale * a(g) * t
  *   d_pre_weight = sum over rows of d_h r' / rms(r'),   d_post_weight = sum over rows of block_scale * a(g) * t * y / rms(y)
  *

@@ -781,8 +781,10 @@ struct StepArgs {
 constexpr int step_groups(int d) { return d == 96 ? 8 : 1024 / d; }  // groups of D / 4 threads; a group takes every step_groups-th row of the state
 constexpr int step_threads(int d) { return d / 4 * step_groups(d); }
 // A workgroup takes one row of the batch and one key/value head: a thread four columns of the state and every so many rows, up to sixteen of them loaded at once, before anything else; HEADS query
-// heads at a time.  Bound by memory (the state, read and written).  STREAM: states larger than the last-level cache (256 MiB) pass it by.  us, kept / streamed: 128 sequences of 32 heads of 128 (541 MB)
-// 123 / 115, 64 of 16 of 256 (541 MB) 117 / 110; but 16 of 32 of 128 (68 MB) 15 / 21.
+// heads at a time.  Bound by memory (the state, read and written).  STREAM: calls that read and write more than the last-level cache (256 MiB), that is states of more than 128 MiB, in place or not, pass it by.  What is
+// better depends on what runs until the same states come again.  us, kept / streamed, 32 heads of 128, four sets of states in place by turns (a layer's states among others'): 32 MiB 13.4 / 11.8, 64 MiB
+// 25 / 26, 96 MiB 44 / 36, 160 MiB 69 / 59, 256 MiB 107 / 93, 512 MiB 214 / 185; one set in place again and again: 64 MiB 23 / 23, 96 MiB 32 / 35, 160 MiB 51 / 59, 256 MiB 81 / 92, 512 MiB 216 / 184.  The rule keeps what
+// is small, where either way may be a sixth ahead, and streams what the states of other layers would drive out of the cache.
 constexpr int64_t kStreamBytes = (int64_t)256 << 20;
 template <int D, int HEADS, bool STREAM>
 __global__ __launch_bounds__(step_threads(D)) void step_kernel(const StepArgs a) {
