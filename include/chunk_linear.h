@@ -19,7 +19,8 @@
  *   states        : [num_states][num_kv_heads][head_dim of k][head_dim of v] float32, 16-byte aligned
  * Rows of no segment stay as they are.  States (and their gradients) that a call leaves are summed up in float32, from products that are as good as float32's; products
  * that form outputs, and sums inside the call that go into no state that it leaves, are good to 2^-16 and summed up in float32.  A result is rounded once.  A value that is not finite
- * in a token makes what its sequence has in the same 64 rows (counted from the sequence's start) not finite, and all that follows it.
+ * in a token may make what its sequence has in the same 64 rows (counted from the sequence's start) not finite, and all that follows it (in gradients: that
+ * comes before it).
  *
  * The calls are asynchronous on `hip_stream`, keep nothing, allocate nothing and may be captured into a graph.  The segment table is HOST memory, read during the call; it
  * travels as kernel arguments.  Scratch space is the caller's `workspace` (DEVICE memory, 256-byte aligned, of chunk_linear_workspace_bytes; its contents

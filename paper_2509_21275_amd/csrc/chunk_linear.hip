@@ -22,11 +22,10 @@
 // 115 -> 131 us, 65536 packed of 32/8 389 -> 441, backward of 16384 326 -> 370) and for the weighted v_j in sums k_j^T (l^(L-1-j) v_j) that only become such an operand; three (24 bits) in sums and walks that go into a state or a
 // state's gradient that is left, which is then as exact as float32 sums are.  At head_dim 128 the terms past the first are 38 of the 82 products of a wave in a block of one query head.
 //
-// Measured (us; head_dim 128 unless said).  Forward, 65536 tokens in 20 sequences, 32/8 heads: 389, of that the walk 320 (1.34 GB, 4.2 TB/s), the pieces' sums 75 and 12; 8192 tokens of 32/32
-// 96 (walk 55 of 268 MB, sums 30 and 11), with a state left 113.  Bound by memory while all places are filled; starts (9 of a piece's 30 - 60) and unequal ends are what is above it.
-// Backward, 16384 tokens of 32/8 in 8 sequences: 333, walk_back 160, dq's walk 81, sums 65 + 23 and 16 + 13.  walk_back's 103 GFLOP (terms counted) run at 0.65 PFLOP/s, in
-// its loops at 0.9, where a large product of matrices reaches 1.1: the clock that the chip's power leaves (1.8 GHz) bounds it, not the chain of a step (a sixth fewer cycles
-// per step left the time where it was).  head_dim 256: 8192 tokens of 16/16, forward 163, backward 447; its walks spill registers (24 - 154).
+// Measured (us; head_dim 128 unless said).  Forward, 65536 tokens in 20 sequences, 32/8 heads: 440, of that the walk 355 (1.34 GB, 3.8 TB/s), the pieces' sums 70 and 12; 8192 tokens of 32/32
+// with a state left 124 (walk 69 of 268 MB, sums 36 and 12), without one 110.  Backward, 16384 tokens of 32/8 in 8 sequences: 394, walk_back 180, dq's walk 101, sums 63 + 26 and 16 + 13.  Neither memory nor the
+// matrix units are the bound of the walks: the latter are busy for 34 - 43 % of the cycles of compute units that have work, and waves wait for 40 % of theirs, on the chain of a step with two waves to a SIMD; 15 - 22 % of the units have no work
+// (starts and unequal ends), and the clock is at 2.0 GHz, lower when calls follow each other.  head_dim 256: 8192 tokens of 16/16, forward 196, backward 496; its walks spill registers (61 - 167).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -938,8 +937,11 @@ struct WalkCost {
   int few, places;
 };
 // Rows of a piece: the estimate of all of it that ends first.  Fewer rows: more walks at once, and ends that leave fewer compute units without work; but more states to write, join and read, and k and v
-// are read twice.  A launch takes as long as its work on the places it fills, or as the rounds of its full pieces.  us by rows of a piece (* chosen): 8192 tokens of 32/32 of 128, forward, 256: 120, *512: 96,
-// 1024: 101, uncut: 343; 16384 in 8 sequences of 32/8, backward, 128: 389, *256: 341, 1024: 427, uncut: 2146; 32 sequences of 2000 of 32/8, backward, 512: 1044, *uncut: 741.
+// are read twice.  A launch takes as long as its work on the places it fills, or as the rounds of its full pieces.  us by rows of a piece (* chosen): 8192 tokens of 32/32 of 128, forward, 256: 133, *512: 110,
+// 1024: 112, uncut: 428; 16384 in 8 sequences of 32/8, backward, 128: 447, 192: 388, *256: 394, 512: 401, 1024: 503, uncut: 2804; 32 sequences of 2000 of 32/8, backward, 512: 1185, 1024: 1079, *uncut: 942.  The other head
+// dimensions go by the same figures; their own are within a tenth of the best cut.  64, 16384 tokens: 32/32, forward, 512: 99, 768: 90, *1024: 94, 2048: 125, backward, 512: 243, *1024: 228, 2048: 281; 16/4, forward, 64: 64, *128: 51,
+// 256: 53, 512: 83, backward, 64: 144, *128: 116, 256: 122, 512: 193.  96, 8192 of 32/8: forward, 64: 72, *128: 59, 256: 55, 512: 83, backward, 64: 190, *128: 158, 256: 145, 512: 222.  256, 8192 of 16/16: forward, 256: 265,
+// *512: 213, 1024: 296, backward, 256: 651, *512: 533, 1024: 602.
 int piece_rows(const chunk_linear_desc* d, const WalkCost& c) {
   int longest = 0;
   int64_t blocks = 0;
@@ -983,8 +985,8 @@ int backward_rows(const chunk_linear_desc* d) {
 }
 
 // Up to this many elements of sums before a piece its walk adds them up itself, which saves a launch.  us, added up by join_states_kernel / by the walks: four sequences of 128 - 512 tokens, 8 heads of 64
-// (up to 8 pieces), 16.4 / 13.2; 8 of 2000, 8 heads of 64, 33.1 / 30.2; 16384 tokens, 32 heads of 64, 84 / 81; but 4096 tokens, 8 heads of 64 in 64 pieces 21.4 / 25.6, 16384 of 32/8 of 128
-// in 64 121 / 141.  Not at head_dim 256, whose walks have no registers for it.
+// (up to 8 pieces), 14.9 / 12.9; 8 of 2000, 8 heads of 64, 37.5 / 34.4; 16384 tokens, 32 heads of 64, 96 / 94; but 4096 tokens, 8 heads of 64 in 64 pieces 22.5 / 26.4, 16384 of 32/8 of 128
+// in 64 125 / 154.  Not at head_dim 256, whose walks have no registers for it.
 constexpr int kDirect = 5 * 128 * 128;
 
 template <class F>
