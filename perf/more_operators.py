@@ -1,0 +1,429 @@
+"""What the operators of a decoding step are timed on: pages for new tokens, their keys and values written into the pages, attention of the
+new tokens over the paged cache, and the verification of drafted tokens.
+
+A case is a dict of plain values.  `op` says which call one pass makes:
+
+  extend, truncate   pages of a pool for the new tokens of many requests, with their slots; pages given back by tokens that are taken off again
+  write              rows of keys and values to the slots of a paged cache, in bf16 or e4m3
+  attn               attention of one or a few new tokens of each sequence over its pages
+  verify             drafted tokens against the target's probabilities, from given random numbers
+
+Sequences: `batch` of them, with lengths that are log-normal (`median`, `sigma`) and clipped to `low` .. `high`, drawn from `lengths_seed`; `new` tokens
+of each are new, or, where `ragged`, 0 to `new`.
+"""
+import math
+import random
+
+import torch
+
+own = False
+
+DEVICE = "cuda"
+BF16, F32, F64, I32, I64, E4M3 = torch.bfloat16, torch.float32, torch.float64, torch.int32, torch.int64, torch.float8_e4m3fn
+E4M3_MOST = 448.0
+
+
+# ---- cases ----
+def _tables(name, op, batch, page, median, sigma=1.0, low=1, high=16384, new=1, ragged=False, prefills=0, lengths_seed=0):
+    return {"name": name, "op": op, "batch": batch, "page": page, "median": median, "sigma": sigma, "low": low, "high": high, "new": new, "ragged": ragged,
+            "prefills": prefills, "lengths_seed": lengths_seed}
+
+
+def _write(name, rows, heads, dim, page, cache, pad=0):
+    return {"name": name, "op": "write", "rows": rows, "kv_heads": heads, "dim": dim, "page": page, "cache": cache, "pad": pad}
+
+
+def _attn(name, heads, kv_heads, dim, batch, page, cache, median, sigma=1.0, low=1, high=16384, new=1, ragged=False, lengths_seed=0):
+    return {"name": name, "op": "attn", "heads": heads, "kv_heads": kv_heads, "dim": dim, "batch": batch, "page": page, "cache": cache, "median": median,
+            "sigma": sigma, "low": low, "high": high, "new": new, "ragged": ragged, "lengths_seed": lengths_seed}
+
+
+def _verify(name, batch, drafts, vocab, probabilities, given=True, ragged=False):
+    return {"name": name, "op": "verify", "batch": batch, "drafts": drafts, "vocab": vocab, "probabilities": probabilities, "given": given, "ragged": ragged}
+
+
+def listed():
+    return [
+        # one new token for each of 64 requests: the smallest call, once in every decoding step
+        _tables("extend_64", "extend", 64, 16, 2048),
+        # a large server's step: thousands of requests that decode, some of which come in with their whole prompt
+        _tables("extend_4096_prefills", "extend", 4096, 64, 1024, 1.2, new=4, ragged=True, prefills=16, lengths_seed=1),
+        # rejected drafts are taken off 256 requests, some requests end
+        _tables("truncate_256", "truncate", 256, 16, 2048, new=7, ragged=True, lengths_seed=2),
+        # the same for thousands
+        _tables("truncate_4096", "truncate", 4096, 16, 1024, 1.2, new=7, ragged=True, lengths_seed=3),
+        # keys and values of 256 single tokens
+        _write("write_256", 256, 8, 128, 16, "bf16"),
+        # keys and values of a 64K chunk after its prefill, out of a projection's rows, to 8 bits
+        _write("write_64k_e4m3", 65536, 8, 128, 64, "e4m3", pad=4096),
+        # a few short sequences: bound by launches and latency
+        _attn("attn_4_short_d64", 8, 8, 64, 4, 16, "bf16", 512, high=2048, lengths_seed=4),
+        # a server's batch of skewed lengths
+        _attn("attn_64_skewed", 32, 8, 128, 64, 64, "bf16", 2048, 1.2, 128, 16384, lengths_seed=5),
+        # one long sequence with drafted tokens behind it, cache in 8 bits
+        _attn("attn_128k_drafts_e4m3", 64, 8, 128, 1, 128, "e4m3", 131072, 0.0, 1, 131072, new=5, lengths_seed=6),
+        # wide heads, drafts of different number, pages that no tile is a multiple of
+        _attn("attn_32_drafts_d256", 16, 4, 256, 32, 48, "bf16", 4096, 1.0, 1, 16384, new=8, ragged=True, lengths_seed=7),
+        # a few requests with a few drafts
+        _verify("verify_8x4_32k", 8, 4, 32000, "f32"),
+        # a large batch over a large vocabulary
+        _verify("verify_256x7_128k", 256, 7, 131072, "bf16", ragged=True),
+    ]
+
+
+def _log_uniform(rng, low, high):
+    return int(round(math.exp(rng.uniform(math.log(low), math.log(high)))))
+
+
+def draw(rng):
+    """One more case of the same ranges."""
+    op = rng.choice(["extend", "truncate", "write", "attn", "attn", "attn", "verify", "verify"])
+    page = rng.choice([16, 16, 64, 128, 32, 48, 1, 7, 256])
+    seed = rng.randint(1, 1 << 30)
+    if op in ("extend", "truncate"):
+        case = _tables("", op, _log_uniform(rng, 1, 4096), page, _log_uniform(rng, 16, 4096), rng.choice([0.5, 1.0, 1.2]), 0, 16384 if page > 7 else 2048,
+                       rng.choice([1, 1, rng.randint(2, 16)]), rng.random() < 0.5, rng.choice([0, 0, rng.randint(1, 8)]) if op == "extend" else 0, seed)
+    elif op == "write":
+        heads, dim = rng.choice([8, 8, 4, 2, 1, 16, 32]), rng.choice([128, 128, 64, 96, 256])
+        case = _write("", min(_log_uniform(rng, 1, 65536), (1 << 26) // (heads * dim)), heads, dim, page, rng.choice(["bf16", "e4m3"]), rng.choice([0, heads * dim, 4, 1]))
+    elif op == "attn":
+        heads, kv_heads = rng.choice([(32, 8), (32, 8), (64, 8), (8, 8), (8, 2), (16, 16), (32, 1), (40, 8), (16, 4)])
+        dim, cache = rng.choice([128, 128, 64, 96, 256]), rng.choice(["bf16", "bf16", "e4m3"])
+        high = _log_uniform(rng, 64, 131072)
+        most = (1 << 27) // (kv_heads * dim)  # keys of all sequences, if each were as long as the longest
+        case = _attn("", heads, kv_heads, dim, max(1, min(_log_uniform(rng, 1, 512), most // high)), page, cache, max(1, int(high * rng.uniform(0.1, 1.0))),
+                     rng.choice([0.3, 1.0, 1.2]), 0, high, rng.choice([1, 1, 1, rng.randint(2, 9)]), rng.random() < 0.4, seed)
+    else:
+        vocab = rng.choice([32000, 131072, _log_uniform(rng, 500, 262144)])
+        drafts = rng.randint(1, 8)
+        batch = max(1, min(_log_uniform(rng, 1, 512), (1 << 28) // (vocab * (drafts + 1))))
+        case = _verify("", batch, drafts, vocab, rng.choice(["f32", "f32", "bf16"]), rng.random() < 0.8, rng.random() < 0.5)
+    del case["name"]
+    return case
+
+
+# ---- what a case is made of ----
+def _sequences(case):
+    """Tokens in the cache behind the new ones, and new tokens, of each sequence."""
+    rng = random.Random(case["lengths_seed"])
+    n = case["batch"]
+    lens = [min(max(int(rng.lognormvariate(math.log(case["median"]), case["sigma"])), case["low"]), case["high"]) for _ in range(n)]
+    new = [rng.randint(0, case["new"]) if case["ragged"] else case["new"] for _ in range(n)]
+    if case["op"] == "attn":  # the new tokens are in the cache already; one sequence at least has one
+        new[0] = max(1, new[0])
+        return [max(a, b) for a, b in zip(lens, new)], new
+    return lens, new
+
+
+def _table_work(case):
+    """Old lengths, new or dropped tokens, most pages to a request, pages that change hands."""
+    lens, new = _sequences(case)
+    page = case["page"]
+    if case["op"] == "extend":
+        rng = random.Random(case["lengths_seed"] + 1)
+        at = sorted(rng.sample(range(len(lens)), min(len(lens), case["prefills"])))  # prompts that come in
+        prompts = {i: rng.randint(1, max(1, case["high"] // 4)) for i in at}
+        lens, new = [0 if i in prompts else a for i, a in enumerate(lens)], [prompts.get(i, b) for i, b in enumerate(new)]
+        moved = sum(-(-(a + b) // page) + -a // page for a, b in zip(lens, new))
+        longest = max(a + b for a, b in zip(lens, new))
+    else:
+        new = [a if i % 16 == 15 else min(a, b) for i, (a, b) in enumerate(zip(lens, new))]  # every sixteenth request ends
+        moved = sum(-(-a // page) + -(a - b) // page for a, b in zip(lens, new))
+        longest = max(lens)
+    return lens, new, max(1, -(-longest // page)), moved
+
+
+# ---- inputs ----
+def prepare(case, seed):
+    gen = torch.Generator(device=DEVICE).manual_seed(seed)
+    op = case["op"]
+
+    def normal(*shape, dtype=BF16, scale=1.0):
+        x = torch.randn(shape, generator=gen, device=DEVICE, dtype=F32).mul_(scale)
+        return (x.clamp_(-E4M3_MOST, E4M3_MOST) if dtype == E4M3 else x).to(dtype)
+
+    def ints(x, dtype=I32):
+        return torch.tensor(x, dtype=dtype, device=DEVICE)
+
+    if op in ("extend", "truncate"):
+        lens, new, width, moved = _table_work(case)
+        page, n = case["page"], len(lens)
+        held = [-(-a // page) for a in lens]
+        pages = sum(held) + (moved if op == "extend" else 0) + 5
+        order = torch.randperm(pages, generator=gen, device=DEVICE, dtype=I64).to(I32)
+        table = torch.full((n, width), -1, dtype=I32, device=DEVICE)
+        owned = torch.arange(width, device=DEVICE)[None] < ints(held)[:, None]
+        table[owned] = order[:sum(held)]
+        free = torch.full((pages,), -1, dtype=I32, device=DEVICE)
+        free[:pages - sum(held)] = order[sum(held):]
+        state = {"case": case, "kv_len": ints(lens), "held": ints(held), "table": table, "free": free, "num_free": ints([pages - sum(held)]),
+                 "change": ints(new), "kv_len_out": ints(lens), "held_out": ints(held), "num_free_out": ints([0])}
+        if op == "extend":
+            rows = sum(new)
+            state.update(q_start=torch.empty(n + 1, dtype=I32, device=DEVICE), granted=torch.empty(n, dtype=I32, device=DEVICE),
+                         slots=torch.empty(max(1, rows), dtype=I64, device=DEVICE))
+        if own:
+            from paper_2509_21275_amd import paged_cache
+            state["desc"] = paged_cache.make_desc(n, width, page, pages)
+            state["ws"] = paged_cache.alloc_workspace(state["desc"], DEVICE)
+        return state
+    if op == "write":
+        rows, heads, dim, page = case["rows"], case["kv_heads"], case["dim"], case["page"]
+        pages = -(-rows // page) + 3
+        ctype = E4M3 if case["cache"] == "e4m3" else BF16
+        k, v = (normal(rows, heads * dim + case["pad"], scale=2.0)[:, :heads * dim].unflatten(1, (heads, dim)) for _ in range(2))
+        scales = [torch.rand(heads, generator=gen, device=DEVICE) * 0.02 + 0.005 for _ in range(2)] if case["cache"] == "e4m3" else [None, None]
+        slots = torch.randperm(pages * page, generator=gen, device=DEVICE)[:rows]
+        slots[rows // 2::97] = -1  # rows of padding
+        shape = (pages, heads, page, dim)
+        return {"case": case, "k": k, "v": v, "slots": slots, "k_scale": scales[0], "v_scale": scales[1], "k_cache": torch.zeros(shape, dtype=ctype, device=DEVICE),
+                "v_cache": torch.zeros(shape, dtype=ctype, device=DEVICE)}
+    if op == "attn":
+        lens, new = _sequences(case)
+        H, heads, dim, page, n = case["heads"], case["kv_heads"], case["dim"], case["page"], case["batch"]
+        width = max(1, -(-max(lens) // page))
+        held = [-(-a // page) for a in lens]
+        pages = sum(held) + 3
+        table = torch.full((n, width), -1, dtype=I32, device=DEVICE)
+        table[torch.arange(width, device=DEVICE)[None] < ints(held)[:, None]] = torch.randperm(pages, generator=gen, device=DEVICE)[:sum(held)].to(I32)
+        total = sum(new)
+        quiet = case["cache"] == "bf16"
+        ctype = BF16 if quiet else E4M3
+        # (values of 8 bits stand for up to 448 scales)
+        k, v = (normal(pages, heads, page, dim, dtype=ctype, scale=1.0 if quiet else 100.0) for _ in range(2))
+        scales = [None, None] if quiet else [(torch.rand(heads, generator=gen, device=DEVICE) * 0.5 + 0.75) / 100.0 for _ in range(2)]
+        state = {"case": case, "q": normal(total, H, dim), "k_cache": k, "v_cache": v, "k_scale": scales[0], "v_scale": scales[1], "table": table,
+                 "kv_len": ints(lens), "q_start": ints([sum(new[:i]) for i in range(n + 1)]), "most_new": max(1, max(new)), "longest": max(1, max(lens)),
+                 "o": torch.empty((total, H, dim), dtype=BF16, device=DEVICE), "lse": torch.empty((H, total), device=DEVICE), "scale": dim ** -0.5}
+        if own:
+            from paper_2509_21275_amd import paged_attn
+            state["desc"] = paged_attn.make_desc(H, heads, dim, n, total, page, pages, width, state["scale"], case["cache"])
+            state["ws"] = paged_attn.alloc_workspace(state["desc"], DEVICE)
+        return state
+    n, K, V = case["batch"], case["drafts"], case["vocab"]
+    ptype = F32 if case["probabilities"] == "f32" else BF16
+    logits = normal(n, K + 1, V, dtype=F32, scale=2.5)
+    guess = torch.softmax(logits[:, :K] + normal(n, K, V, dtype=F32, scale=0.6), -1)
+    tokens = torch.multinomial(guess.flatten(0, 1), 1, generator=gen).view(n, K).to(I32)
+    target = torch.softmax(logits, -1).to(ptype)
+    del logits
+    state = {"case": case, "target": target, "draft": guess.to(ptype) if case["given"] else None, "tokens": tokens, "count": None,
+             "uniforms": torch.rand((n, K), generator=gen, device=DEVICE), "last_uniform": torch.rand(n, generator=gen, device=DEVICE),
+             "accepted": torch.empty(n, dtype=I32, device=DEVICE), "rejected": torch.empty(n, dtype=I32, device=DEVICE),
+             "out": torch.empty((n, K + 1), dtype=I32, device=DEVICE)}
+    if case["ragged"]:
+        state["count"] = torch.randint(0, K + 1, (n,), generator=gen, device=DEVICE, dtype=I32)
+    if own:
+        from paper_2509_21275_amd import draft_verify
+        state["ws"] = draft_verify.alloc_workspace(n, K, V, DEVICE)
+    return state
+
+
+# ---- the passes ----
+def run(state):
+    return {"extend": _run_extend, "truncate": _run_truncate, "write": _run_write, "attn": _run_attn, "verify": _run_verify}[state["case"]["op"]](state)
+
+
+def _before(x):
+    """Sums of the entries before each."""
+    return torch.cumsum(x, 0) - x
+
+
+def _run_extend(s):
+    page = s["case"]["page"]
+    if own:
+        from paper_2509_21275_amd import paged_cache
+        paged_cache.paged_cache_extend(s["desc"], s["change"], s["kv_len"], s["held"], s["table"], s["free"], s["num_free"], s["kv_len_out"], s["held_out"],
+                                       s["num_free_out"], s["q_start"], s["slots"], s["granted"], s["ws"])
+    else:
+        old, held, new = s["kv_len"].to(I64), s["held"].to(I64), s["change"].to(I64)
+        need = ((old + new + page - 1) // page - held).clamp(min=0)
+        served = (need == 0) | (torch.cumsum(need, 0) <= s["num_free"])
+        taken = torch.where(served, need, 0)
+        # each new page, from the top of the stack, in the order of the requests
+        width = s["table"].shape[1]
+        b = torch.arange(width, device=DEVICE)[None] - held[:, None]
+        place = s["num_free"] - 1 - _before(need)[:, None] - b
+        s["table"].copy_(torch.where((b >= 0) & (b < taken[:, None]), s["free"][place.clamp(0, s["free"].shape[0] - 1)], s["table"]))
+        s["num_free_out"].copy_(s["num_free"] - taken.sum())
+        s["held_out"].copy_(held + taken)
+        s["kv_len_out"].copy_(old + torch.where(served, new, 0))
+        s["granted"].copy_(served)
+        s["q_start"][0] = 0
+        s["q_start"][1:] = torch.cumsum(new, 0)
+        row = torch.arange(s["slots"].shape[0], device=DEVICE)
+        i = torch.searchsorted(s["q_start"][1:].to(I64), row, right=True).clamp(max=len(new) - 1)
+        at = old[i] + row - s["q_start"][i]
+        slot = s["table"][i, (at // page).clamp(max=width - 1)].to(I64) * page + at % page
+        s["slots"].copy_(torch.where(served[i] & (row < s["q_start"][-1]), slot, -1))
+    return {x: s[x] for x in ("kv_len_out", "held_out", "num_free_out", "table", "q_start", "slots", "granted")}
+
+
+def _run_truncate(s):
+    page = s["case"]["page"]
+    if own:
+        from paper_2509_21275_amd import paged_cache
+        paged_cache.paged_cache_truncate(s["desc"], s["change"], s["kv_len"], s["held"], s["table"], s["free"], s["num_free"], s["kv_len_out"], s["held_out"],
+                                         s["num_free_out"], s["ws"])
+    else:
+        left = (s["kv_len"] - s["change"].clamp(min=0)).clamp(min=0).to(I64)
+        keep = torch.minimum(s["held"].to(I64), (left + page - 1) // page)
+        back = s["held"].to(I64) - keep
+        # pages that go back, in the order of the requests and of their tables
+        b = torch.arange(s["table"].shape[1], device=DEVICE)[None] - keep[:, None]
+        gone = (b >= 0) & (b < back[:, None])
+        s["free"][(s["num_free"] + _before(back)[:, None] + b)[gone]] = s["table"][gone]
+        s["num_free_out"].copy_(s["num_free"] + back.sum())
+        s["held_out"].copy_(keep)
+        s["kv_len_out"].copy_(left)
+    return {x: s[x] for x in ("kv_len_out", "held_out", "num_free_out", "free")}
+
+
+def _run_write(s):
+    if own:
+        from paper_2509_21275_amd import paged_cache
+        paged_cache.paged_cache_write(s["k"], s["v"], s["slots"], s["k_cache"], s["v_cache"], s["k_scale"], s["v_scale"])
+    else:
+        page, live = s["case"]["page"], s["slots"] >= 0
+        at = s["slots"][live]
+
+        def put(x, scale, cache):
+            x = x[live]
+            if scale is not None:
+                x = (x.to(F32) / scale[:, None]).clamp(-E4M3_MOST, E4M3_MOST).to(E4M3)
+            cache.view(torch.uint8 if scale is not None else BF16)[at // page, :, at % page] = x.view(torch.uint8) if scale is not None else x
+
+        put(s["k"], s["k_scale"], s["k_cache"])
+        put(s["v"], s["v_scale"], s["v_cache"])
+    return {"k_cache": s["k_cache"], "v_cache": s["v_cache"]}
+
+
+def _run_attn(s):
+    if own:
+        from paper_2509_21275_amd import paged_attn
+        paged_attn.paged_attn_fwd(s["desc"], s["q"], s["k_cache"], s["v_cache"], s["table"], s["kv_len"], s["q_start"], s["o"], s["lse"], s["ws"],
+                                  k_scale=s["k_scale"], v_scale=s["v_scale"])
+        return {"o": s["o"], "lse": s["lse"]}
+    case, page, n, R = s["case"], s["case"]["page"], s["case"]["batch"], s["most_new"]
+    H, heads, dim = case["heads"], case["kv_heads"], case["dim"]
+    # every sequence as long as the longest, every one with as many new tokens as the most
+    key = torch.arange(s["longest"], device=DEVICE)
+    inside = key[None] < s["kv_len"][:, None]
+    of = s["table"][:, key // page].to(I64).clamp(min=0)
+
+    def rows(cache, scale):  # [sequence, head, key, dim]
+        x = cache.view(torch.uint8)[of, :, (key % page)[None]].view(cache.dtype).to(F32) if scale is not None else cache[of, :, (key % page)[None]].to(F32)
+        x = x.permute(0, 2, 1, 3)
+        return x * scale[None, :, None, None] if scale is not None else x
+
+    count = s["q_start"][1:] - s["q_start"][:-1]
+    j = torch.arange(R, device=DEVICE)
+    live = j[None] < count[:, None]
+    row = (s["q_start"][:-1, None] + j[None])[live].to(I64)
+    q = torch.zeros((n, R, H, dim), device=DEVICE)
+    q[live] = s["q"].to(F32)[row]
+    q = q.view(n, R, heads, H // heads, dim).permute(0, 2, 1, 3, 4).reshape(n, heads, -1, dim)
+    scores = torch.matmul(q, rows(s["k_cache"], s["k_scale"]).transpose(-1, -2).contiguous()).view(n, heads, R, H // heads, -1) * s["scale"]
+    seen = inside[:, None] & (key[None, None] <= (s["kv_len"] - count)[:, None, None] + j[None, :, None])
+    scores = scores.masked_fill(~seen[:, None, :, None], -math.inf)
+    most = scores.amax(-1, keepdim=True).clamp(min=-1e30)
+    p = torch.exp(scores - most)
+    total = p.sum(-1, keepdim=True)
+    o = torch.matmul(p.flatten(2, 3), rows(s["v_cache"], s["v_scale"])).view(n, heads, R, H // heads, dim) / total.clamp(min=1e-30)
+    s["o"][row] = o.permute(0, 2, 1, 3, 4).reshape(n, R, H, dim)[live].to(BF16)
+    s["lse"][:, row] = (most + torch.log(total)).squeeze(-1).permute(0, 2, 1, 3).reshape(n, R, H)[live].T
+    return {"o": s["o"], "lse": s["lse"]}
+
+
+def _run_verify(s):
+    n, K = s["tokens"].shape
+    if own:
+        from paper_2509_21275_amd import draft_verify
+        draft_verify.draft_verify(s["target"], s["draft"], s["tokens"], s["count"], s["uniforms"], s["last_uniform"], s["accepted"], s["rejected"], s["out"], s["ws"])
+    else:
+        at, j = s["tokens"].to(I64)[..., None], torch.arange(K, device=DEVICE)
+        count = s["count"] if s["count"] is not None else torch.full((n,), K, device=DEVICE, dtype=I32)
+        # in 64 bits products and sums of two are exact enough that no border is missed
+        p = s["target"][:, :K].gather(-1, at).squeeze(-1).to(F64)
+        q = s["draft"].gather(-1, at).squeeze(-1).to(F64) if s["draft"] is not None else torch.ones_like(p)
+        stands = (s["uniforms"].to(F64) * q < p) & (j[None] < count[:, None])
+        accepted = torch.cumprod(stands.to(I64), -1).sum(-1)
+        i = torch.arange(n, device=DEVICE)
+        row = s["target"][i, accepted].to(F64)
+        some = (accepted < count)[:, None]
+        last = accepted.clamp(max=K - 1)
+        if s["draft"] is not None:
+            left = torch.where(some, (row - s["draft"][i, last].to(F64)).clamp(min=0), row)
+        else:
+            left = torch.where(some & (torch.arange(row.shape[1], device=DEVICE)[None] == at[i, last]), 0.0, row)
+        left = torch.where((left > 0).any(-1, keepdim=True), left, row)
+        sums = torch.cumsum(left, -1)
+        found = (sums <= s["last_uniform"].to(F64)[:, None] * sums[:, -1:]).sum(-1)
+        s["accepted"].copy_(accepted)
+        s["rejected"].copy_(count - accepted)
+        place = torch.arange(K + 1, device=DEVICE)[None]
+        drafted = torch.nn.functional.pad(s["tokens"], (0, 1))
+        s["out"].copy_(torch.where(place < accepted[:, None], drafted, torch.where(place == accepted[:, None], found[:, None], -1)))
+    return {"accepted": s["accepted"], "rejected": s["rejected"], "out": s["out"]}
+
+
+# ---- what a pass cannot do without ----
+def work(case):
+    op = case["op"]
+    if op in ("extend", "truncate"):
+        lens, new, _, moved = _table_work(case)
+        rows = sum(new) if op == "extend" else 0
+        return {"bytes": 20 * len(lens) + 8 * moved + 8 * rows + 8 + 8 * len(lens) * (op == "extend"), "flops": 0}
+    if op == "write":
+        elements = 2 * case["rows"] * case["kv_heads"] * case["dim"]
+        return {"bytes": elements * (3 if case["cache"] == "e4m3" else 4) + 8 * case["rows"], "flops": 0}
+    if op == "attn":
+        lens, new = _sequences(case)
+        size = 1 if case["cache"] == "e4m3" else 2
+        seen = sum(a for a, b in zip(lens, new) if b > 0)
+        pairs = sum(b * a - b * (b - 1) // 2 for a, b in zip(lens, new))
+        return {"bytes": 2 * seen * case["kv_heads"] * case["dim"] * size + sum(new) * case["heads"] * (4 * case["dim"] + 4), "flops": 4 * pairs * case["heads"] * case["dim"]}
+    # one row of the target's probabilities for each request, and one of the draft's where a draft is rejected (most of the time one of several is)
+    size = 4 if case["probabilities"] == "f32" else 2
+    return {"bytes": case["batch"] * case["vocab"] * size * (2 if case["given"] else 1), "flops": 0}
+
+
+# ---- the definitions in 64 bits ----
+def exact(case, seed):
+    op = case["op"]
+    if op in ("extend", "truncate", "verify"):
+        return None  # whole numbers
+    s = prepare(case, seed)
+    if op == "write":
+        out = {}
+        page = case["page"]
+        for x in ("k", "v"):
+            cache = s[x + "_cache"].to(F64)
+            value = s[x].to(F64)
+            if s[x + "_scale"] is not None:  # the nearest of the values that 8 bits hold: steps of 1/8 of a power of two, of 2^-9 at the least
+                value = value / s[x + "_scale"].to(F64)[:, None]
+                step = torch.exp2(torch.floor(torch.log2(value.abs().clamp(min=2.0 ** -6))) - 3)
+                value = (torch.round(value / step) * step).clamp(-E4M3_MOST, E4M3_MOST)
+            live = s["slots"] >= 0
+            at = s["slots"][live]
+            cache.transpose(1, 2)[at // page, at % page] = value[live]
+            out[x + "_cache"] = cache
+        return out
+    H, heads, page = case["heads"], case["kv_heads"], case["page"]
+    G = H // heads
+    o, lse = torch.empty(s["o"].shape, dtype=F64, device=DEVICE), torch.empty(s["lse"].shape, dtype=F64, device=DEVICE)
+    starts, lens, table = s["q_start"].tolist(), s["kv_len"].tolist(), s["table"].tolist()
+    for i, L in enumerate(lens):
+        count = starts[i + 1] - starts[i]
+        if count == 0:
+            continue
+        pages = torch.tensor(table[i][:-(-L // page)], device=DEVICE)
+        k, v = ((s[x + "_cache"].view(torch.uint8)[pages].view(E4M3) if s[x + "_scale"] is not None else s[x + "_cache"][pages]).to(F64).transpose(0, 1).flatten(1, 2)[:, :L]
+                * (s[x + "_scale"].to(F64)[:, None, None] if s[x + "_scale"] is not None else 1.0) for x in ("k", "v"))
+        for j in range(count):
+            row, seen = starts[i] + j, L - count + j + 1
+            x = torch.matmul(s["q"][row].to(F64).view(heads, G, -1), k[:, :seen].transpose(1, 2)) * s["scale"]
+            z = torch.logsumexp(x, -1, keepdim=True)
+            o[row] = torch.matmul(torch.exp(x - z), v[:, :seen]).reshape(H, -1)
+            lse[:, row] = z.flatten()
+    return {"o": o, "lse": lse}
