@@ -89,8 +89,8 @@ def draw(rng):
     elif op == "attn":
         heads, kv_heads = rng.choice([(32, 8), (32, 8), (64, 8), (8, 8), (8, 2), (16, 16), (32, 1), (40, 8), (16, 4)])
         dim, cache = rng.choice([128, 128, 64, 96, 256]), rng.choice(["bf16", "bf16", "e4m3"])
-        high = _log_uniform(rng, 64, 131072)
-        most = (1 << 27) // (kv_heads * dim)  # keys of all sequences, if each were as long as the longest
+        most = 240000000 // (kv_heads * dim)  # keys of all sequences, if each were as long as the longest
+        high = _log_uniform(rng, 64, min(131072, most))
         case = _attn("", heads, kv_heads, dim, max(1, min(_log_uniform(rng, 1, 512), most // high)), page, cache, max(1, int(high * rng.uniform(0.1, 1.0))),
                      rng.choice([0.3, 1.0, 1.2]), 0, high, rng.choice([1, 1, 1, rng.randint(2, 9)]), rng.random() < 0.4, seed)
     else:
