@@ -8,11 +8,13 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libchunk_attn.so")
-SOURCES = ["plan.cpp", "chunk_plan.cpp", "chunk_sched.cpp", "fused_ce.hip", "chunk_rope.hip", "fused_norm.hip", "chunk_linear.hip", "fwd_kernel.hip", "bwd_kernel.hip", "bwd_fused_kernel.hip", "bwd_share_kernel.hip", "measure.hip", "api.hip"]
+SOURCES = ["plan.cpp", "chunk_plan.cpp", "chunk_sched.cpp", "fused_ce.hip", "chunk_rope.hip", "fused_norm.hip", "chunk_linear.hip", "paged_cache.hip", "paged_attn.hip", "draft_verify.hip", "fwd_kernel.hip", "bwd_kernel.hip", "bwd_fused_kernel.hip", "bwd_share_kernel.hip", "measure.hip", "api.hip"]
 # -packed-fp32-ops off: the compiler must not form packed fp32 VALU instructions on this target
 # -fno-honor-nans: no input of these kernels is NaN; it lets max/compare lower to single instructions
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function", "-fno-honor-nans",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
+# ... but for those that say what becomes of a NaN
+HONOR_NANS = {"paged_cache.hip", "paged_attn.hip", "draft_verify.hip"}
 
 
 def build_library(verbose: bool = False) -> str:
@@ -22,7 +24,7 @@ def build_library(verbose: bool = False) -> str:
 
     def compile_one(src):
         obj = os.path.join(bdir, os.path.splitext(src)[0] + ".o")
-        cmd = [hipcc, *FLAGS, "-x", "hip", "-c", os.path.join(CSRC, src), "-o", obj]
+        cmd = [hipcc, *FLAGS, *(["-fhonor-nans"] if src in HONOR_NANS else []), "-x", "hip", "-c", os.path.join(CSRC, src), "-o", obj]
         r = subprocess.run(cmd, capture_output=True, text=True)
         msgs = "\n".join(l for l in (r.stdout + r.stderr).splitlines() if "packed-fp32-ops" not in l)
         if r.returncode != 0:

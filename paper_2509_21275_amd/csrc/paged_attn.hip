@@ -1,0 +1,565 @@
+// Attention of new tokens over a paged cache (include/paged_attn.h).
+//
+// Rows: the new tokens of a sequence times the query heads of a key/value head, 32 of them to a block (the columns of a 32 x 32 product).  Units: a block of rows against a block of kBlockKeys keys.
+// All units of a key/value head, sequence after sequence, are dealt to `shares` workgroups in equal shares, so that ragged lengths fill the chip evenly and one long sequence as well as many
+// short ones.  A workgroup finds its share itself, from the lengths (a sum over the sequences: the host does not know them).  Inside it, each wave takes every fourth tile of 32 keys
+// with a softmax (maximum, sum, weighted values) of its own; what belongs to one block of rows is put together in LDS when the workgroup leaves it, and written, or, where the block's walk began in or goes on
+// in another share, left in the workspace for join_kernel.
+//
+// A wave's tile: K from memory into the registers of the product K Q^T (no LDS: each key is read by one wave, once), V in whole rows through registers into LDS, from where it is read
+// transposed; both are loaded one tile ahead.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "../../include/paged_attn.h"
+#include "kernels.hpp"
+#include "operators.hpp"
+#include "paged.hpp"
+#include "tiles.hpp"
+
+namespace chunk_attn {
+namespace {
+
+constexpr int kWaves = 4, kThreads = 64 * kWaves;
+constexpr int kRows = 32;               // rows of a block
+constexpr int kTile = 32;               // keys of a tile
+constexpr int kBlockKeys = kTile * kWaves;
+constexpr int kLeastShare = 2;          // units of a share, at least
+constexpr float kFloor = -3e38f;        // of a running maximum: what is masked (-inf) stays below it, so that no difference of two infinities is formed
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+struct AttnArgs {
+  const __bf16* q;
+  int64_t q_stride;
+  const void *k, *v;
+  const float *k_scale, *v_scale;
+  const int32_t *table, *kv_len, *q_start;
+  __bf16* o;
+  int64_t o_stride;
+  float* lse;
+  float* parts;   // two of each (share, head): the block of rows that came from the share before, and the one that goes on in the next
+  int32_t* cuts;  // [shares][kCut]: the block of rows that goes on in the next share
+  int32_t num_seqs, total_q, heads, group, page_size, num_pages, max_pages, shares;
+  float scale_log2;
+  Divide by_page, by_group;
+};
+enum { kCutSeq, kCutBlock, kCutShares, kCut = 4 };  // sequence, block of rows, shares that it reaches into (0: none)
+
+template <int D>
+constexpr int part_floats() { return kRows * (D + 2); }
+
+// Sequence i, its numbers brought into their ranges.
+struct Sequence {
+  int len, rows, first_row;  // tokens; rows of a key/value head; first row of q
+  __device__ int row_blocks() const { return (rows + kRows - 1) / kRows; }
+  __device__ int key_blocks() const { return max(1, (int)(((unsigned)len + kBlockKeys - 1) / kBlockKeys)); }
+  __device__ int64_t units() const { return (int64_t)row_blocks() * key_blocks(); }
+};
+__device__ __forceinline__ Sequence sequence_at(const AttnArgs& a, int i) {
+  Sequence s;
+  const int most = a.max_pages * a.page_size;
+  s.len = min(max(a.kv_len[i], 0), most);
+  s.first_row = max(a.q_start[i], 0);
+  s.rows = max(min(a.q_start[i + 1], a.total_q) - s.first_row, 0) * a.group;
+  return s;
+}
+
+__device__ __forceinline__ int64_t wave_sum_up_to(int64_t x) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int64_t y = __shfl_up(x, o);
+    if (lane >= o) x += y;
+  }
+  return x;
+}
+
+// A value that all lanes of a wave have, as one the compiler knows to be so.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t uniform64(int64_t x) { return (int64_t)(((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32) | (uint32_t)uniform((int)x)); }
+
+// 16 bytes of the cache.
+__device__ __forceinline__ u32x4 load16(const char* p) { return *reinterpret_cast<const u32x4*>(p); }
+// Eight e4m3 numbers as bf16, which has them all.
+__device__ __forceinline__ bf16x8 widen8(unsigned a, unsigned b) {
+  bf16x8 r;
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(w ? b : a, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w ? b : a, true);
+    r[4 * w] = (__bf16)lo[0];
+    r[4 * w + 1] = (__bf16)lo[1];
+    r[4 * w + 2] = (__bf16)hi[0];
+    r[4 * w + 3] = (__bf16)hi[1];
+  }
+  return r;
+}
+// Whether one of eight bf16 numbers is infinite or none.
+__device__ __forceinline__ bool some_not_finite(bf16x8 x) {
+  bool r = false;
+  const u32x4 w = __builtin_bit_cast(u32x4, x);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) r |= (w[e] & 0x7f80u) == 0x7f80u || (w[e] & 0x7f800000u) == 0x7f800000u;
+  return r;
+}
+
+// Bytes from row to row of V's tile in LDS: 64 bytes past a multiple of 256 (192: 64 short of it), so that the four rows of a transposed read lie on different banks.
+template <int D>
+constexpr int v_pitch() { return D == 96 ? 192 : D * 2 + 64; }
+
+template <int D, bool E4M3>
+__global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_kernel(const AttnArgs a) {
+  constexpr int kBytes = E4M3 ? 1 : 2;                  // of a number in the cache
+  constexpr int kDims = D / 32;                         // 32 dimensions of the output, or of the scores' sum, at a time
+  constexpr int kPitch = v_pitch<D>() / 2;              // elements
+  constexpr int kRowChunks = D * kBytes / 16, kVChunks = kRowChunks / 2;  // 16-byte chunks of a row; of a tile, for each lane
+  __shared__ __attribute__((aligned(16))) __bf16 tiles[kWaves][kTile * kPitch];
+  __shared__ float maxima[kWaves][kRows], sums[kWaves][kRows];
+  __shared__ int64_t wave_units[kWaves];
+  __shared__ int64_t start_unit;
+  __shared__ int start_seq;
+  __shared__ unsigned bad_rows[kWaves];
+  static_assert(sizeof(tiles) >= 2 * kRows * D * 4, "two waves' values find room");
+
+  const int head = blockIdx.x % a.heads, share = blockIdx.x / a.heads;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
+
+  // ---- the share: units first .. last - 1 of all ----
+  const int each = (a.num_seqs + kThreads - 1) / kThreads;
+  const int seq0 = min((int)threadIdx.x * each, a.num_seqs), seq1 = min(seq0 + each, a.num_seqs);
+  int64_t mine = 0;
+  for (int i = seq0; i < seq1; ++i) mine += sequence_at(a, i).units();
+  int64_t before = wave_sum_up_to(mine);
+  if (lane == 63) wave_units[wave] = before;
+  if (threadIdx.x == 0) start_seq = -1;
+  before -= mine;
+  __syncthreads();
+  int64_t total = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < wave) before += wave_units[w];
+    total += wave_units[w];
+  }
+  const int64_t size = uniform64(max((int64_t)kLeastShare, (total + a.shares - 1) / a.shares));
+  const int64_t first = share * size, last = uniform64(min(first + size, total));
+  if (first >= before && first < before + mine) {
+    int64_t at = first - before;
+    int i = seq0;
+    while (true) {
+      const int64_t u = sequence_at(a, i).units();
+      if (at < u) break;
+      at -= u;
+      ++i;
+    }
+    start_seq = i;
+    start_unit = at;
+  }
+  __syncthreads();
+  int seq = uniform(start_seq);
+  if (threadIdx.x == 0 && head == 0) a.cuts[share * kCut + kCutShares] = 0;
+  if (seq < 0 || first >= total) return;
+  int64_t in_seq = uniform64(start_unit);  // units of the sequence before the next
+  const float k_scale = E4M3 ? a.k_scale[head] : 1.f, v_scale = E4M3 ? a.v_scale[head] : 1.f;
+  const float scale = a.scale_log2 * k_scale;
+  const char *const k_base = (const char*)a.k, *const v_base = (const char*)a.v;
+
+  for (int64_t unit = first; unit < last;) {
+    Sequence s = sequence_at(a, seq);
+    s = Sequence{uniform(s.len), uniform(s.rows), uniform(s.first_row)};
+    if (s.rows == 0 || in_seq >= s.units()) {
+      ++seq;
+      in_seq = 0;
+      continue;
+    }
+    const int key_blocks = s.key_blocks();
+    const int row_block = (int)(in_seq / key_blocks), block0 = (int)(in_seq - (int64_t)row_block * key_blocks);
+    const int block1 = (int)min((int64_t)key_blocks, block0 + (last - unit));
+    // rows of this lane's column
+    const int row = row_block * kRows + col;
+    const bool live = row < s.rows;
+    const int token = a.by_group(min(row, s.rows - 1)), q_row = s.first_row + token, q_head = head * a.group + min(row, s.rows - 1) - token * a.group;
+    const int tokens = s.rows / a.group;
+    const int seen = s.len - tokens + token + 1;  // keys that the row sees (none if <= 0)
+    const int first_seen = s.len - tokens + a.by_group(row_block * kRows) + 1;                               // of the block's first row,
+    const int most_seen = max(0, s.len - tokens + a.by_group(min(row_block * kRows + kRows, s.rows) - 1) + 1);  // and of its last
+    // operand B of K Q^T: in step 2 t + u, half h has dimensions 32 t + 16 h + 8 u .. + 7
+    bf16x8 q[2 * kDims];
+    {
+      const __bf16* const p = a.q + (int64_t)q_row * a.q_stride + (int64_t)q_head * D + 16 * half;
+#pragma unroll
+      for (int n = 0; n < 2 * kDims; ++n) {
+        const Loose8 x = *reinterpret_cast<const Loose8*>(p + (n >> 1) * 32 + (n & 1) * 8);
+        q[n] = __builtin_bit_cast(bf16x8, x);
+        if (!live) q[n] = bf16x8{};
+      }
+    }
+    f32x16 acc[kDims] = {};
+    float m = kFloor, l = 0.f;
+
+    // ---- the walk ----
+    const int tile1 = min(block1 * kWaves, (most_seen + kTile - 1) / kTile);
+    const int32_t* const pages = a.table + (int64_t)seq * a.max_pages;
+    // row of the cache that holds key `col` of a tile, or -1
+    auto cache_row = [&](int tile) {
+      const int key = tile * kTile + col;
+      if (key >= most_seen) return -1;
+      const int page = a.by_page(key), number = pages[page];
+      return number >= 0 && number < a.num_pages ? (int)(number * a.heads * a.page_size + head * a.page_size + key - page * a.page_size) : -1;
+    };
+    u32x4 kr[kDims * kBytes], vr[kVChunks];
+    auto load_tile = [&](int at) {
+      const char* const p = k_base + (int64_t)max(at, 0) * (D * kBytes) + half * (16 * kBytes);
+#pragma unroll
+      for (int t = 0; t < kDims; ++t)
+#pragma unroll
+        for (int u = 0; u < kBytes; ++u) kr[t * kBytes + u] = load16(p + t * (32 * kBytes) + u * 16);
+#pragma unroll
+      for (int n = 0; n < kVChunks; ++n) {
+        const int c = lane + 64 * n, r = c / kRowChunks;
+        vr[n] = load16(v_base + (int64_t)max(__shfl(at, r), 0) * (D * kBytes) + (c - r * kRowChunks) * 16);
+      }
+    };
+    int tile = block0 * kWaves + wave;
+    int at = tile < tile1 ? cache_row(tile) : -1, next_at = tile + kWaves < tile1 ? cache_row(tile + kWaves) : -1;
+    if (tile < tile1) load_tile(at);
+    __bf16* const v_tile = tiles[wave];
+    for (; tile < tile1; tile += kWaves) {
+      const bool there = at >= 0;
+      const bool whole = (tile + 1) * kTile <= first_seen && __all(there);
+      // V to LDS, rows that nobody sees as zeros
+      unsigned odd = 0;  // whether this lane has numbers that are not finite
+#pragma unroll
+      for (int n = 0; n < kVChunks; ++n) {
+        const int c = lane + 64 * n, r = c / kRowChunks;
+        u32x4 x = vr[n];
+        if (!whole && __shfl((int)there, r) == 0) x = u32x4{};
+        if constexpr (E4M3) {
+          const bf16x8 lo = widen8(x[0], x[1]), hi = widen8(x[2], x[3]);
+          if (!whole && (some_not_finite(lo) || some_not_finite(hi))) odd |= 1u << r;
+          __bf16* const p = v_tile + r * kPitch + (c - r * kRowChunks) * 16;
+          *reinterpret_cast<bf16x8*>(p) = lo;
+          *reinterpret_cast<bf16x8*>(p + 8) = hi;
+        } else {
+          const bf16x8 y = __builtin_bit_cast(bf16x8, x);
+          if (!whole && some_not_finite(y)) odd |= 1u << r;
+          *reinterpret_cast<bf16x8*>(v_tile + r * kPitch + (c - r * kRowChunks) * 8) = y;
+        }
+      }
+      // scores
+      f32x16 score = {};
+#pragma unroll
+      for (int n = 0; n < 2 * kDims; ++n) {
+        bf16x8 x;
+        if constexpr (E4M3) x = n & 1 ? widen8(kr[n >> 1][2], kr[n >> 1][3]) : widen8(kr[n >> 1][0], kr[n >> 1][1]);
+        else x = __builtin_bit_cast(bf16x8, kr[n]);
+        score = mfma32(x, q[n], score);
+      }
+      // the next tile, and the page of the one after it
+      const unsigned keys_there = whole ? 0xffffffffu : (unsigned)__ballot(there);
+      at = next_at;
+      if (tile + kWaves < tile1) {
+        load_tile(at);
+        next_at = tile + 2 * kWaves < tile1 ? cache_row(tile + 2 * kWaves) : -1;
+      }
+      // bit e: key of score[e] is one that the row sees
+      unsigned visible = 0xffffu;
+      if (!whole) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int key = 8 * (e >> 2) + 4 * half + (e & 3);
+          if (tile * kTile + key >= seen || !(keys_there >> key & 1)) {
+            visible &= ~(1u << e);
+            score[e] = -INFINITY;
+          }
+        }
+      }
+      // softmax
+      float top = score[0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) top = fmaxf(top, score[e]);
+      top = fmaxf(m, max_halves(top) * scale);
+      if (__any(top > m)) {
+        const float f = __builtin_amdgcn_exp2f(m - top);
+        l *= f;
+#pragma unroll
+        for (int t = 0; t < kDims; ++t)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) acc[t][e] *= f;
+        m = top;
+      }
+      float p[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        p[e] = __builtin_amdgcn_exp2f(score[e] * scale - m);
+        l += p[e];
+      }
+      if (!whole && __any(odd != 0)) {
+        // Values that are not finite, in keys that some rows do not see: zero times them is not zero.  Such values are added without the product, to the rows that see them, and leave it.
+        if (lane == 0) bad_rows[wave] = 0;
+        __builtin_amdgcn_wave_barrier();
+        if (odd != 0) atomicOr(&bad_rows[wave], odd);
+        __builtin_amdgcn_wave_barrier();
+        for (unsigned bad = *(volatile unsigned*)&bad_rows[wave]; bad != 0; bad &= bad - 1) {
+          const int key = __ffs((int)bad) - 1;
+          float weight = 0.f;
+          bool sees = false;
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (8 * (e >> 2) + 4 * half + (e & 3) == key) {
+              weight = p[e];
+              sees = visible >> e & 1;
+            }
+          const int from = col + 32 * (key >> 2 & 1);  // the half that has the key
+          weight = __shfl(weight, from);
+          sees = __shfl((int)sees, from) != 0;
+#pragma unroll
+          for (int t = 0; t < kDims; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const float x = (float)v_tile[key * kPitch + 32 * t + 8 * (e >> 2) + 4 * half + (e & 3)];
+              if (sees && !(fabsf(x) < INFINITY)) acc[t][e] += weight * x;
+            }
+          __builtin_amdgcn_wave_barrier();
+          for (int i = lane; i < D; i += 64)
+            if (!(fabsf((float)v_tile[key * kPitch + i]) < INFINITY)) v_tile[key * kPitch + i] = (__bf16)0.f;
+          __builtin_amdgcn_wave_barrier();
+        }
+      }
+      // weights as two terms, the values' sums
+#pragma unroll
+      for (int st = 0; st < 2; ++st) {
+        bf16x8 hi, lo;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          hi[e] = (__bf16)p[8 * st + e];
+          lo[e] = (__bf16)(p[8 * st + e] - (float)hi[e]);
+        }
+        // lanes 4 e + c of a group of 16 address dimensions 4 c .. 4 c + 3 of its key e
+        const __bf16* const from = v_tile + (16 * st + 4 * half + (lane >> 2 & 3)) * kPitch + (lane >> 4 & 1) * 16 + (lane & 3) * 4;
+#pragma unroll
+        for (int t = 0; t < kDims; ++t) {
+          const s16x4 x = lds_read_tr(from + 32 * t), y = lds_read_tr(from + 32 * t + 8 * kPitch);
+          const bf16x8 v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+          acc[t] = mfma32(v, hi, acc[t]);
+          acc[t] = mfma32(v, lo, acc[t]);
+        }
+      }
+    }
+
+    // ---- the waves' results together ----
+    l = sum_halves(l);
+    if (half == 0) {
+      maxima[wave][col] = m;
+      sums[wave][col] = l;
+    }
+    __syncthreads();  // (and no wave reads its tile any more)
+    float top = kFloor, sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, maxima[w][col]);
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) sum += sums[w][col] * __builtin_amdgcn_exp2f(maxima[w][col] - top);
+    const float f = __builtin_amdgcn_exp2f(m - top);
+#pragma unroll
+    for (int t = 0; t < kDims; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[t][e] *= f;
+    f32x4* const given = reinterpret_cast<f32x4*>(&tiles[0][0]);
+    auto give = [&](int to) {
+#pragma unroll
+      for (int t = 0; t < kDims; ++t)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) given[(to * kDims * 4 + t * 4 + g) * 64 + lane] = f32x4{acc[t][4 * g], acc[t][4 * g + 1], acc[t][4 * g + 2], acc[t][4 * g + 3]};
+    };
+    auto take = [&](int from) {
+#pragma unroll
+      for (int t = 0; t < kDims; ++t)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const f32x4 x = given[(from * kDims * 4 + t * 4 + g) * 64 + lane];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[t][4 * g + e] += x[e];
+        }
+    };
+    if (wave >= 2) give(wave - 2);
+    __syncthreads();
+    if (wave < 2) take(wave);
+    __syncthreads();
+    if (wave == 1) give(0);
+    __syncthreads();
+    if (wave == 0) {
+      take(0);
+      if (block0 == 0 && block1 == key_blocks) {
+        if (live) {
+          const float inv = sum > 0.f || sum != sum ? v_scale / sum : 0.f;
+          __bf16* const to = a.o + (int64_t)q_row * a.o_stride + (int64_t)q_head * D + 4 * half;
+#pragma unroll
+          for (int t = 0; t < kDims; ++t)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+              struct __attribute__((packed, aligned(2))) Loose4 {
+                bf16x4 x;
+              };
+              reinterpret_cast<Loose4*>(to + 32 * t + 8 * g)->x = pack4(acc[t][4 * g] * inv, acc[t][4 * g + 1] * inv, acc[t][4 * g + 2] * inv, acc[t][4 * g + 3] * inv);
+            }
+          if (a.lse && half == 0) a.lse[(int64_t)q_head * a.total_q + q_row] = sum > 0.f || sum != sum ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+        }
+      } else {
+        float* const part = a.parts + ((int64_t)(share * 2 + (block0 == 0)) * a.heads + head) * part_floats<D>();
+        if (live) {
+#pragma unroll
+          for (int t = 0; t < kDims; ++t)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+              *reinterpret_cast<f32x4*>(part + col * D + 32 * t + 8 * g + 4 * half) = f32x4{acc[t][4 * g], acc[t][4 * g + 1], acc[t][4 * g + 2], acc[t][4 * g + 3]};
+          if (half == 0) {
+            part[kRows * D + col] = top;
+            part[kRows * D + kRows + col] = sum;
+          }
+        }
+        if (lane == 0 && head == 0 && block0 == 0) {
+          a.cuts[share * kCut + kCutSeq] = seq;
+          a.cuts[share * kCut + kCutBlock] = row_block;
+          a.cuts[share * kCut + kCutShares] = (int)((unit + key_blocks - 1) / size) - share + 1;
+        }
+      }
+    }
+    __syncthreads();
+    unit += block1 - block0;
+    in_seq += block1 - block0;
+  }
+}
+
+// Blocks of rows that were cut: the parts of one row, in the order of the keys, joined by a workgroup (each wave takes every fourth part).
+template <int D>
+__global__ __launch_bounds__(kThreads) void join_kernel(const AttnArgs a, const int row_groups) {
+  constexpr int kPer = (D + 63) / 64;
+  __shared__ float tops[kWaves], sums[kWaves], values[kWaves][D];
+  const int head = blockIdx.x % a.heads, at = blockIdx.x / a.heads, share = at / row_groups;
+  const int n = a.cuts[share * kCut + kCutShares];
+  if (n <= 1) return;
+  const int seq = a.cuts[share * kCut + kCutSeq], block = a.cuts[share * kCut + kCutBlock];
+  const Sequence s = sequence_at(a, seq);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (int col = at % row_groups; col < kRows && block * kRows + col < s.rows; col += row_groups) {
+    const int row = block * kRows + col, token = a.by_group(row), q_row = s.first_row + token, q_head = head * a.group + row - token * a.group;
+    auto part_of = [&](int i) { return a.parts + ((int64_t)((share + i) * 2 + (i == 0)) * a.heads + head) * part_floats<D>(); };
+    float m = kFloor;
+    for (int i = wave; i < n; i += kWaves) m = fmaxf(m, part_of(i)[kRows * D + col]);
+    float l = 0.f, acc[kPer] = {};
+#pragma unroll 4
+    for (int i = wave; i < n; i += kWaves) {
+      const float* const p = part_of(i);
+      const float f = __builtin_amdgcn_exp2f(p[kRows * D + col] - m);
+      l += p[kRows * D + kRows + col] * f;
+#pragma unroll
+      for (int e = 0; e < kPer; ++e)
+        if (e * 64 + lane < D) acc[e] += p[col * D + e * 64 + lane] * f;
+    }
+    if (lane == 0) {
+      tops[wave] = m;
+      sums[wave] = l;
+    }
+#pragma unroll
+    for (int e = 0; e < kPer; ++e)
+      if (e * 64 + lane < D) values[wave][e * 64 + lane] = acc[e];
+    __syncthreads();
+    float top = kFloor, sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, tops[w]);
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) sum += sums[w] * __builtin_amdgcn_exp2f(tops[w] - top);
+    const bool some = sum > 0.f || sum != sum;
+    const float inv = some ? (a.v_scale ? a.v_scale[head] : 1.f) / sum : 0.f;
+    for (int i = threadIdx.x; i < D; i += kThreads) {
+      float x = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) x += values[w][i] * __builtin_amdgcn_exp2f(tops[w] - top);
+      a.o[(int64_t)q_row * a.o_stride + (int64_t)q_head * D + i] = (__bf16)(x * inv);
+    }
+    if (a.lse && threadIdx.x == 0) a.lse[(int64_t)q_head * a.total_q + q_row] = some ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+    __syncthreads();
+  }
+}
+
+// ---- host ----
+int check_desc(const paged_attn_desc* d) {
+  if (!d || d->num_q_heads < 1 || d->num_kv_heads < 1 || d->num_seqs < 1 || d->total_q < 0 || d->page_size < 1 || d->num_pages < 1 || d->max_pages < 1 ||
+      (d->cache_type != PAGED_CACHE_BF16 && d->cache_type != PAGED_CACHE_E4M3) || !finite_number(d->softmax_scale) || d->softmax_scale <= 0.f)
+    return CHUNK_ATTN_INVALID_ARG;
+  if (!paged_head_dim(d->head_dim) || d->num_q_heads % d->num_kv_heads != 0 || d->num_q_heads > PAGED_MAX_HEADS || d->num_seqs > PAGED_CACHE_MAX_REQUESTS ||
+      d->page_size > PAGED_CACHE_MAX_PAGE_SIZE)
+    return CHUNK_ATTN_UNSUPPORTED;
+  // (products of three are formed of factors below 2^31 and 2^30)
+  if ((int64_t)d->total_q * d->num_q_heads > INT32_MAX || (int64_t)d->max_pages * d->page_size > 1 << 30 ||
+      (int64_t)d->num_pages * d->page_size > INT32_MAX / d->num_kv_heads)
+    return CHUNK_ATTN_INVALID_ARG;
+  return CHUNK_ATTN_OK;
+}
+// Workgroups for each key/value head: two to a compute unit (256: one), and no more than there can be shares.
+int count_shares(const paged_attn_desc* d) {
+  const int64_t most_keys = (int64_t)d->max_pages * d->page_size, group = d->num_q_heads / d->num_kv_heads;
+  const int64_t blocks = std::min<int64_t>((int64_t)d->num_seqs + d->total_q * group / kRows, std::max<int64_t>(d->total_q * group, 1)) * ((most_keys + kBlockKeys - 1) / kBlockKeys);
+  const int64_t fill = ((d->head_dim == 256 ? 1 : 2) * kCus + d->num_kv_heads - 1) / d->num_kv_heads;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(fill, (blocks + kLeastShare - 1) / kLeastShare));
+}
+size_t part_bytes(const paged_attn_desc* d) { return (size_t)count_shares(d) * 2 * d->num_kv_heads * kRows * (d->head_dim + 2) * sizeof(float); }
+size_t need_bytes(const paged_attn_desc* d) { return part_bytes(d) + (size_t)count_shares(d) * kCut * sizeof(int32_t); }
+bool aligned(const void* p, uintptr_t to) { return p && ((uintptr_t)p & (to - 1)) == 0; }
+
+template <class F>
+hipError_t by_dim(int d, F&& f) {
+  switch (d) {
+    case 64: return f(std::integral_constant<int, 64>{});
+    case 96: return f(std::integral_constant<int, 96>{});
+    case 128: return f(std::integral_constant<int, 128>{});
+    default: return f(std::integral_constant<int, 256>{});
+  }
+}
+
+}  // namespace
+}  // namespace chunk_attn
+
+extern "C" int paged_attn_validate(const paged_attn_desc* d) { return chunk_attn::check_desc(d); }
+
+extern "C" int paged_attn_workspace_bytes(const paged_attn_desc* d, size_t* bytes) {
+  const int rc = chunk_attn::check_desc(d);
+  if (rc != CHUNK_ATTN_OK) return rc;
+  if (!bytes) return CHUNK_ATTN_INVALID_ARG;
+  *bytes = chunk_attn::need_bytes(d);
+  return CHUNK_ATTN_OK;
+}
+
+extern "C" int paged_attn_fwd(const paged_attn_desc* d, const void* q, int64_t q_stride, const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
+                              const int32_t* table, const int32_t* kv_len, const int32_t* q_start, void* o, int64_t o_stride, float* lse, void* workspace, size_t workspace_bytes,
+                              void* hip_stream) {
+  using namespace chunk_attn;
+  const int rc = check_desc(d);
+  if (rc != CHUNK_ATTN_OK) return rc;
+  if (d->total_q == 0) return CHUNK_ATTN_OK;
+  const int64_t row = (int64_t)d->num_q_heads * d->head_dim;
+  const bool e4m3 = d->cache_type == PAGED_CACHE_E4M3;
+  if (!aligned(q, 2) || !aligned(o, 2) || q_stride < row || o_stride < row || !aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(table, 4) || !aligned(kv_len, 4) ||
+      !aligned(q_start, 4) || ((uintptr_t)lse & 3) != 0 || (e4m3 && (!aligned(k_scale, 4) || !aligned(v_scale, 4))) || !aligned(workspace, 256))
+    return CHUNK_ATTN_INVALID_ARG;
+  if (workspace_bytes < need_bytes(d)) return CHUNK_ATTN_WORKSPACE_TOO_SMALL;
+  const int heads = d->num_kv_heads, group = d->num_q_heads / heads, shares = count_shares(d);
+  const AttnArgs a{(const __bf16*)q, q_stride, k_cache, v_cache, e4m3 ? k_scale : nullptr, e4m3 ? v_scale : nullptr, table, kv_len, q_start, (__bf16*)o, o_stride, lse,
+                   (float*)workspace, (int32_t*)((char*)workspace + part_bytes(d)), d->num_seqs, d->total_q, heads, group, d->page_size, d->num_pages, d->max_pages, shares,
+                   d->softmax_scale * kLog2e, Divide(d->page_size), Divide(group)};
+  const hipStream_t stream = (hipStream_t)hip_stream;
+  const hipError_t e = by_dim(d->head_dim, [&](auto dim) {
+    constexpr int D = decltype(dim)::value;
+    const dim3 grid((unsigned)(shares * heads));
+    if (e4m3) hipLaunchKernelGGL((attn_kernel<D, true>), grid, dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL((attn_kernel<D, false>), grid, dim3(kThreads), 0, stream, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || shares == 1) return e;
+    // rows of a block that is cut: one to a workgroup, as long as that makes no more than 4096 of them
+    const int most = (int)std::min<int64_t>(kRows, (int64_t)d->total_q * group);
+    const int row_groups = std::max(1, std::min(most, 4096 / (shares * heads)));
+    hipLaunchKernelGGL((join_kernel<D>), dim3((unsigned)(shares * heads * row_groups)), dim3(kThreads), 0, stream, a, row_groups);
+    return hipGetLastError();
+  });
+  return e == hipSuccess ? CHUNK_ATTN_OK : report_hip(e, "attention over a paged cache");
+}

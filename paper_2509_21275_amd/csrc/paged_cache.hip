@@ -1,0 +1,384 @@
+// Pages of a cache for the tokens of many requests, and keys and values on their way into them (include/paged_cache.h).
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "../../include/paged_cache.h"
+#include "kernels.hpp"
+#include "operators.hpp"
+#include "paged.hpp"
+
+namespace chunk_attn {
+namespace {
+
+// ---- tables ----
+// Requests in order, pages in order: two running sums, of rows and of pages.  One workgroup of 1024 threads takes them, each thread over neighbouring requests; what follows
+// from the sums (slots of rows, entries of the table, entries of the stack) goes row by row and page by page, each of which finds its request by halving in the sums.  Few requests with few
+// rows: the same workgroup does that too, with the sums in LDS (one launch).  Else the sums go to the workspace and a second launch fills the chip.
+constexpr int kScanThreads = 1024;
+constexpr int kInOne = 4096;  // rows that the one workgroup goes through itself
+
+struct TableArgs {
+  int32_t n, max_pages, page_size, num_pages;
+  const int32_t* change;  // new tokens, or tokens to drop
+  const int32_t *kv_len, *held;
+  int32_t* table;
+  int32_t* free_pages;
+  const int32_t* num_free;
+  int32_t *kv_len_out, *held_out, *num_free_out, *q_start, *granted;
+  int64_t* slots;
+  int32_t max_rows;
+  // workspace: what the second launch goes by
+  int32_t* sums;  // [kSums][n] and the totals behind them
+};
+// Of each request: pages before it, tokens before the call (extend: -1 if it is not served), pages that it had (truncate: that it keeps).
+enum { kPagesBefore, kOldLen, kHeld, kSums };
+// Behind them: pages that change hands, pages on the stack before the call.
+enum { kMoved, kOnStack, kTotals };
+
+__device__ __forceinline__ int64_t wave_scan(int64_t x) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int64_t y = __shfl_up(x, o);
+    if (lane >= o) x += y;
+  }
+  return x;
+}
+// Sum over the threads before the own one; `room`: one number for each wave.
+__device__ __forceinline__ int64_t sum_before(int64_t x, int64_t* room) {
+  const int64_t up_to = wave_scan(x);
+  if ((threadIdx.x & 63) == 63) room[threadIdx.x >> 6] = up_to;
+  __syncthreads();
+  int64_t before = up_to - x;
+  for (int w = 0; w < (int)(threadIdx.x >> 6); ++w) before += room[w];
+  __syncthreads();
+  return before;
+}
+__device__ __forceinline__ int at_most(int64_t x, int64_t most) { return (int)(x < most ? x : most); }
+
+// A request, its numbers brought into their ranges.
+struct Request {
+  int old_len, held, change, len, need;  // need: pages that it takes (extend, if it is served) or gives (truncate)
+  bool fits;
+};
+template <bool EXTEND>
+__device__ __forceinline__ Request request_at(const TableArgs& a, int i) {
+  const int64_t most = (int64_t)a.max_pages * a.page_size;  // < 2^31
+  Request r;
+  r.old_len = at_most(max(a.kv_len[i], 0), most);
+  r.held = min(max(a.held[i], 0), a.max_pages);
+  r.change = max(a.change[i], 0);
+  if (EXTEND) {
+    const int64_t len = (int64_t)r.old_len + r.change;
+    r.fits = len <= most;
+    r.len = r.fits ? (int)len : r.old_len;
+    r.need = r.fits ? max(0, (int)((len + a.page_size - 1) / a.page_size) - r.held) : 0;
+  } else {
+    r.fits = true;
+    r.len = max(r.old_len - r.change, 0);
+    r.need = r.held - min(r.held, (int)(((int64_t)r.len + a.page_size - 1) / a.page_size));
+  }
+  return r;
+}
+
+// Last i < n with sums[i] <= x, for sums[0] = 0 <= x.
+__device__ __forceinline__ int find(const int32_t* sums, int n, int x) {
+  int lo = 0;
+  for (int hi = n; hi - lo > 1;) {
+    const int mid = (lo + hi) >> 1;
+    if (sums[mid] <= x) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+// Slots of rows, from the sums.
+__device__ __forceinline__ int64_t slot_of_row(const TableArgs& a, const int32_t* q_start, const int32_t* pages_before, const int32_t* old_lens, const int32_t* helds, int on_stack, int row) {
+  if (row >= q_start[a.n]) return -1;
+  const int i = find(q_start, a.n, row);
+  if (old_lens[i] < 0) return -1;
+  const int at = old_lens[i] + row - q_start[i], b = at / a.page_size;
+  const int page = b < helds[i] ? a.table[(int64_t)i * a.max_pages + b] : a.free_pages[on_stack - 1 - (pages_before[i] + b - helds[i])];
+  return page >= 0 && page < a.num_pages ? (int64_t)page * a.page_size + at % a.page_size : -1;
+}
+// One page that changes hands.
+template <bool EXTEND>
+__device__ __forceinline__ void move_page(const TableArgs& a, const int32_t* pages_before, const int32_t* helds, int on_stack, int p) {
+  const int i = find(pages_before, a.n, p);
+  int32_t* const entry = a.table + (int64_t)i * a.max_pages + helds[i] + p - pages_before[i];
+  if (EXTEND) *entry = a.free_pages[on_stack - 1 - p];
+  else if (on_stack + p < a.num_pages) a.free_pages[on_stack + p] = *entry;
+}
+
+// IN_ONE: at most kScanThreads requests and kInOne rows; everything is done here.
+template <bool EXTEND, bool IN_ONE>
+__global__ __launch_bounds__(kScanThreads) void tables_kernel(const TableArgs a) {
+  __shared__ int64_t room[kScanThreads / 64];
+  __shared__ int32_t in_lds[IN_ONE ? kSums + 1 : 1][IN_ONE ? kScanThreads + 1 : 1];
+  __shared__ int moved;
+  const int each = IN_ONE ? 1 : (a.n + kScanThreads - 1) / kScanThreads;
+  const int first = min((int)threadIdx.x * each, a.n), last = min(first + each, a.n);
+  const int on_stack = min(max(*a.num_free, 0), a.num_pages);
+  int32_t* const pages_before = IN_ONE ? in_lds[kPagesBefore] : a.sums + (int64_t)kPagesBefore * a.n;
+  int32_t* const old_lens = IN_ONE ? in_lds[kOldLen] : a.sums + (int64_t)kOldLen * a.n;
+  int32_t* const helds = IN_ONE ? in_lds[kHeld] : a.sums + (int64_t)kHeld * a.n;
+  int32_t* const starts = IN_ONE ? in_lds[kSums] : a.q_start;
+  if (threadIdx.x == 0) moved = 0;
+  // rows first: who does not fit in them has no claim on pages
+  int64_t rows = 0, pages = 0;
+  if (EXTEND) {
+    for (int i = first; i < last; ++i) rows += max(a.change[i], 0);
+    rows = sum_before(rows, room);
+  }
+  int64_t row = rows;
+  for (int i = first; i < last; ++i) {
+    const Request r = request_at<EXTEND>(a, i);
+    row += r.change;
+    if (!EXTEND || r.change == 0 || row <= a.max_rows) pages += r.need;
+  }
+  pages = sum_before(pages, room);
+  row = rows;
+  int mine = 0;
+  for (int i = first; i < last; ++i) {
+    const Request r = request_at<EXTEND>(a, i);
+    const int64_t end = row + r.change;
+    const bool in_rows = !EXTEND || r.change == 0 || end <= a.max_rows;
+    const int need = in_rows ? r.need : 0;
+    const bool served = r.fits && in_rows && (!EXTEND || need == 0 || pages + need <= on_stack);
+    pages_before[i] = at_most(pages, INT32_MAX);
+    pages += need;
+    if (served && need > 0) mine = at_most(pages, INT32_MAX);  // (the sums grow: those that are served are the first of those that need pages)
+    old_lens[i] = served ? r.old_len : -1;
+    helds[i] = EXTEND ? r.held : r.held - need;
+    if (EXTEND) {
+      const int start = at_most(row, a.max_rows);
+      starts[i] = start;
+      if (IN_ONE) a.q_start[i] = start;
+      if (i == a.n - 1) {
+        starts[a.n] = at_most(end, a.max_rows);
+        if (IN_ONE) a.q_start[a.n] = at_most(end, a.max_rows);
+      }
+      if (a.granted) a.granted[i] = served;
+    }
+    row = end;
+    a.kv_len_out[i] = served ? r.len : r.old_len;
+    a.held_out[i] = EXTEND ? r.held + (served ? need : 0) : r.held - need;
+  }
+  if (mine > 0) atomicMax(&moved, mine);
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    *a.num_free_out = EXTEND ? on_stack - moved : at_most((int64_t)on_stack + moved, a.num_pages);
+    if (!IN_ONE) {
+      a.sums[(int64_t)kSums * a.n + kMoved] = moved;
+      a.sums[(int64_t)kSums * a.n + kOnStack] = on_stack;
+    }
+  }
+  if constexpr (IN_ONE) {
+    if (EXTEND)
+      for (int r = threadIdx.x; r < a.max_rows; r += kScanThreads) a.slots[r] = slot_of_row(a, starts, pages_before, old_lens, helds, on_stack, r);
+    for (int p = threadIdx.x; p < moved; p += kScanThreads) move_page<EXTEND>(a, pages_before, helds, on_stack, p);
+  }
+}
+
+template <bool EXTEND>
+__global__ __launch_bounds__(256) void fill_kernel(const TableArgs a) {
+  const int32_t *const pages_before = a.sums + (int64_t)kPagesBefore * a.n, *const old_lens = a.sums + (int64_t)kOldLen * a.n, *const helds = a.sums + (int64_t)kHeld * a.n;
+  const int moved = a.sums[(int64_t)kSums * a.n + kMoved], on_stack = a.sums[(int64_t)kSums * a.n + kOnStack];
+  const int64_t step = (int64_t)gridDim.x * 256, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (EXTEND)
+    for (int64_t r = at; r < a.max_rows; r += step) a.slots[r] = slot_of_row(a, a.q_start, pages_before, old_lens, helds, on_stack, (int)r);
+  for (int64_t p = at; p < moved; p += step) move_page<EXTEND>(a, pages_before, helds, on_stack, (int)p);
+}
+
+int check_desc(const paged_cache_desc* d) {
+  if (!d || d->num_requests < 1 || d->max_pages < 1 || d->num_pages < 1 || d->page_size < 1) return CHUNK_ATTN_INVALID_ARG;
+  if (d->num_requests > PAGED_CACHE_MAX_REQUESTS || d->page_size > PAGED_CACHE_MAX_PAGE_SIZE) return CHUNK_ATTN_UNSUPPORTED;
+  return (int64_t)d->max_pages * d->page_size > INT32_MAX ? CHUNK_ATTN_INVALID_ARG : CHUNK_ATTN_OK;
+}
+size_t table_bytes(const paged_cache_desc* d) { return ((size_t)d->num_requests * kSums + kTotals) * sizeof(int32_t); }
+bool aligned(const void* p, uintptr_t to) { return p && ((uintptr_t)p & (to - 1)) == 0; }
+
+template <bool EXTEND>
+int run_tables(const paged_cache_desc* d, TableArgs a, void* workspace, size_t workspace_bytes, hipStream_t stream, const char* what) {
+  for (const void* p : {(const void*)a.change, (const void*)a.kv_len, (const void*)a.held, (const void*)a.table, (const void*)a.free_pages, (const void*)a.num_free,
+                        (const void*)a.kv_len_out, (const void*)a.held_out, (const void*)a.num_free_out})
+    if (!aligned(p, 4)) return CHUNK_ATTN_INVALID_ARG;
+  if (!aligned(workspace, 256)) return CHUNK_ATTN_INVALID_ARG;
+  if (workspace_bytes < table_bytes(d)) return CHUNK_ATTN_WORKSPACE_TOO_SMALL;
+  a.n = d->num_requests;
+  a.max_pages = d->max_pages;
+  a.page_size = d->page_size;
+  a.num_pages = d->num_pages;
+  a.sums = (int32_t*)workspace;
+  if (a.n <= kScanThreads && a.max_rows <= kInOne) {
+    hipLaunchKernelGGL((tables_kernel<EXTEND, true>), dim3(1), dim3(kScanThreads), 0, stream, a);
+  } else {
+    hipLaunchKernelGGL((tables_kernel<EXTEND, false>), dim3(1), dim3(kScanThreads), 0, stream, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return report_hip(e, what);
+    // (a page or more to a thread's rows: pages that change hands are hardly ever more than rows, and few of the pool's)
+    const int64_t threads = EXTEND ? std::max<int64_t>(a.max_rows, a.n) : std::min<int64_t>((int64_t)a.n * 4, a.num_pages);
+    hipLaunchKernelGGL((fill_kernel<EXTEND>), dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>((threads + 255) / 256, 4 * kCus))), dim3(256), 0, stream, a);
+  }
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? CHUNK_ATTN_OK : report_hip(e, what);
+}
+
+// ---- keys and values into the pages ----
+// Bound by memory: 16 elements to a thread and tensor, kAtOnce such pieces loaded before any is stored.  A workgroup takes neighbouring rows.
+constexpr int kWriteThreads = 256, kAtOnce = 2;
+
+struct WriteArgs {
+  const __bf16 *k, *v;
+  int64_t k_stride, v_stride;
+  const int64_t* slots;
+  const float *k_scale, *v_scale;
+  void *k_cache, *v_cache;
+  int64_t num_slots, pieces;  // pieces of 16 elements in all rows
+  int32_t heads, head_pieces, row_pieces, page_size;
+  Divide by_row, by_head, by_page;
+};
+
+struct __attribute__((packed, aligned(2))) Loose16 {
+  u32x4 w[2];
+};
+
+__device__ __forceinline__ u32x4 to_e4m3(const Loose16& x, float scale) {
+  u32x4 r;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    unsigned word = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const unsigned two = x.w[w >> 1][(w & 1) * 2 + (e >> 1)];
+      const float f = __uint_as_float(e & 1 ? two & 0xffff0000u : two << 16) / scale;  // (true division: rounded once)
+      // |f| up to 448 by clamping; a NaN passes neither comparison
+      const float c = f > 448.f ? 448.f : f < -448.f ? -448.f : f;
+      const unsigned byte = f != f ? 0x7fu : (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(c, c, 0, false) & 0xffu;
+      word |= byte << (8 * e);
+    }
+    r[w] = word;
+  }
+  return r;
+}
+
+template <bool E4M3>
+__global__ __launch_bounds__(kWriteThreads) void write_kernel(const WriteArgs a) {
+  Loose16 k[kAtOnce], v[kAtOnce];
+  int64_t to[kAtOnce];
+  int head[kAtOnce];
+  const int64_t first = (int64_t)blockIdx.x * (kWriteThreads * kAtOnce) + threadIdx.x;
+#pragma unroll
+  for (int n = 0; n < kAtOnce; ++n) {
+    const int64_t piece = first + n * kWriteThreads;
+    to[n] = -1;
+    head[n] = 0;
+    if (piece >= a.pieces) continue;
+    // (pieces < 2^36; rows < 2^31)
+    const int64_t row = a.by_row.wide(piece);
+    const int in_row = (int)(piece - row * a.row_pieces);
+    const int64_t slot = a.slots[row];
+    if (slot < 0 || slot >= a.num_slots) continue;
+    head[n] = a.by_head(in_row);
+    const int64_t page = a.by_page.wide(slot);
+    to[n] = ((page * a.heads + head[n]) * a.page_size + (slot - page * a.page_size)) * a.head_pieces + (in_row - head[n] * a.head_pieces);
+    k[n] = *reinterpret_cast<const Loose16*>(a.k + row * a.k_stride + in_row * 16);
+    v[n] = *reinterpret_cast<const Loose16*>(a.v + row * a.v_stride + in_row * 16);
+  }
+#pragma unroll
+  for (int n = 0; n < kAtOnce; ++n) {
+    if (to[n] < 0) continue;
+    if constexpr (E4M3) {
+      reinterpret_cast<u32x4*>(a.k_cache)[to[n]] = to_e4m3(k[n], a.k_scale[head[n]]);
+      reinterpret_cast<u32x4*>(a.v_cache)[to[n]] = to_e4m3(v[n], a.v_scale[head[n]]);
+    } else {
+      u32x4 *const pk = reinterpret_cast<u32x4*>(a.k_cache) + 2 * to[n], *const pv = reinterpret_cast<u32x4*>(a.v_cache) + 2 * to[n];
+      pk[0] = k[n].w[0];
+      pk[1] = k[n].w[1];
+      pv[0] = v[n].w[0];
+      pv[1] = v[n].w[1];
+    }
+  }
+}
+
+}  // namespace
+}  // namespace chunk_attn
+
+extern "C" int paged_cache_validate(const paged_cache_desc* d) { return chunk_attn::check_desc(d); }
+
+extern "C" int paged_cache_workspace_bytes(const paged_cache_desc* d, size_t* bytes) {
+  const int rc = chunk_attn::check_desc(d);
+  if (rc != CHUNK_ATTN_OK) return rc;
+  if (!bytes) return CHUNK_ATTN_INVALID_ARG;
+  *bytes = chunk_attn::table_bytes(d);
+  return CHUNK_ATTN_OK;
+}
+
+extern "C" int paged_cache_extend(const paged_cache_desc* d, const int32_t* new_tokens, const int32_t* kv_len, const int32_t* held, int32_t* table, const int32_t* free_pages,
+                                  const int32_t* num_free, int32_t* kv_len_out, int32_t* held_out, int32_t* num_free_out, int32_t* q_start, int64_t* slots, int32_t max_rows,
+                                  int32_t* granted, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  using namespace chunk_attn;
+  const int rc = check_desc(d);
+  if (rc != CHUNK_ATTN_OK) return rc;
+  if (max_rows < 0 || !aligned(q_start, 4) || (max_rows > 0 && !aligned(slots, 8)) || ((uintptr_t)granted & 3) != 0) return CHUNK_ATTN_INVALID_ARG;
+  TableArgs a{};
+  a.change = new_tokens;
+  a.kv_len = kv_len;
+  a.held = held;
+  a.table = table;
+  a.free_pages = const_cast<int32_t*>(free_pages);  // (read only where tokens come in)
+  a.num_free = num_free;
+  a.kv_len_out = kv_len_out;
+  a.held_out = held_out;
+  a.num_free_out = num_free_out;
+  a.q_start = q_start;
+  a.slots = slots;
+  a.max_rows = max_rows;
+  a.granted = granted;
+  return run_tables<true>(d, a, workspace, workspace_bytes, (hipStream_t)hip_stream, "pages for new tokens");
+}
+
+extern "C" int paged_cache_truncate(const paged_cache_desc* d, const int32_t* drop, const int32_t* kv_len, const int32_t* held, const int32_t* table, int32_t* free_pages,
+                                    const int32_t* num_free, int32_t* kv_len_out, int32_t* held_out, int32_t* num_free_out, void* workspace, size_t workspace_bytes,
+                                    void* hip_stream) {
+  using namespace chunk_attn;
+  const int rc = check_desc(d);
+  if (rc != CHUNK_ATTN_OK) return rc;
+  TableArgs a{};
+  a.change = drop;
+  a.kv_len = kv_len;
+  a.held = held;
+  a.table = const_cast<int32_t*>(table);  // (read only where tokens go)
+  a.free_pages = free_pages;
+  a.num_free = num_free;
+  a.kv_len_out = kv_len_out;
+  a.held_out = held_out;
+  a.num_free_out = num_free_out;
+  return run_tables<false>(d, a, workspace, workspace_bytes, (hipStream_t)hip_stream, "pages given back");
+}
+
+extern "C" int paged_cache_write(int32_t rows, int32_t num_kv_heads, int32_t head_dim, int32_t page_size, int32_t num_pages, int32_t cache_type, const void* k, int64_t k_stride,
+                                 const void* v, int64_t v_stride, const int64_t* slots, const float* k_scale, const float* v_scale, void* k_cache, void* v_cache,
+                                 void* hip_stream) {
+  using namespace chunk_attn;
+  if (rows < 0 || num_kv_heads < 1 || page_size < 1 || num_pages < 1 || (cache_type != PAGED_CACHE_BF16 && cache_type != PAGED_CACHE_E4M3)) return CHUNK_ATTN_INVALID_ARG;
+  if (!paged_head_dim(head_dim) || num_kv_heads > PAGED_MAX_HEADS || page_size > PAGED_CACHE_MAX_PAGE_SIZE) return CHUNK_ATTN_UNSUPPORTED;
+  const int64_t row_elements = (int64_t)num_kv_heads * head_dim;
+  if ((int64_t)rows * row_elements >= (int64_t)1 << 40) return CHUNK_ATTN_INVALID_ARG;
+  if (rows == 0) return CHUNK_ATTN_OK;
+  if (!aligned(k, 2) || !aligned(v, 2) || k_stride < row_elements || v_stride < row_elements || !aligned(slots, 8) || !aligned(k_cache, 16) || !aligned(v_cache, 16) ||
+      (cache_type == PAGED_CACHE_E4M3 && (!aligned(k_scale, 4) || !aligned(v_scale, 4))))
+    return CHUNK_ATTN_INVALID_ARG;
+  const int row_pieces = (int)(row_elements / 16), head_pieces = head_dim / 16;
+  const int64_t pieces = (int64_t)rows * row_pieces;
+  const WriteArgs a{(const __bf16*)k, (const __bf16*)v, k_stride, v_stride, slots, k_scale, v_scale, k_cache, v_cache, (int64_t)num_pages * page_size, pieces, num_kv_heads,
+                    head_pieces, row_pieces, page_size, Divide(row_pieces), Divide(head_pieces), Divide(page_size)};
+  const int64_t groups = (pieces + kWriteThreads * kAtOnce - 1) / (kWriteThreads * kAtOnce);
+  if (groups * kWriteThreads >= (int64_t)1 << 32) return CHUNK_ATTN_INVALID_ARG;
+  if (cache_type == PAGED_CACHE_E4M3) hipLaunchKernelGGL(write_kernel<true>, dim3((unsigned)groups), dim3(kWriteThreads), 0, (hipStream_t)hip_stream, a);
+  else hipLaunchKernelGGL(write_kernel<false>, dim3((unsigned)groups), dim3(kWriteThreads), 0, (hipStream_t)hip_stream, a);
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? CHUNK_ATTN_OK : report_hip(e, "keys and values into pages");
+}

@@ -1,0 +1,244 @@
+"""Attention over a paged cache against float64.  Tolerance: a result is rounded once (half a step of bf16, 2^-8 of it).  Before that, a score is a sum of d products in float32, off by at most
+(d + 8) 2^-24 of the sum of their sizes; the argument of an exponential, below 2^7 in size, is off by 2^-17 more, the weight's two bf16 terms by 2^-17 of it, and sums over L keys by L 2^-24 at
+most.  With e the sum of these, weights are off by the factor 1 + e, the values' sum by e times the weighted sum of their sizes, and the sum of weights that divides it by the same: 2 e."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged_oracle as orc
+
+pytestmark = pytest.mark.gpu
+BF16, E4M3, I32 = torch.bfloat16, torch.float8_e4m3fn, torch.int32
+
+
+class Case:
+    """Sequences of `lens` tokens with `new` new ones each, their pages scattered over a pool; what no sequence holds is `waste`."""
+
+    def __init__(self, lens, new, heads, kv_heads, dim, page, kind="bf16", seed=0, waste=float("nan"), spare_rows=3, pad=0, spare_pages=3):
+        g = torch.Generator().manual_seed(seed)
+        n = len(lens)
+        held = [-(-L // page) for L in lens]
+        self.width, self.pages = max(1, max(held)), sum(held) + spare_pages
+        order = torch.randperm(self.pages, generator=g)
+        self.table, at = torch.full((n, self.width), -1, dtype=I32), 0
+        for i, h in enumerate(held):
+            self.table[i, :h] = order[at:at + h].to(I32)
+            at += h
+        self.kind, self.page, self.lens, self.new = kind, page, lens, new
+        self.heads, self.kv_heads, self.dim = heads, kv_heads, dim
+        self.q_start = np.concatenate([[0], np.cumsum(new)]).tolist()
+        self.total = self.q_start[-1] + spare_rows
+        self.q = torch.randn((self.total, heads * dim + pad), generator=g).to(BF16).cuda()[:, :heads * dim].unflatten(1, (heads, dim))
+        dtype, size = (BF16, 1.0) if kind == "bf16" else (E4M3, 100.0)
+        self.scales = [None, None] if kind == "bf16" else [(torch.rand(kv_heads, generator=g) * 0.5 + 0.75).cuda() / size for _ in range(2)]
+        self.caches = []
+        for _ in range(2):
+            c = torch.randn((self.pages, kv_heads, page, dim), generator=g).mul_(size).clamp_(-448, 448)
+            used = torch.zeros((self.pages, page), dtype=torch.bool)
+            for i, L in enumerate(lens):
+                t = torch.arange(L)
+                used[self.table[i, t // page].long(), t % page] = True
+            c = torch.where(used[:, None, :, None], c, torch.tensor(waste))
+            self.caches.append(c.to(dtype).cuda())
+        self.table, self.kv_len = self.table.cuda(), torch.tensor(lens, dtype=I32, device="cuda")
+
+    def desc(self):
+        from paper_2509_21275_amd import paged_attn as pa
+        return pa.make_desc(self.heads, self.kv_heads, self.dim, len(self.lens), self.total, self.page, self.pages, self.width, self.dim ** -0.5, self.kind)
+
+    def run(self, stream=None, lse=True, o=None, ws=None):
+        from paper_2509_21275_amd import paged_attn as pa
+        desc = self.desc()
+        o = torch.full((self.total, self.heads, self.dim), 7.0, dtype=BF16, device="cuda") if o is None else o
+        out = torch.full((self.heads, self.total), 7.0, device="cuda") if lse else None
+        ws = torch.full_like(pa.alloc_workspace(desc), 255) if ws is None else ws  # (NaN everywhere)
+        torch.cuda.synchronize()
+        pa.paged_attn_fwd(desc, self.q, *self.caches, self.table, self.kv_len, torch.tensor(self.q_start, dtype=I32, device="cuda"), o, out, ws, k_scale=self.scales[0],
+                          v_scale=self.scales[1], stream=stream)
+        torch.cuda.synchronize()
+        return o, out
+
+    def check(self, o, lse, table=None):
+        k, v = (c.double().cpu().numpy() if s is None else (c.float().double() * s.double()[:, None, None]).cpu().numpy() for c, s in zip(self.caches, self.scales))
+        o, q = o.double().cpu().numpy(), self.q.double().cpu().numpy()
+        lse = None if lse is None else lse.double().cpu().numpy()
+        table = self.table.cpu().numpy() if table is None else table
+        with np.errstate(invalid="ignore"):
+            for row, want, want_lse, size, score, keys in orc.attention(q, k, v, table, self.lens, self.q_start, self.dim ** -0.5):
+                if keys == 0:
+                    assert not o[row].any() and (lse is None or np.all(lse[:, row] == -np.inf))
+                    continue
+                e = (self.dim + 8) * 2.0 ** -24 * score + 2.0 ** -16 + keys * 2.0 ** -24
+                assert np.all(np.abs(o[row] - want) <= 2.0 ** -8 * np.abs(want) + 2 * e[:, None] * size), (row, float(np.abs(o[row] - want).max()))
+                # (a float32 of the lse's size is off by 2^-24 of it)
+                assert lse is None or np.all(np.abs(lse[:, row] - want_lse) <= e + 2.0 ** -22 * np.abs(want_lse)), row
+        last = self.q_start[-1]
+        assert np.all(o[last:] == 7.0) and (lse is None or np.all(lse[:, last:] == 7.0))
+
+
+LENS = [0, 1, 31, 32, 33, 127, 128, 129, 300, 2, 1000]
+CASES = [
+    # one token each, every head dimension, heads shared by none, four, all, five
+    ("one_token", LENS, [min(1, L) for L in LENS], 8, 2, 128, 16), ("one_token", LENS, [min(1, L) for L in LENS], 2, 2, 64, 64), ("one_token", LENS, [1] * len(LENS), 4, 1, 96, 48),
+    ("one_token", LENS, [1] * len(LENS), 10, 2, 256, 16), ("one_token", [1], [1], 1, 1, 64, 1),
+    # several tokens, more of them than keys among them, idle sequences, more than one block of 32 rows
+    ("drafts", LENS, [0, 1, 5, 3, 0, 9, 2, 8, 4, 5, 7], 8, 2, 128, 7), ("drafts", LENS, [3, 1, 5, 3, 0, 9, 2, 8, 4, 5, 7], 16, 2, 64, 16), ("drafts", [700, 5], [40, 33], 16, 2, 128, 64),
+    ("drafts", LENS, [3, 1, 5, 3, 0, 9, 2, 8, 4, 5, 7], 32, 1, 96, 32), ("drafts", LENS, [3, 1, 5, 3, 0, 9, 2, 8, 4, 5, 7], 12, 4, 256, 1),
+    # long ones, cut into shares; many short ones
+    ("long", [5000], [1], 4, 1, 128, 16), ("long", [20000, 3, 777], [2, 1, 5], 4, 1, 64, 128), ("long", [9001, 12000], [6, 1], 8, 2, 256, 48), ("long", [7000], [8], 8, 1, 96, 33),
+    ("many", [(i * 37) % 150 for i in range(700)], [(i * 37) % 150 and 1 + i % 2 for i in range(700)], 8, 4, 64, 16), ("a_prompt", [260], [260], 4, 2, 128, 16),
+]
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("name,lens,new,heads,kv_heads,dim,page", CASES)
+def test_against_float64(name, lens, new, heads, kv_heads, dim, page, kind):
+    c = Case(lens, new, heads, kv_heads, dim, page, kind, pad=0 if kind == "bf16" else 3)
+    print(name, heads, kv_heads, dim, page, kind, flush=True)
+    o, lse = c.run()
+    c.check(o, lse)
+    again, lse_again = c.run()
+    assert torch.equal(o, again) and torch.equal(lse, lse_again)
+
+
+def test_without_lse_into_wider_rows():
+    c = Case(LENS, [1] * len(LENS), 8, 2, 128, 16)
+    wide = torch.full((c.total, 8 * 128 + 5), 7.0, dtype=BF16, device="cuda")
+    o = wide[:, :8 * 128].unflatten(1, (8, 128))
+    c.run(lse=False, o=o)
+    c.check(o, None)
+    assert bool((wide[:, 8 * 128:] == 7.0).all())
+
+
+@pytest.mark.parametrize("dim,kind", [(64, "bf16"), (96, "bf16"), (128, "bf16"), (256, "bf16"), (128, "e4m3")])
+def test_what_a_row_does_not_see_does_not_reach_it(dim, kind):
+    """Infinities and NaN in the keys and values of drafted tokens: rows before them are as they were, bit for bit; rows that see them are not finite."""
+    lens, new = [131, 40, 2500], [6, 5, 7]
+    c = Case(lens, new, 8, 2, dim, 16, kind, waste=0.0)
+    o, lse = c.run()
+    c.check(o, lse)
+    table = c.table.cpu()
+    for which in (0, 1):
+        for back, value in ((1, float("nan")), (3, float("inf") if kind == "bf16" else float("nan"))):
+            kept = c.caches[which].clone()
+            for i, L in enumerate(lens):
+                t = L - back
+                c.caches[which][table[i, t // 16], :, t % 16, dim // 2:] = torch.tensor(value).to(kept.dtype).cuda()
+            got, got_lse = c.run()
+            for i, n in enumerate(new):
+                before, behind = slice(c.q_start[i], c.q_start[i] + n - back), slice(c.q_start[i] + n - back, c.q_start[i + 1])
+                assert torch.equal(got[before], o[before]) and torch.equal(got_lse[:, before], lse[:, before]), (which, back, i)
+                if which == 1:
+                    assert not bool(torch.isfinite(got[behind][..., dim // 2:]).any()) and torch.equal(got[behind][..., :dim // 2], o[behind][..., :dim // 2])
+                elif value != value:
+                    assert not bool(torch.isfinite(got[behind]).any())
+            c.caches[which].copy_(kept)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_scores_of_any_size(dim):
+    """Scores that grow along the keys (every tile moves the maximum), that shrink, that are all far below zero, and a weight on one key only."""
+    for how in ("grow", "shrink", "far", "one"):
+        c = Case([700, 90], [2, 1], 4, 2, dim, 16, seed=3)
+        c.q.copy_(torch.ones_like(c.q))
+        for i, L in enumerate(c.lens):
+            t = torch.arange(L, device="cuda")
+            x = {"grow": t / 16.0, "shrink": -t / 16.0, "far": torch.full_like(t, -100.0, dtype=torch.float), "one": (t == L // 2) * 60.0}[how]
+            c.caches[0][c.table[i, t // 16].long(), :, t % 16] = (x / dim ** 0.5).to(BF16)[:, None, None].expand(-1, 2, dim)
+        o, lse = c.run()
+        c.check(o, lse)
+
+
+def test_pages_that_are_none():
+    """Tokens on a page whose number is none are masked; lengths past the table count as its own."""
+    c = Case([300, 64, 20, 16], [2, 1, 1, 1], 4, 2, 128, 16)
+    c.table[0, 3], c.table[0, 18], c.table[1, 0], c.table[2, 0], c.table[2, 1], c.table[3, 0] = -1, c.pages, 2**31 - 1, -5, -(2**31), -1
+    o, lse = c.run()
+    c.check(o, lse)
+    c = Case([48, 10], [1, 1], 4, 2, 128, 16)
+    c.kv_len[0] = 2**31 - 1
+    c.kv_len[1] = -3
+    o, lse = c.run()
+    c.lens = [48, 0]
+    c.check(o, lse)
+
+
+def test_starts_of_rows_out_of_range():
+    """Rows that are not there are not touched, whatever the starts say."""
+    c = Case([50, 60, 70], [1, 2, 3], 4, 2, 64, 16)
+    c.q_start = [0, 1, 3, 50]  # the last sequence's rows go past the tensor
+    o, lse = c.run()
+    n = c.total - 3  # rows that are there count as its new tokens
+    c.q_start, c.new = [0, 1, 3, c.total], [1, 2, n]
+    c.check(o, lse)
+    c.q_start = [0, -5, 1000, 2]
+    o, _ = c.run()
+    assert bool(torch.isfinite(o).all())
+
+
+def test_pool_past_offsets_of_32_bits():
+    """Pages past the first 2^32 elements of the pool."""
+    heads, dim, page = 8, 128, 64
+    pages = (1 << 32) // (heads * dim * page) + 40
+    c = Case([1500, 600], [1, 2], 16, heads, dim, page)
+    big, moved = [], pages - 1 - torch.arange(c.pages, device="cuda")
+    for x in c.caches:
+        y = torch.empty((pages, heads, page, dim), dtype=BF16, device="cuda")
+        y[moved] = x
+        big.append(y)
+    want, want_lse = c.run()
+    c.check(want, want_lse)
+    c.caches, c.pages, c.table = big, pages, torch.where(c.table >= 0, pages - 1 - c.table, c.table)
+    print("pool past 2^32 elements", flush=True)
+    o, lse = c.run()
+    assert torch.equal(o, want) and torch.equal(lse, want_lse)
+
+
+def test_replayed_graphs_follow_the_lengths_and_may_share_a_workspace():
+    """Two captured calls on one workspace, replayed one after the other while the sequences grow, with eager work between."""
+    from paper_2509_21275_amd import paged_attn as pa
+    cases = [Case([4000, 100], [1, 1], 8, 2, 128, 16, seed=1), Case([900, 3000], [2, 1], 8, 2, 64, 32, seed=2)]
+    descs = [c.desc() for c in cases]
+    ws = torch.empty(max(pa.paged_attn_workspace_bytes(d) for d in descs), dtype=torch.uint8, device="cuda")
+    starts = [torch.tensor(c.q_start, dtype=I32, device="cuda") for c in cases]
+    outs = [(torch.full((c.total, 8, c.dim), 7.0, dtype=BF16, device="cuda"), torch.full((8, c.total), 7.0, device="cuda")) for c in cases]
+    side, graphs = torch.cuda.Stream(), []
+    side.wait_stream(torch.cuda.current_stream())
+    full = [list(c.lens) for c in cases]
+    for c, d, s, (o, lse) in zip(cases, descs, starts, outs):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=side):
+            pa.paged_attn_fwd(d, c.q, *c.caches, c.table, c.kv_len, s, o, lse, ws)
+    torch.cuda.synchronize()
+    for rep in range(4):
+        for c, lens in zip(cases, full):
+            c.lens = [max(n, L * (rep + 1) // 4 - rep) for L, n in zip(lens, c.new)]
+            c.kv_len.copy_(torch.tensor(c.lens, dtype=I32))
+        for o, lse in outs:
+            o.fill_(7.0)
+            lse.fill_(7.0)
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for c, (o, lse) in zip(cases, outs):
+            c.check(o, lse)
+            eager, eager_lse = c.run()
+            assert torch.equal(o, eager) and torch.equal(lse, eager_lse)
+
+
+def test_on_another_stream_at_the_same_time():
+    cases = [Case([3000, 50], [1, 3], 8, 2, 128, 16, seed=s) for s in (4, 5)]
+    streams = [torch.cuda.Stream() for _ in cases]
+    from paper_2509_21275_amd import paged_attn as pa
+    outs = []
+    torch.cuda.synchronize()
+    for c, s in zip(cases, streams):
+        o, lse = torch.full((c.total, 8, 128), 7.0, dtype=BF16, device="cuda"), torch.full((8, c.total), 7.0, device="cuda")
+        outs.append((o, lse, torch.tensor(c.q_start, dtype=I32, device="cuda"), pa.alloc_workspace(c.desc())))
+    torch.cuda.synchronize()
+    for c, s, (o, lse, start, ws) in zip(cases, streams, outs):
+        for _ in range(3):
+            pa.paged_attn_fwd(c.desc(), c.q, *c.caches, c.table, c.kv_len, start, o, lse, ws, stream=s)
+    torch.cuda.synchronize()
+    for c, (o, lse, *_) in zip(cases, outs):
+        c.check(o, lse)
