@@ -28,6 +28,7 @@ constexpr int kTile = 32;               // keys of a tile
 constexpr int kBlockKeys = kTile * kWaves;
 constexpr int kLeastShare = 2;          // units of a share, at least
 constexpr float kFloor = -3e38f;        // of a running maximum: what is masked (-inf) stays below it, so that no difference of two infinities is formed
+constexpr float kGrowth = 8.f;            // log2
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct AttnArgs {
@@ -80,18 +81,19 @@ __device__ __forceinline__ int64_t wave_sum_up_to(int64_t x) {
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ int64_t uniform64(int64_t x) { return (int64_t)(((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32) | (uint32_t)uniform((int)x)); }
 
+// The lowest n bits (none if n < 0, all if n > 31).
+__device__ __forceinline__ unsigned first_bits(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1; }
+
 // 16 bytes of the cache.
 __device__ __forceinline__ u32x4 load16(const char* p) { return *reinterpret_cast<const u32x4*>(p); }
 // Eight e4m3 numbers as bf16, which has them all.
 __device__ __forceinline__ bf16x8 widen8(unsigned a, unsigned b) {
   bf16x8 r;
 #pragma unroll
-  for (int w = 0; w < 2; ++w) {
-    const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(w ? b : a, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w ? b : a, true);
-    r[4 * w] = (__bf16)lo[0];
-    r[4 * w + 1] = (__bf16)lo[1];
-    r[4 * w + 2] = (__bf16)hi[0];
-    r[4 * w + 3] = (__bf16)hi[1];
+  for (int w = 0; w < 4; ++w) {
+    const bf16x2 x = w & 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w & 2 ? b : a, 1.f, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w & 2 ? b : a, 1.f, false);
+    r[2 * w] = x[0];
+    r[2 * w + 1] = x[1];
   }
   return r;
 }
@@ -108,18 +110,42 @@ __device__ __forceinline__ bool some_not_finite(bf16x8 x) {
 template <int D>
 constexpr int v_pitch() { return D == 96 ? 192 : D * 2 + 64; }
 
-template <int D, bool E4M3>
+// Where the keys of a tile are: numbers of their pages and rows in them, of the first key of each half (HALVES: page_size is a multiple of 16, so that 16 keys lie on one page), or of this
+// lane's key (col); bit k of `there`: key k lies on a page that is one.
+template <bool HALVES>
+struct Place {
+  int number[2], row[2];
+  unsigned there;
+};
+template <>
+struct Place<false> {
+  int number, row;
+  unsigned there;
+};
+
+template <int D, bool E4M3, bool HALVES>
 __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_kernel(const AttnArgs a) {
   constexpr int kBytes = E4M3 ? 1 : 2;                  // of a number in the cache
   constexpr int kDims = D / 32;                         // 32 dimensions of the output, or of the scores' sum, at a time
   constexpr int kPitch = v_pitch<D>() / 2;              // elements
+  constexpr int kRowBytes = D * kBytes;
   constexpr int kRowChunks = D * kBytes / 16, kVChunks = kRowChunks / 2;  // 16-byte chunks of a row; of a tile, for each lane
+  constexpr bool kEven = 64 % kRowChunks == 0;          // a wave's 16-byte loads are whole rows
+  constexpr int kRowsApart = kEven ? 64 / kRowChunks : 0;
+  // The n-th 16 bytes of a tile's V that a lane has: key, place in the row, place in LDS.
+  struct Chunk {
+    int row, in_row, in_lds;
+    __device__ Chunk(int lane, int n) {
+      row = kEven ? lane / kRowChunks + n * kRowsApart : (lane + 64 * n) / kRowChunks;
+      in_row = kEven ? lane % kRowChunks : lane + 64 * n - row * kRowChunks;
+      in_lds = (kEven ? lane / kRowChunks * kPitch + n * (kRowsApart * kPitch) : row * kPitch) + in_row * (16 / kBytes);
+    }
+  };
   __shared__ __attribute__((aligned(16))) __bf16 tiles[kWaves][kTile * kPitch];
   __shared__ float maxima[kWaves][kRows], sums[kWaves][kRows];
   __shared__ int64_t wave_units[kWaves];
   __shared__ int64_t start_unit;
   __shared__ int start_seq;
-  __shared__ unsigned bad_rows[kWaves];
   static_assert(sizeof(tiles) >= 2 * kRows * D * 4, "two waves' values find room");
 
   const int head = blockIdx.x % a.heads, share = blockIdx.x / a.heads;
@@ -198,52 +224,91 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_kernel(const 
     float m = kFloor, l = 0.f;
 
     // ---- the walk ----
-    const int tile1 = min(block1 * kWaves, (most_seen + kTile - 1) / kTile);
+    const int tile1 = min(block1 * kWaves, (int)(((unsigned)most_seen + kTile - 1) / kTile));
     const int32_t* const pages = a.table + (int64_t)seq * a.max_pages;
-    // row of the cache that holds key `col` of a tile, or -1
-    auto cache_row = [&](int tile) {
-      const int key = tile * kTile + col;
-      if (key >= most_seen) return -1;
-      const int page = a.by_page(key), number = pages[page];
-      return number >= 0 && number < a.num_pages ? (int)(number * a.heads * a.page_size + head * a.page_size + key - page * a.page_size) : -1;
-    };
     u32x4 kr[kDims * kBytes], vr[kVChunks];
-    auto load_tile = [&](int at) {
-      const char* const p = k_base + (int64_t)max(at, 0) * (D * kBytes) + half * (16 * kBytes);
+    Place<HALVES> at, next;
+    auto find = [&](int tile) {
+      Place<HALVES> r;
+      if constexpr (HALVES) {
 #pragma unroll
-      for (int t = 0; t < kDims; ++t)
+        for (int h = 0; h < 2; ++h) {
+          const int key = tile * kTile + 16 * h, page = a.by_page(min(key, most_seen - 1));
+          r.number[h] = key < most_seen ? pages[page] : -1;
+          r.row[h] = key - page * a.page_size;
+        }
+      } else {
+        const int key = tile * kTile + col, page = a.by_page(min(key, most_seen - 1));
+        r.number = key < most_seen ? pages[page] : -1;
+        r.row = key - page * a.page_size;
+      }
+      return r;
+    };
+    // Starts the loads of a tile; afterwards at.there says which of its keys there are.
+    auto load_tile = [&]() {
+      if constexpr (HALVES) {
+        int rows[2];
+        bool ok[2];
 #pragma unroll
-        for (int u = 0; u < kBytes; ++u) kr[t * kBytes + u] = load16(p + t * (32 * kBytes) + u * 16);
+        for (int h = 0; h < 2; ++h) {
+          const int number = uniform(at.number[h]);
+          ok[h] = number >= 0 && number < a.num_pages;
+          rows[h] = ok[h] ? (number * a.heads + head) * a.page_size + at.row[h] : 0;
+        }
+        at.there = (ok[0] ? 0xffffu : 0u) | (ok[1] ? 0xffff0000u : 0u);
+        const char* const p = k_base + (int64_t)(col & 16 ? rows[1] : rows[0]) * kRowBytes + (col & 15) * kRowBytes + half * (16 * kBytes);
 #pragma unroll
-      for (int n = 0; n < kVChunks; ++n) {
-        const int c = lane + 64 * n, r = c / kRowChunks;
-        vr[n] = load16(v_base + (int64_t)max(__shfl(at, r), 0) * (D * kBytes) + (c - r * kRowChunks) * 16);
+        for (int t = 0; t < kDims; ++t)
+#pragma unroll
+          for (int u = 0; u < kBytes; ++u) kr[t * kBytes + u] = load16(p + t * (32 * kBytes) + u * 16);
+        if constexpr (kVChunks % 2 == 0) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const char* const from = v_base + (int64_t)rows[h] * kRowBytes;
+#pragma unroll
+            for (int n = 0; n < kVChunks / 2; ++n) vr[h * (kVChunks / 2) + n] = load16(from + (unsigned)(lane * 16 + n * 1024));
+          }
+        } else {
+#pragma unroll
+          for (int n = 0; n < kVChunks; ++n) {
+            const int c = lane * 16 + n * 1024;
+            vr[n] = load16(v_base + (c >= 16 * kRowBytes ? (int64_t)rows[1] * kRowBytes + (c - 16 * kRowBytes) : (int64_t)rows[0] * kRowBytes + c));
+          }
+        }
+      } else {
+        const bool ok = at.number >= 0 && at.number < a.num_pages;
+        const int row = ok ? (at.number * a.heads + head) * a.page_size + at.row : 0;
+        at.there = (unsigned)__ballot(ok);
+        const char* const p = k_base + (int64_t)row * kRowBytes + half * (16 * kBytes);
+#pragma unroll
+        for (int t = 0; t < kDims; ++t)
+#pragma unroll
+          for (int u = 0; u < kBytes; ++u) kr[t * kBytes + u] = load16(p + t * (32 * kBytes) + u * 16);
+#pragma unroll
+        for (int n = 0; n < kVChunks; ++n) {
+          const Chunk c(lane, n);
+          vr[n] = load16(v_base + (int64_t)__shfl(row, c.row) * kRowBytes + c.in_row * 16);
+        }
       }
     };
-    int tile = block0 * kWaves + wave;
-    int at = tile < tile1 ? cache_row(tile) : -1, next_at = tile + kWaves < tile1 ? cache_row(tile + kWaves) : -1;
-    if (tile < tile1) load_tile(at);
     __bf16* const v_tile = tiles[wave];
+    int tile = block0 * kWaves + wave;
+    at = find(tile);
+    next = find(tile + kWaves);
+    load_tile();
     for (; tile < tile1; tile += kWaves) {
-      const bool there = at >= 0;
-      const bool whole = (tile + 1) * kTile <= first_seen && __all(there);
-      // V to LDS, rows that nobody sees as zeros
-      unsigned odd = 0;  // whether this lane has numbers that are not finite
+      // bit k: key k of the tile is there and seen by a row of the block; is seen by this lane's row
+      const unsigned keys = at.there & first_bits(most_seen - tile * kTile), visible = at.there & first_bits(seen - tile * kTile);
+      const bool border = (tile + 1) * kTile > first_seen || at.there != 0xffffffffu;
+      // V to LDS
 #pragma unroll
       for (int n = 0; n < kVChunks; ++n) {
-        const int c = lane + 64 * n, r = c / kRowChunks;
-        u32x4 x = vr[n];
-        if (!whole && __shfl((int)there, r) == 0) x = u32x4{};
+        __bf16* const to = v_tile + Chunk(lane, n).in_lds;
         if constexpr (E4M3) {
-          const bf16x8 lo = widen8(x[0], x[1]), hi = widen8(x[2], x[3]);
-          if (!whole && (some_not_finite(lo) || some_not_finite(hi))) odd |= 1u << r;
-          __bf16* const p = v_tile + r * kPitch + (c - r * kRowChunks) * 16;
-          *reinterpret_cast<bf16x8*>(p) = lo;
-          *reinterpret_cast<bf16x8*>(p + 8) = hi;
+          *reinterpret_cast<bf16x8*>(to) = widen8(vr[n][0], vr[n][1]);
+          *reinterpret_cast<bf16x8*>(to + 8) = widen8(vr[n][2], vr[n][3]);
         } else {
-          const bf16x8 y = __builtin_bit_cast(bf16x8, x);
-          if (!whole && some_not_finite(y)) odd |= 1u << r;
-          *reinterpret_cast<bf16x8*>(v_tile + r * kPitch + (c - r * kRowChunks) * 8) = y;
+          *reinterpret_cast<u32x4*>(to) = vr[n];
         }
       }
       // scores
@@ -255,23 +320,25 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_kernel(const 
         else x = __builtin_bit_cast(bf16x8, kr[n]);
         score = mfma32(x, q[n], score);
       }
-      // the next tile, and the page of the one after it
-      const unsigned keys_there = whole ? 0xffffffffu : (unsigned)__ballot(there);
-      at = next_at;
-      if (tile + kWaves < tile1) {
-        load_tile(at);
-        next_at = tile + 2 * kWaves < tile1 ? cache_row(tile + 2 * kWaves) : -1;
-      }
-      // bit e: key of score[e] is one that the row sees
-      unsigned visible = 0xffffu;
-      if (!whole) {
+      // the next tile, and the page of the one after it (behind the last one: loads that nobody waits for, of a row that is there)
+      at = next;
+      load_tile();
+      next = find(tile + 2 * kWaves);
+      __builtin_amdgcn_sched_barrier(0);
+      unsigned odd = 0;  // bit k: values of key k are not all finite
+      if (border) {
+        const unsigned mine = visible >> (4 * half);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int key = 8 * (e >> 2) + 4 * half + (e & 3);
-          if (tile * kTile + key >= seen || !(keys_there >> key & 1)) {
-            visible &= ~(1u << e);
-            score[e] = -INFINITY;
+        for (int e = 0; e < 16; ++e) score[e] = mine & (1u << (8 * (e >> 2) + (e & 3))) ? score[e] : -INFINITY;
+        // keys that no row sees are zeros
+#pragma unroll 1
+        for (int key = 0; key < kTile; ++key) {
+          bool bad = false;
+          for (int i = lane; i < D; i += 64) {
+            if (!(keys >> key & 1)) v_tile[key * kPitch + i] = (__bf16)0.f;
+            else bad = bad || !(fabsf((float)v_tile[key * kPitch + i]) < INFINITY);
           }
+          if (__any(bad)) odd |= 1u << key;
         }
       }
       // softmax
@@ -279,7 +346,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_kernel(const 
 #pragma unroll
       for (int e = 1; e < 16; ++e) top = fmaxf(top, score[e]);
       top = fmaxf(m, max_halves(top) * scale);
-      if (__any(top > m)) {
+      if (__any(top > m + kGrowth)) {
         const float f = __builtin_amdgcn_exp2f(m - top);
         l *= f;
 #pragma unroll
@@ -288,37 +355,30 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_kernel(const 
           for (int e = 0; e < 16; ++e) acc[t][e] *= f;
         m = top;
       }
-      float p[16];
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        p[e] = __builtin_amdgcn_exp2f(score[e] * scale - m);
-        l += p[e];
+        score[e] = __builtin_amdgcn_exp2f(score[e] * scale - m);
+        l += score[e];
       }
-      if (!whole && __any(odd != 0)) {
-        // Values that are not finite, in keys that some rows do not see: zero times them is not zero.  Such values are added without the product, to the rows that see them, and leave it.
-        if (lane == 0) bad_rows[wave] = 0;
-        __builtin_amdgcn_wave_barrier();
-        if (odd != 0) atomicOr(&bad_rows[wave], odd);
-        __builtin_amdgcn_wave_barrier();
-        for (unsigned bad = *(volatile unsigned*)&bad_rows[wave]; bad != 0; bad &= bad - 1) {
-          const int key = __ffs((int)bad) - 1;
+      // Values that are not finite, in keys that some rows do not see: zero times them is not zero.  Such values are added without the product, to the rows that see them, and leave it.
+      {
+        for (; odd != 0; odd &= odd - 1) {
+          const int key = __ffs((int)odd) - 1;
           float weight = 0.f;
-          bool sees = false;
 #pragma unroll
           for (int e = 0; e < 16; ++e)
-            if (8 * (e >> 2) + 4 * half + (e & 3) == key) {
-              weight = p[e];
-              sees = visible >> e & 1;
-            }
-          const int from = col + 32 * (key >> 2 & 1);  // the half that has the key
-          weight = __shfl(weight, from);
-          sees = __shfl((int)sees, from) != 0;
+            if (key - 4 * half == 8 * (e >> 2) + (e & 3)) weight = score[e];
+          weight = __shfl(weight, col + 32 * (key >> 2 & 1));  // from the half that has the key
+          const bool sees = visible >> key & 1;
 #pragma unroll
           for (int t = 0; t < kDims; ++t)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const float x = (float)v_tile[key * kPitch + 32 * t + 8 * (e >> 2) + 4 * half + (e & 3)];
-              if (sees && !(fabsf(x) < INFINITY)) acc[t][e] += weight * x;
+            for (int g = 0; g < 4; ++g) {
+              const bf16x4 x = *reinterpret_cast<const bf16x4*>(v_tile + key * kPitch + 32 * t + 8 * g + 4 * half);
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                acc[t][4 * g + e] += sees && !(fabsf((float)x[e]) < INFINITY) ? weight * (float)x[e] : 0.f;
+              __builtin_amdgcn_sched_barrier(0);
             }
           __builtin_amdgcn_wave_barrier();
           for (int i = lane; i < D; i += 64)
@@ -332,8 +392,8 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_kernel(const 
         bf16x8 hi, lo;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          hi[e] = (__bf16)p[8 * st + e];
-          lo[e] = (__bf16)(p[8 * st + e] - (float)hi[e]);
+          hi[e] = (__bf16)score[8 * st + e];
+          lo[e] = (__bf16)(score[8 * st + e] - (float)hi[e]);
         }
         // lanes 4 e + c of a group of 16 address dimensions 4 c .. 4 c + 3 of its key e
         const __bf16* const from = v_tile + (16 * st + 4 * half + (lane >> 2 & 3)) * kPitch + (lane >> 4 & 1) * 16 + (lane & 3) * 4;
@@ -551,8 +611,13 @@ extern "C" int paged_attn_fwd(const paged_attn_desc* d, const void* q, int64_t q
   const hipError_t e = by_dim(d->head_dim, [&](auto dim) {
     constexpr int D = decltype(dim)::value;
     const dim3 grid((unsigned)(shares * heads));
-    if (e4m3) hipLaunchKernelGGL((attn_kernel<D, true>), grid, dim3(kThreads), 0, stream, a);
-    else hipLaunchKernelGGL((attn_kernel<D, false>), grid, dim3(kThreads), 0, stream, a);
+    auto with_pages = [&](auto halves) {
+      constexpr bool HALVES = decltype(halves)::value;
+      if (e4m3) hipLaunchKernelGGL((attn_kernel<D, true, HALVES>), grid, dim3(kThreads), 0, stream, a);
+      else hipLaunchKernelGGL((attn_kernel<D, false, HALVES>), grid, dim3(kThreads), 0, stream, a);
+    };
+    if (d->page_size % 16 == 0) with_pages(std::true_type{});
+    else with_pages(std::false_type{});
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || shares == 1) return e;
     // rows of a block that is cut: one to a workgroup, as long as that makes no more than 4096 of them
