@@ -142,6 +142,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_kernel(const 
     }
   };
   __shared__ __attribute__((aligned(16))) __bf16 tiles[kWaves][kTile * kPitch];
+  __shared__ bf16x8 q[2 * kDims][64];
   __shared__ float maxima[kWaves][kRows], sums[kWaves][kRows];
   __shared__ int64_t wave_units[kWaves];
   __shared__ int64_t start_unit;
@@ -209,17 +210,20 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_kernel(const 
     const int seen = s.len - tokens + token + 1;  // keys that the row sees (none if <= 0)
     const int first_seen = s.len - tokens + a.by_group(row_block * kRows) + 1;                               // of the block's first row,
     const int most_seen = max(0, s.len - tokens + a.by_group(min(row_block * kRows + kRows, s.rows) - 1) + 1);  // and of its last
-    // operand B of K Q^T: in step 2 t + u, half h has dimensions 32 t + 16 h + 8 u .. + 7
-    bf16x8 q[2 * kDims];
+    // operand B of K Q^T, to LDS in the order in which the lanes read it: in step 2 t + u, half h has dimensions 32 t + 16 h + 8 u .. + 7 (in registers it would leave too few
+    // for the loads ahead)
     {
       const __bf16* const p = a.q + (int64_t)q_row * a.q_stride + (int64_t)q_head * D + 16 * half;
 #pragma unroll
-      for (int n = 0; n < 2 * kDims; ++n) {
-        const Loose8 x = *reinterpret_cast<const Loose8*>(p + (n >> 1) * 32 + (n & 1) * 8);
-        q[n] = __builtin_bit_cast(bf16x8, x);
-        if (!live) q[n] = bf16x8{};
+      for (int i = 0; i < (2 * kDims + kWaves - 1) / kWaves; ++i) {
+        const int n = i * kWaves + wave;
+        if (n < 2 * kDims) {
+          const Loose8 x = *reinterpret_cast<const Loose8*>(p + (n >> 1) * 32 + (n & 1) * 8);
+          q[n][lane] = live ? __builtin_bit_cast(bf16x8, x) : bf16x8{};
+        }
       }
     }
+    __syncthreads();
     f32x16 acc[kDims] = {};
     float m = kFloor, l = 0.f;
 
@@ -318,7 +322,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_kernel(const 
         bf16x8 x;
         if constexpr (E4M3) x = n & 1 ? widen8(kr[n >> 1][2], kr[n >> 1][3]) : widen8(kr[n >> 1][0], kr[n >> 1][1]);
         else x = __builtin_bit_cast(bf16x8, kr[n]);
-        score = mfma32(x, q[n], score);
+        score = mfma32(x, q[n][lane], score);
       }
       // the next tile, and the page of the one after it (behind the last one: loads that nobody waits for, of a row that is there)
       at = next;
