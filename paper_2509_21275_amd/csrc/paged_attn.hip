@@ -97,13 +97,17 @@ __device__ __forceinline__ bf16x8 widen8(unsigned a, unsigned b) {
   }
   return r;
 }
-// Whether one of eight bf16 numbers is infinite or none.
-__device__ __forceinline__ bool some_not_finite(bf16x8 x) {
-  bool r = false;
-  const u32x4 w = __builtin_bit_cast(u32x4, x);
+// Whether one of the numbers in 16 bytes of the cache is infinite or none.
+template <bool E4M3>
+__device__ __forceinline__ bool some_not_finite(u32x4 x) {
+  unsigned r = 0;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) r |= (w[e] & 0x7f80u) == 0x7f80u || (w[e] & 0x7f800000u) == 0x7f800000u;
-  return r;
+  for (int e = 0; e < 4; ++e) {
+    // an exponent of ones (e4m3: a NaN, all other bits ones), plus one in its last place, overflows into the bit above it
+    if (E4M3) r |= ((x[e] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+    else r |= ((x[e] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+  }
+  return r != 0;
 }
 
 // Bytes from row to row of V's tile in LDS: 64 bytes past a multiple of 256 (192: 64 short of it), so that the four rows of a transposed read lie on different banks.
@@ -124,12 +128,14 @@ struct Place<false> {
 };
 
 template <int D, bool E4M3, bool HALVES>
-__global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_kernel(const AttnArgs a) {
+__global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
   constexpr int kBytes = E4M3 ? 1 : 2;                  // of a number in the cache
-  constexpr int kDims = D / 32;                         // 32 dimensions of the output, or of the scores' sum, at a time
-  constexpr int kPitch = v_pitch<D>() / 2;              // elements
-  constexpr int kRowBytes = D * kBytes;
-  constexpr int kRowChunks = D * kBytes / 16, kVChunks = kRowChunks / 2;  // 16-byte chunks of a row; of a tile, for each lane
+  constexpr int kParts = D == 256 ? 2 : 1, kTeams = kWaves / kParts;
+  constexpr int kOwn = D / kParts;                      // dimensions of a wave
+  constexpr int kDims = kOwn / 32;                      // 32 dimensions of the output, or of the scores' sum, at a time
+  constexpr int kPitch = v_pitch<kOwn>() / 2;           // elements
+  constexpr int kRowBytes = D * kBytes, kOwnBytes = kOwn * kBytes;
+  constexpr int kRowChunks = kOwnBytes / 16, kVChunks = kRowChunks / 2;  // 16-byte chunks of a wave's part of a row; of a tile, for each lane
   constexpr bool kEven = 64 % kRowChunks == 0;          // a wave's 16-byte loads are whole rows
   constexpr int kRowsApart = kEven ? 64 / kRowChunks : 0;
   // The n-th 16 bytes of a tile's V that a lane has: key, place in the row, place in LDS.
@@ -142,15 +148,17 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_kernel(const 
     }
   };
   __shared__ __attribute__((aligned(16))) __bf16 tiles[kWaves][kTile * kPitch];
-  __shared__ bf16x8 q[2 * kDims][64];
+  __shared__ bf16x8 q[D / 16][64];
+  __shared__ f32x4 partial[kParts == 2 ? kWaves : 1][4][64];  // scores of a wave's dimensions
   __shared__ float maxima[kWaves][kRows], sums[kWaves][kRows];
   __shared__ int64_t wave_units[kWaves];
   __shared__ int64_t start_unit;
   __shared__ int start_seq;
-  static_assert(sizeof(tiles) >= 2 * kRows * D * 4, "two waves' values find room");
+  static_assert(sizeof(tiles) >= 2 * kRows * kOwn * 4, "two waves' values find room");
 
   const int head = blockIdx.x % a.heads, share = blockIdx.x / a.heads;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
+  const int part = wave % kParts, team = wave / kParts;
 
   // ---- the share: units first .. last - 1 of all ----
   const int each = (a.num_seqs + kThreads - 1) / kThreads;
@@ -189,7 +197,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_kernel(const 
   int64_t in_seq = uniform64(start_unit);  // units of the sequence before the next
   const float k_scale = E4M3 ? a.k_scale[head] : 1.f, v_scale = E4M3 ? a.v_scale[head] : 1.f;
   const float scale = a.scale_log2 * k_scale;
-  const char *const k_base = (const char*)a.k, *const v_base = (const char*)a.v;
+  const char *const k_base = (const char*)a.k + part * kOwnBytes, *const v_base = (const char*)a.v + part * kOwnBytes;
 
   for (int64_t unit = first; unit < last;) {
     Sequence s = sequence_at(a, seq);
@@ -215,9 +223,9 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_kernel(const 
     {
       const __bf16* const p = a.q + (int64_t)q_row * a.q_stride + (int64_t)q_head * D + 16 * half;
 #pragma unroll
-      for (int i = 0; i < (2 * kDims + kWaves - 1) / kWaves; ++i) {
+      for (int i = 0; i < (D / 16 + kWaves - 1) / kWaves; ++i) {
         const int n = i * kWaves + wave;
-        if (n < 2 * kDims) {
+        if (n < D / 16) {
           const Loose8 x = *reinterpret_cast<const Loose8*>(p + (n >> 1) * 32 + (n & 1) * 8);
           q[n][lane] = live ? __builtin_bit_cast(bf16x8, x) : bf16x8{};
         }
@@ -265,19 +273,13 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_kernel(const 
         for (int t = 0; t < kDims; ++t)
 #pragma unroll
           for (int u = 0; u < kBytes; ++u) kr[t * kBytes + u] = load16(p + t * (32 * kBytes) + u * 16);
-        if constexpr (kVChunks % 2 == 0) {
+        const char* const from[2] = {v_base + (int64_t)rows[0] * kRowBytes, v_base + (int64_t)rows[1] * kRowBytes};
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const char* const from = v_base + (int64_t)rows[h] * kRowBytes;
-#pragma unroll
-            for (int n = 0; n < kVChunks / 2; ++n) vr[h * (kVChunks / 2) + n] = load16(from + (unsigned)(lane * 16 + n * 1024));
-          }
-        } else {
-#pragma unroll
-          for (int n = 0; n < kVChunks; ++n) {
-            const int c = lane * 16 + n * 1024;
-            vr[n] = load16(v_base + (c >= 16 * kRowBytes ? (int64_t)rows[1] * kRowBytes + (c - 16 * kRowBytes) : (int64_t)rows[0] * kRowBytes + c));
-          }
+        for (int n = 0; n < kVChunks; ++n) {
+          // (where a wave's loads are whole rows, the n-th is of one half)
+          const Chunk c(lane, n);
+          if constexpr (kEven && kRowsApart <= 16) vr[n] = load16(from[n * kRowsApart / 16] + (unsigned)(lane / kRowChunks * kRowBytes + c.in_row * 16) + (n * kRowsApart % 16) * kRowBytes);
+          else vr[n] = load16((c.row & 16 ? from[1] : from[0]) + (c.row & 15) * kRowBytes + c.in_row * 16);
         }
       } else {
         const bool ok = at.number >= 0 && at.number < a.num_pages;
@@ -296,15 +298,30 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_kernel(const 
       }
     };
     __bf16* const v_tile = tiles[wave];
-    int tile = block0 * kWaves + wave;
+    int tile = block0 * kWaves + team;
     at = find(tile);
-    next = find(tile + kWaves);
+    next = find(tile + kTeams);
     load_tile();
-    for (; tile < tile1; tile += kWaves) {
+    // (teams of two waves: all of them go on to the last tile of any, as they wait for each other)
+    for (; kParts == 1 ? tile < tile1 : tile - team < tile1; tile += kTeams) {
       // bit k: key k of the tile is there and seen by a row of the block; is seen by this lane's row
       const unsigned keys = at.there & first_bits(most_seen - tile * kTile), visible = at.there & first_bits(seen - tile * kTile);
       const bool border = (tile + 1) * kTile > first_seen || at.there != 0xffffffffu;
       // V to LDS
+      unsigned odd = 0;  // bit k: this lane has values of key k that are not finite
+      if (border) {      // keys that no row sees are zeros
+        const int first_row = kEven ? lane / kRowChunks : 0;
+        const unsigned mine = keys >> first_row;
+#pragma unroll
+        for (int n = 0; n < kVChunks; ++n) {
+          const int row = kEven ? n * kRowsApart : Chunk(lane, n).row;  // (less first_row)
+          const bool there = mine & (1u << row);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) vr[n][e] = there ? vr[n][e] : 0;
+          odd |= some_not_finite<E4M3>(vr[n]) ? 1u << row : 0u;
+        }
+        odd <<= first_row;
+      }
 #pragma unroll
       for (int n = 0; n < kVChunks; ++n) {
         __bf16* const to = v_tile + Chunk(lane, n).in_lds;
@@ -322,28 +339,30 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_kernel(const 
         bf16x8 x;
         if constexpr (E4M3) x = n & 1 ? widen8(kr[n >> 1][2], kr[n >> 1][3]) : widen8(kr[n >> 1][0], kr[n >> 1][1]);
         else x = __builtin_bit_cast(bf16x8, kr[n]);
-        score = mfma32(x, q[n][lane], score);
+        score = mfma32(x, q[part * 2 * kDims + n][lane], score);
       }
       // the next tile, and the page of the one after it (behind the last one: loads that nobody waits for, of a row that is there)
       at = next;
       load_tile();
-      next = find(tile + 2 * kWaves);
+      next = find(tile + 2 * kTeams);
       __builtin_amdgcn_sched_barrier(0);
-      unsigned odd = 0;  // bit k: values of key k are not all finite
+      if constexpr (kParts == 2) {  // the other half of the dimensions
+        wg_barrier();  // (the last tile's have been read: their sums were used)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) partial[wave][g][lane] = f32x4{score[4 * g], score[4 * g + 1], score[4 * g + 2], score[4 * g + 3]};
+        __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): what this wave wrote is there; its loads go on
+        wg_barrier();
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const f32x4 x = partial[wave ^ 1][g][lane];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) score[4 * g + e] += x[e];
+        }
+      }
       if (border) {
         const unsigned mine = visible >> (4 * half);
 #pragma unroll
         for (int e = 0; e < 16; ++e) score[e] = mine & (1u << (8 * (e >> 2) + (e & 3))) ? score[e] : -INFINITY;
-        // keys that no row sees are zeros
-#pragma unroll 1
-        for (int key = 0; key < kTile; ++key) {
-          bool bad = false;
-          for (int i = lane; i < D; i += 64) {
-            if (!(keys >> key & 1)) v_tile[key * kPitch + i] = (__bf16)0.f;
-            else bad = bad || !(fabsf((float)v_tile[key * kPitch + i]) < INFINITY);
-          }
-          if (__any(bad)) odd |= 1u << key;
-        }
       }
       // softmax
       float top = score[0];
@@ -365,9 +384,12 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_kernel(const 
         l += score[e];
       }
       // Values that are not finite, in keys that some rows do not see: zero times them is not zero.  Such values are added without the product, to the rows that see them, and leave it.
-      {
-        for (; odd != 0; odd &= odd - 1) {
-          const int key = __ffs((int)odd) - 1;
+      if (border && __any(odd != 0)) {
+#pragma unroll
+        for (int o = 32; o >= 1; o >>= 1) odd |= __shfl_xor((int)odd, o);
+#pragma unroll 1
+        for (unsigned left = uniform((int)odd); left != 0; left &= left - 1) {
+          const int key = __ffs((int)left) - 1;
           float weight = 0.f;
 #pragma unroll
           for (int e = 0; e < 16; ++e)
@@ -385,7 +407,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_kernel(const 
               __builtin_amdgcn_sched_barrier(0);
             }
           __builtin_amdgcn_wave_barrier();
-          for (int i = lane; i < D; i += 64)
+          for (int i = lane; i < kOwn; i += 64)
             if (!(fabsf((float)v_tile[key * kPitch + i]) < INFINITY)) v_tile[key * kPitch + i] = (__bf16)0.f;
           __builtin_amdgcn_wave_barrier();
         }
@@ -399,6 +421,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_kernel(const 
           hi[e] = (__bf16)score[8 * st + e];
           lo[e] = (__bf16)(score[8 * st + e] - (float)hi[e]);
         }
+        __builtin_amdgcn_sched_barrier(0);
         // lanes 4 e + c of a group of 16 address dimensions 4 c .. 4 c + 3 of its key e
         const __bf16* const from = v_tile + (16 * st + 4 * half + (lane >> 2 & 3)) * kPitch + (lane >> 4 & 1) * 16 + (lane & 3) * 4;
 #pragma unroll
@@ -413,16 +436,16 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_kernel(const 
 
     // ---- the waves' results together ----
     l = sum_halves(l);
-    if (half == 0) {
+    if (half == 0) {  // (a team's waves have the same)
       maxima[wave][col] = m;
       sums[wave][col] = l;
     }
     __syncthreads();  // (and no wave reads its tile any more)
     float top = kFloor, sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, maxima[w][col]);
+    for (int w = 0; w < kWaves; w += kParts) top = fmaxf(top, maxima[w][col]);
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) sum += sums[w][col] * __builtin_amdgcn_exp2f(maxima[w][col] - top);
+    for (int w = 0; w < kWaves; w += kParts) sum += sums[w][col] * __builtin_amdgcn_exp2f(maxima[w][col] - top);
     const float f = __builtin_amdgcn_exp2f(m - top);
 #pragma unroll
     for (int t = 0; t < kDims; ++t)
@@ -448,15 +471,17 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_kernel(const 
     if (wave >= 2) give(wave - 2);
     __syncthreads();
     if (wave < 2) take(wave);
-    __syncthreads();
-    if (wave == 1) give(0);
-    __syncthreads();
-    if (wave == 0) {
-      take(0);
+    if constexpr (kParts == 1) {
+      __syncthreads();
+      if (wave == 1) give(0);
+      __syncthreads();
+      if (wave == 0) take(0);
+    }
+    if (team == 0) {
       if (block0 == 0 && block1 == key_blocks) {
         if (live) {
           const float inv = sum > 0.f || sum != sum ? v_scale / sum : 0.f;
-          __bf16* const to = a.o + (int64_t)q_row * a.o_stride + (int64_t)q_head * D + 4 * half;
+          __bf16* const to = a.o + (int64_t)q_row * a.o_stride + (int64_t)q_head * D + part * kOwn + 4 * half;
 #pragma unroll
           for (int t = 0; t < kDims; ++t)
 #pragma unroll
@@ -466,22 +491,22 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_kernel(const 
               };
               reinterpret_cast<Loose4*>(to + 32 * t + 8 * g)->x = pack4(acc[t][4 * g] * inv, acc[t][4 * g + 1] * inv, acc[t][4 * g + 2] * inv, acc[t][4 * g + 3] * inv);
             }
-          if (a.lse && half == 0) a.lse[(int64_t)q_head * a.total_q + q_row] = sum > 0.f || sum != sum ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+          if (a.lse && half == 0 && part == 0) a.lse[(int64_t)q_head * a.total_q + q_row] = sum > 0.f || sum != sum ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
         }
       } else {
-        float* const part = a.parts + ((int64_t)(share * 2 + (block0 == 0)) * a.heads + head) * part_floats<D>();
+        float* const into = a.parts + ((int64_t)(share * 2 + (block0 == 0)) * a.heads + head) * part_floats<D>();
         if (live) {
 #pragma unroll
           for (int t = 0; t < kDims; ++t)
 #pragma unroll
             for (int g = 0; g < 4; ++g)
-              *reinterpret_cast<f32x4*>(part + col * D + 32 * t + 8 * g + 4 * half) = f32x4{acc[t][4 * g], acc[t][4 * g + 1], acc[t][4 * g + 2], acc[t][4 * g + 3]};
-          if (half == 0) {
-            part[kRows * D + col] = top;
-            part[kRows * D + kRows + col] = sum;
+              *reinterpret_cast<f32x4*>(into + col * D + part * kOwn + 32 * t + 8 * g + 4 * half) = f32x4{acc[t][4 * g], acc[t][4 * g + 1], acc[t][4 * g + 2], acc[t][4 * g + 3]};
+          if (half == 0 && part == 0) {
+            into[kRows * D + col] = top;
+            into[kRows * D + kRows + col] = sum;
           }
         }
-        if (lane == 0 && head == 0 && block0 == 0) {
+        if (lane == 0 && wave == 0 && head == 0 && block0 == 0) {
           a.cuts[share * kCut + kCutSeq] = seq;
           a.cuts[share * kCut + kCutBlock] = row_block;
           a.cuts[share * kCut + kCutShares] = (int)((unit + key_blocks - 1) / size) - share + 1;
@@ -560,11 +585,11 @@ int check_desc(const paged_attn_desc* d) {
     return CHUNK_ATTN_INVALID_ARG;
   return CHUNK_ATTN_OK;
 }
-// Workgroups for each key/value head: two to a compute unit (256: one), and no more than there can be shares.
+// Workgroups for each key/value head: two to a compute unit, and no more than there can be shares.
 int count_shares(const paged_attn_desc* d) {
   const int64_t most_keys = (int64_t)d->max_pages * d->page_size, group = d->num_q_heads / d->num_kv_heads;
   const int64_t blocks = std::min<int64_t>((int64_t)d->num_seqs + d->total_q * group / kRows, std::max<int64_t>(d->total_q * group, 1)) * ((most_keys + kBlockKeys - 1) / kBlockKeys);
-  const int64_t fill = ((d->head_dim == 256 ? 1 : 2) * kCus + d->num_kv_heads - 1) / d->num_kv_heads;
+  const int64_t fill = (2 * kCus + d->num_kv_heads - 1) / d->num_kv_heads;
   return (int)std::max<int64_t>(1, std::min<int64_t>(fill, (blocks + kLeastShare - 1) / kLeastShare));
 }
 size_t part_bytes(const paged_attn_desc* d) { return (size_t)count_shares(d) * 2 * d->num_kv_heads * kRows * (d->head_dim + 2) * sizeof(float); }
