@@ -43,20 +43,29 @@ struct AttnArgs {
   float* parts;   // two of each (share, head): the block of rows that came from the share before, and the one that goes on in the next
   int32_t* cuts;  // [shares][kCut]: the block of rows that goes on in the next share
   int32_t num_seqs, total_q, heads, group, page_size, num_pages, max_pages, shares;
+  int32_t most_subs;  // groups of rows that walk over the keys together, at most
   float scale_log2;
   Divide by_page, by_group;
 };
 enum { kCutSeq, kCutBlock, kCutShares, kCut = 4 };  // sequence, block of rows, shares that it reaches into (0: none)
 
+// Head dimension 256: a tile takes two waves, and LDS has no room for the queries of more groups.
+template <int D>
+constexpr int most_subs() { return D == 256 ? 1 : 4; }
 template <int D>
 constexpr int part_floats() { return kRows * (D + 2); }
 
 // Sequence i, its numbers brought into their ranges.
 struct Sequence {
   int len, rows, first_row;  // tokens; rows of a key/value head; first row of q
-  __device__ int row_blocks() const { return (rows + kRows - 1) / kRows; }
+  // groups of kRows rows that walk over the keys together: 1, 2 or 4 (`most` at most)
+  __device__ int subs(int most) const { return rows <= kRows ? 1 : rows <= 2 * kRows ? min(2, most) : most; }
+  __device__ int row_blocks(int most) const {
+    const int n = kRows * subs(most);
+    return (rows + n - 1) / n;
+  }
   __device__ int key_blocks() const { return max(1, (int)(((unsigned)len + kBlockKeys - 1) / kBlockKeys)); }
-  __device__ int64_t units() const { return (int64_t)row_blocks() * key_blocks(); }
+  __device__ int64_t units(int most) const { return (int64_t)row_blocks(most) * key_blocks(); }
 };
 __device__ __forceinline__ Sequence sequence_at(const AttnArgs& a, int i) {
   Sequence s;
@@ -130,12 +139,13 @@ struct Place<false> {
 template <int D, bool E4M3, bool HALVES>
 __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
   constexpr int kBytes = E4M3 ? 1 : 2;                  // of a number in the cache
-  constexpr int kParts = D == 256 ? 2 : 1, kTeams = kWaves / kParts;
+  constexpr int kParts = D == 256 ? 2 : 1, kSubs = most_subs<D>();
   constexpr int kOwn = D / kParts;                      // dimensions of a wave
   constexpr int kDims = kOwn / 32;                      // 32 dimensions of the output, or of the scores' sum, at a time
   constexpr int kPitch = v_pitch<kOwn>() / 2;           // elements
   constexpr int kRowBytes = D * kBytes, kOwnBytes = kOwn * kBytes;
   constexpr int kRowChunks = kOwnBytes / 16, kVChunks = kRowChunks / 2;  // 16-byte chunks of a wave's part of a row; of a tile, for each lane
+  constexpr int kAhead = E4M3 ? 2 : 1;                  // tiles that are loaded ahead
   constexpr bool kEven = 64 % kRowChunks == 0;          // a wave's 16-byte loads are whole rows
   constexpr int kRowsApart = kEven ? 64 / kRowChunks : 0;
   // The n-th 16 bytes of a tile's V that a lane has: key, place in the row, place in LDS.
@@ -148,7 +158,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
     }
   };
   __shared__ __attribute__((aligned(16))) __bf16 tiles[kWaves][kTile * kPitch];
-  __shared__ bf16x8 q[D / 16][64];
+  __shared__ bf16x8 q[kSubs][D / 16][64];
   __shared__ f32x4 partial[kParts == 2 ? kWaves : 1][4][64];  // scores of a wave's dimensions
   __shared__ float maxima[kWaves][kRows], sums[kWaves][kRows];
   __shared__ int64_t wave_units[kWaves];
@@ -158,13 +168,13 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
 
   const int head = blockIdx.x % a.heads, share = blockIdx.x / a.heads;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
-  const int part = wave % kParts, team = wave / kParts;
+  const int part = wave % kParts;
 
   // ---- the share: units first .. last - 1 of all ----
   const int each = (a.num_seqs + kThreads - 1) / kThreads;
   const int seq0 = min((int)threadIdx.x * each, a.num_seqs), seq1 = min(seq0 + each, a.num_seqs);
   int64_t mine = 0;
-  for (int i = seq0; i < seq1; ++i) mine += sequence_at(a, i).units();
+  for (int i = seq0; i < seq1; ++i) mine += sequence_at(a, i).units(a.most_subs);
   int64_t before = wave_sum_up_to(mine);
   if (lane == 63) wave_units[wave] = before;
   if (threadIdx.x == 0) start_seq = -1;
@@ -182,7 +192,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
     int64_t at = first - before;
     int i = seq0;
     while (true) {
-      const int64_t u = sequence_at(a, i).units();
+      const int64_t u = sequence_at(a, i).units(a.most_subs);
       if (at < u) break;
       at -= u;
       ++i;
@@ -202,7 +212,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
   for (int64_t unit = first; unit < last;) {
     Sequence s = sequence_at(a, seq);
     s = Sequence{uniform(s.len), uniform(s.rows), uniform(s.first_row)};
-    if (s.rows == 0 || in_seq >= s.units()) {
+    if (s.rows == 0 || in_seq >= s.units(a.most_subs)) {
       ++seq;
       in_seq = 0;
       continue;
@@ -211,24 +221,25 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
     const int row_block = (int)(in_seq / key_blocks), block0 = (int)(in_seq - (int64_t)row_block * key_blocks);
     const int block1 = (int)min((int64_t)key_blocks, block0 + (last - unit));
     // rows of this lane's column
-    const int row = row_block * kRows + col;
+    // Waves: `part` of the dimensions, `sub` of the block's rows, and `team`, which takes every teams-th tile.  (Waves of one team load the same tile at about the same time, so that it
+    // comes from memory once.)
+    const int subs = s.subs(a.most_subs), sub = wave / kParts % subs, team = wave / kParts / subs, teams = kWaves / kParts / subs;
+    const int row0 = min((row_block * subs + sub) * kRows, s.rows - 1);
+    const int row = (row_block * subs + sub) * kRows + col;
     const bool live = row < s.rows;
     const int token = a.by_group(min(row, s.rows - 1)), q_row = s.first_row + token, q_head = head * a.group + min(row, s.rows - 1) - token * a.group;
     const int tokens = s.rows / a.group;
     const int seen = s.len - tokens + token + 1;  // keys that the row sees (none if <= 0)
-    const int first_seen = s.len - tokens + a.by_group(row_block * kRows) + 1;                               // of the block's first row,
-    const int most_seen = max(0, s.len - tokens + a.by_group(min(row_block * kRows + kRows, s.rows) - 1) + 1);  // and of its last
+    const int first_seen = s.len - tokens + a.by_group(row0) + 1;                               // of the first row,
+    const int most_seen = max(0, s.len - tokens + a.by_group(min(row0 + kRows, s.rows) - 1) + 1);  // and of the last
     // operand B of K Q^T, to LDS in the order in which the lanes read it: in step 2 t + u, half h has dimensions 32 t + 16 h + 8 u .. + 7 (in registers it would leave too few
     // for the loads ahead)
     {
       const __bf16* const p = a.q + (int64_t)q_row * a.q_stride + (int64_t)q_head * D + 16 * half;
-#pragma unroll
-      for (int i = 0; i < (D / 16 + kWaves - 1) / kWaves; ++i) {
-        const int n = i * kWaves + wave;
-        if (n < D / 16) {
-          const Loose8 x = *reinterpret_cast<const Loose8*>(p + (n >> 1) * 32 + (n & 1) * 8);
-          q[n][lane] = live ? __builtin_bit_cast(bf16x8, x) : bf16x8{};
-        }
+      // (the waves of a sub share the work)
+      for (int n = team * kParts + part; n < D / 16; n += teams * kParts) {
+        const Loose8 x = *reinterpret_cast<const Loose8*>(p + (n >> 1) * 32 + (n & 1) * 8);
+        q[sub][n][lane] = live ? __builtin_bit_cast(bf16x8, x) : bf16x8{};
       }
     }
     __syncthreads();
@@ -238,8 +249,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
     // ---- the walk ----
     const int tile1 = min(block1 * kWaves, (int)(((unsigned)most_seen + kTile - 1) / kTile));
     const int32_t* const pages = a.table + (int64_t)seq * a.max_pages;
-    u32x4 kr[kDims * kBytes], vr[kVChunks];
-    Place<HALVES> at, next;
+    u32x4 kr[kAhead][kDims * kBytes], vr[kAhead][kVChunks];
+    Place<HALVES> places[kAhead], next;
     auto find = [&](int tile) {
       Place<HALVES> r;
       if constexpr (HALVES) {
@@ -257,7 +268,9 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
       return r;
     };
     // Starts the loads of a tile; afterwards at.there says which of its keys there are.
-    auto load_tile = [&]() {
+    auto load_tile = [&](auto slot) {
+      constexpr int S = decltype(slot)::value;
+      Place<HALVES>& at = places[S];
       if constexpr (HALVES) {
         int rows[2];
         bool ok[2];
@@ -272,14 +285,14 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
 #pragma unroll
         for (int t = 0; t < kDims; ++t)
 #pragma unroll
-          for (int u = 0; u < kBytes; ++u) kr[t * kBytes + u] = load16(p + t * (32 * kBytes) + u * 16);
+          for (int u = 0; u < kBytes; ++u) kr[S][t * kBytes + u] = load16(p + t * (32 * kBytes) + u * 16);
         const char* const from[2] = {v_base + (int64_t)rows[0] * kRowBytes, v_base + (int64_t)rows[1] * kRowBytes};
 #pragma unroll
         for (int n = 0; n < kVChunks; ++n) {
           // (where a wave's loads are whole rows, the n-th is of one half)
           const Chunk c(lane, n);
-          if constexpr (kEven && kRowsApart <= 16) vr[n] = load16(from[n * kRowsApart / 16] + (unsigned)(lane / kRowChunks * kRowBytes + c.in_row * 16) + (n * kRowsApart % 16) * kRowBytes);
-          else vr[n] = load16((c.row & 16 ? from[1] : from[0]) + (c.row & 15) * kRowBytes + c.in_row * 16);
+          if constexpr (kEven && kRowsApart <= 16) vr[S][n] = load16(from[n * kRowsApart / 16] + (unsigned)(lane / kRowChunks * kRowBytes + c.in_row * 16) + (n * kRowsApart % 16) * kRowBytes);
+          else vr[S][n] = load16((c.row & 16 ? from[1] : from[0]) + (c.row & 15) * kRowBytes + c.in_row * 16);
         }
       } else {
         const bool ok = at.number >= 0 && at.number < a.num_pages;
@@ -289,21 +302,26 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
 #pragma unroll
         for (int t = 0; t < kDims; ++t)
 #pragma unroll
-          for (int u = 0; u < kBytes; ++u) kr[t * kBytes + u] = load16(p + t * (32 * kBytes) + u * 16);
+          for (int u = 0; u < kBytes; ++u) kr[S][t * kBytes + u] = load16(p + t * (32 * kBytes) + u * 16);
 #pragma unroll
         for (int n = 0; n < kVChunks; ++n) {
           const Chunk c(lane, n);
-          vr[n] = load16(v_base + (int64_t)__shfl(row, c.row) * kRowBytes + c.in_row * 16);
+          vr[S][n] = load16(v_base + (int64_t)__shfl(row, c.row) * kRowBytes + c.in_row * 16);
         }
       }
     };
     __bf16* const v_tile = tiles[wave];
     int tile = block0 * kWaves + team;
-    at = find(tile);
-    next = find(tile + kTeams);
-    load_tile();
-    // (teams of two waves: all of them go on to the last tile of any, as they wait for each other)
-    for (; kParts == 1 ? tile < tile1 : tile - team < tile1; tile += kTeams) {
+    static_for<0, kAhead>([&](auto slot) {
+      places[decltype(slot)::value] = find(tile + decltype(slot)::value * teams);
+      load_tile(slot);
+    });
+    next = find(tile + kAhead * teams);
+    // (waves that share a tile's dimensions all go on to the last tile of any, as they wait for each other)
+    auto more = [&]() { return kParts == 1 ? tile < tile1 : tile - team < tile1; };
+    auto step = [&](auto slot) {
+      constexpr int S = decltype(slot)::value;
+      Place<HALVES>& at = places[S];
       // bit k: key k of the tile is there and seen by a row of the block; is seen by this lane's row
       const unsigned keys = at.there & first_bits(most_seen - tile * kTile), visible = at.there & first_bits(seen - tile * kTile);
       const bool border = (tile + 1) * kTile > first_seen || at.there != 0xffffffffu;
@@ -317,8 +335,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
           const int row = kEven ? n * kRowsApart : Chunk(lane, n).row;  // (less first_row)
           const bool there = mine & (1u << row);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) vr[n][e] = there ? vr[n][e] : 0;
-          odd |= some_not_finite<E4M3>(vr[n]) ? 1u << row : 0u;
+          for (int e = 0; e < 4; ++e) vr[S][n][e] = there ? vr[S][n][e] : 0;
+          odd |= some_not_finite<E4M3>(vr[S][n]) ? 1u << row : 0u;
         }
         odd <<= first_row;
       }
@@ -326,10 +344,10 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
       for (int n = 0; n < kVChunks; ++n) {
         __bf16* const to = v_tile + Chunk(lane, n).in_lds;
         if constexpr (E4M3) {
-          *reinterpret_cast<bf16x8*>(to) = widen8(vr[n][0], vr[n][1]);
-          *reinterpret_cast<bf16x8*>(to + 8) = widen8(vr[n][2], vr[n][3]);
+          *reinterpret_cast<bf16x8*>(to) = widen8(vr[S][n][0], vr[S][n][1]);
+          *reinterpret_cast<bf16x8*>(to + 8) = widen8(vr[S][n][2], vr[S][n][3]);
         } else {
-          *reinterpret_cast<u32x4*>(to) = vr[n];
+          *reinterpret_cast<u32x4*>(to) = vr[S][n];
         }
       }
       // scores
@@ -337,14 +355,14 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
 #pragma unroll
       for (int n = 0; n < 2 * kDims; ++n) {
         bf16x8 x;
-        if constexpr (E4M3) x = n & 1 ? widen8(kr[n >> 1][2], kr[n >> 1][3]) : widen8(kr[n >> 1][0], kr[n >> 1][1]);
-        else x = __builtin_bit_cast(bf16x8, kr[n]);
-        score = mfma32(x, q[part * 2 * kDims + n][lane], score);
+        if constexpr (E4M3) x = n & 1 ? widen8(kr[S][n >> 1][2], kr[S][n >> 1][3]) : widen8(kr[S][n >> 1][0], kr[S][n >> 1][1]);
+        else x = __builtin_bit_cast(bf16x8, kr[S][n]);
+        score = mfma32(x, q[sub][part * 2 * kDims + n][lane], score);
       }
       // the next tile, and the page of the one after it (behind the last one: loads that nobody waits for, of a row that is there)
       at = next;
-      load_tile();
-      next = find(tile + 2 * kTeams);
+      load_tile(slot);
+      next = find(tile + (kAhead + 1) * teams);
       __builtin_amdgcn_sched_barrier(0);
       if constexpr (kParts == 2) {  // the other half of the dimensions
         wg_barrier();  // (the last tile's have been read: their sums were used)
@@ -432,6 +450,14 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
           acc[t] = mfma32(v, lo, acc[t]);
         }
       }
+      tile += teams;
+    };
+    while (more()) {
+      step(std::integral_constant<int, 0>{});
+      if constexpr (kAhead == 2) {
+        if (!more()) break;
+        step(std::integral_constant<int, kAhead - 1>{});
+      }
     }
 
     // ---- the waves' results together ----
@@ -443,9 +469,11 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
     __syncthreads();  // (and no wave reads its tile any more)
     float top = kFloor, sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWaves; w += kParts) top = fmaxf(top, maxima[w][col]);
+    for (int w = 0; w < kWaves; w += kParts)
+      if (w / kParts % subs == sub) top = fmaxf(top, maxima[w][col]);
 #pragma unroll
-    for (int w = 0; w < kWaves; w += kParts) sum += sums[w][col] * __builtin_amdgcn_exp2f(maxima[w][col] - top);
+    for (int w = 0; w < kWaves; w += kParts)
+      if (w / kParts % subs == sub) sum += sums[w][col] * __builtin_amdgcn_exp2f(maxima[w][col] - top);
     const float f = __builtin_amdgcn_exp2f(m - top);
 #pragma unroll
     for (int t = 0; t < kDims; ++t)
@@ -468,10 +496,12 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
           for (int e = 0; e < 4; ++e) acc[t][4 * g + e] += x[e];
         }
     };
-    if (wave >= 2) give(wave - 2);
-    __syncthreads();
-    if (wave < 2) take(wave);
-    if constexpr (kParts == 1) {
+    if (teams >= 2) {
+      if (wave >= 2) give(wave - 2);
+      __syncthreads();
+      if (wave < 2) take(wave);
+    }
+    if (teams == 4) {
       __syncthreads();
       if (wave == 1) give(0);
       __syncthreads();
@@ -494,7 +524,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
           if (a.lse && half == 0 && part == 0) a.lse[(int64_t)q_head * a.total_q + q_row] = sum > 0.f || sum != sum ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
         }
       } else {
-        float* const into = a.parts + ((int64_t)(share * 2 + (block0 == 0)) * a.heads + head) * part_floats<D>();
+        float* const into = a.parts + (((int64_t)(share * 2 + (block0 == 0)) * a.heads + head) * a.most_subs + sub) * part_floats<D>();
         if (live) {
 #pragma unroll
           for (int t = 0; t < kDims; ++t)
@@ -530,9 +560,10 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const AttnArgs a, const 
   const int seq = a.cuts[share * kCut + kCutSeq], block = a.cuts[share * kCut + kCutBlock];
   const Sequence s = sequence_at(a, seq);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int col = at % row_groups; col < kRows && block * kRows + col < s.rows; col += row_groups) {
-    const int row = block * kRows + col, token = a.by_group(row), q_row = s.first_row + token, q_head = head * a.group + row - token * a.group;
-    auto part_of = [&](int i) { return a.parts + ((int64_t)((share + i) * 2 + (i == 0)) * a.heads + head) * part_floats<D>(); };
+  const int rows = kRows * s.subs(a.most_subs);
+  for (int in_block = at % row_groups; in_block < rows && block * rows + in_block < s.rows; in_block += row_groups) {
+    const int row = block * rows + in_block, col = in_block % kRows, token = a.by_group(row), q_row = s.first_row + token, q_head = head * a.group + row - token * a.group;
+    auto part_of = [&](int i) { return a.parts + (((int64_t)((share + i) * 2 + (i == 0)) * a.heads + head) * a.most_subs + in_block / kRows) * part_floats<D>(); };
     float m = kFloor;
     for (int i = wave; i < n; i += kWaves) m = fmaxf(m, part_of(i)[kRows * D + col]);
     float l = 0.f, acc[kPer] = {};
@@ -592,7 +623,11 @@ int count_shares(const paged_attn_desc* d) {
   const int64_t fill = (2 * kCus + d->num_kv_heads - 1) / d->num_kv_heads;
   return (int)std::max<int64_t>(1, std::min<int64_t>(fill, (blocks + kLeastShare - 1) / kLeastShare));
 }
-size_t part_bytes(const paged_attn_desc* d) { return (size_t)count_shares(d) * 2 * d->num_kv_heads * kRows * (d->head_dim + 2) * sizeof(float); }
+int count_subs(const paged_attn_desc* d) {
+  const int64_t rows = (int64_t)d->total_q * (d->num_q_heads / d->num_kv_heads);
+  return d->head_dim == 256 || rows <= kRows ? 1 : rows <= 2 * kRows ? 2 : 4;
+}
+size_t part_bytes(const paged_attn_desc* d) { return (size_t)count_shares(d) * count_subs(d) * 2 * d->num_kv_heads * kRows * (d->head_dim + 2) * sizeof(float); }
 size_t need_bytes(const paged_attn_desc* d) { return part_bytes(d) + (size_t)count_shares(d) * kCut * sizeof(int32_t); }
 bool aligned(const void* p, uintptr_t to) { return p && ((uintptr_t)p & (to - 1)) == 0; }
 
@@ -634,7 +669,7 @@ extern "C" int paged_attn_fwd(const paged_attn_desc* d, const void* q, int64_t q
   if (workspace_bytes < need_bytes(d)) return CHUNK_ATTN_WORKSPACE_TOO_SMALL;
   const int heads = d->num_kv_heads, group = d->num_q_heads / heads, shares = count_shares(d);
   const AttnArgs a{(const __bf16*)q, q_stride, k_cache, v_cache, e4m3 ? k_scale : nullptr, e4m3 ? v_scale : nullptr, table, kv_len, q_start, (__bf16*)o, o_stride, lse,
-                   (float*)workspace, (int32_t*)((char*)workspace + part_bytes(d)), d->num_seqs, d->total_q, heads, group, d->page_size, d->num_pages, d->max_pages, shares,
+                   (float*)workspace, (int32_t*)((char*)workspace + part_bytes(d)), d->num_seqs, d->total_q, heads, group, d->page_size, d->num_pages, d->max_pages, shares, count_subs(d),
                    d->softmax_scale * kLog2e, Divide(d->page_size), Divide(group)};
   const hipStream_t stream = (hipStream_t)hip_stream;
   const hipError_t e = by_dim(d->head_dim, [&](auto dim) {
@@ -650,7 +685,7 @@ extern "C" int paged_attn_fwd(const paged_attn_desc* d, const void* q, int64_t q
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || shares == 1) return e;
     // rows of a block that is cut: one to a workgroup, as long as that makes no more than 4096 of them
-    const int most = (int)std::min<int64_t>(kRows, (int64_t)d->total_q * group);
+    const int most = (int)std::min<int64_t>(kRows * count_subs(d), (int64_t)d->total_q * group);
     const int row_groups = std::max(1, std::min(most, 4096 / (shares * heads)));
     hipLaunchKernelGGL((join_kernel<D>), dim3((unsigned)(shares * heads * row_groups)), dim3(kThreads), 0, stream, a, row_groups);
     return hipGetLastError();

@@ -86,6 +86,9 @@ CASES = [
     ("drafts", LENS, [3, 1, 5, 3, 0, 9, 2, 8, 4, 5, 7], 32, 1, 96, 32), ("drafts", LENS, [3, 1, 5, 3, 0, 9, 2, 8, 4, 5, 7], 12, 4, 256, 1),
     # long ones, cut into shares; many short ones
     ("long", [5000], [1], 4, 1, 128, 16), ("long", [20000, 3, 777], [2, 1, 5], 4, 1, 64, 128), ("long", [9001, 12000], [6, 1], 8, 2, 256, 48), ("long", [7000], [8], 8, 1, 96, 33),
+    # cut, with two, three and more blocks of 32 rows
+    ("long", [5000], [10], 8, 2, 128, 16), ("long", [6000, 10], [9, 1], 32, 4, 64, 32), ("long", [3500], [21], 16, 2, 128, 64), ("long", [2000, 1500], [12, 17], 8, 1, 96, 20),
+    ("long", [4000], [11], 8, 2, 256, 16),
     ("many", [(i * 37) % 150 for i in range(700)], [(i * 37) % 150 and 1 + i % 2 for i in range(700)], 8, 4, 64, 16), ("a_prompt", [260], [260], 4, 2, 128, 16),
 ]
 
