@@ -22,13 +22,19 @@
 namespace chunk_attn {
 namespace {
 
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr int kRows = 32;               // rows of a block
 constexpr int kTile = 32;               // keys of a tile
 constexpr int kBlockKeys = kTile * kWaves;
 constexpr int kLeastShare = 2;          // units of a share, at least
+constexpr int kMostShares = 2 * kCus;     // of a head
 constexpr float kFloor = -3e38f;        // of a running maximum: what is masked (-inf) stays below it, so that no difference of two infinities is formed
-constexpr float kGrowth = 8.f;            // log2
+// Weights are 2^(score - m) for an m that the largest score may exceed by kGrowth before it moves, to kBelow below that score (log2): weights that go into products as float16 (e4m3 values) then stay
+// under 2^15, and what is flushed to zero is below 2^-32 of the largest.
+constexpr float kGrowth = 15.f, kBelow = 7.f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct AttnArgs {
@@ -41,13 +47,14 @@ struct AttnArgs {
   int64_t o_stride;
   float* lse;
   float* parts;   // two of each (share, head): the block of rows that came from the share before, and the one that goes on in the next
-  int32_t* cuts;  // [shares][kCut]: the block of rows that goes on in the next share
+  int32_t* cuts;  // [shares][kCut]: the block of rows that begins in the share and goes on in the next
   int32_t num_seqs, total_q, heads, group, page_size, num_pages, max_pages, shares;
   int32_t most_subs;  // groups of rows that walk over the keys together, at most
   float scale_log2;
   Divide by_page, by_group;
 };
-enum { kCutSeq, kCutBlock, kCutShares, kCut = 4 };  // sequence, block of rows, shares that it reaches into (0: none)
+// First row of q of its sequence, its first row of the sequence's, how many rows, and in how many shares it lies.
+enum { kCutSeqRow, kCutRow, kCutRows, kCutShares, kCut };
 
 // Head dimension 256: a tile takes two waves, and LDS has no room for the queries of more groups.
 template <int D>
@@ -106,6 +113,17 @@ __device__ __forceinline__ bf16x8 widen8(unsigned a, unsigned b) {
   }
   return r;
 }
+// The same as float16, which has them all too, and weights to go with them in one term: half a step is 2^-11.
+__device__ __forceinline__ f16x8 widen8_f16(unsigned a, unsigned b) {
+  f16x8 r;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const f16x2 x = w & 1 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w & 2 ? b : a, 1.f, true) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w & 2 ? b : a, 1.f, false);
+    r[2 * w] = x[0];
+    r[2 * w + 1] = x[1];
+  }
+  return r;
+}
 // Whether one of the numbers in 16 bytes of the cache is infinite or none.
 template <bool E4M3>
 __device__ __forceinline__ bool some_not_finite(u32x4 x) {
@@ -145,6 +163,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
   constexpr int kPitch = v_pitch<kOwn>() / 2;           // elements
   constexpr int kRowBytes = D * kBytes, kOwnBytes = kOwn * kBytes;
   constexpr int kRowChunks = kOwnBytes / 16, kVChunks = kRowChunks / 2;  // 16-byte chunks of a wave's part of a row; of a tile, for each lane
+  using Value = std::conditional_t<E4M3, _Float16, __bf16>;  // of V in LDS
   constexpr int kAhead = E4M3 ? 2 : 1;                  // tiles that are loaded ahead
   constexpr bool kEven = 64 % kRowChunks == 0;          // a wave's 16-byte loads are whole rows
   constexpr int kRowsApart = kEven ? 64 / kRowChunks : 0;
@@ -164,6 +183,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
   __shared__ int64_t wave_units[kWaves];
   __shared__ int64_t start_unit;
   __shared__ int start_seq;
+  __shared__ Sequence in_lds[kThreads];  // where there are no more than threads
   static_assert(sizeof(tiles) >= 2 * kRows * kOwn * 4, "two waves' values find room");
 
   const int head = blockIdx.x % a.heads, share = blockIdx.x / a.heads;
@@ -174,7 +194,11 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
   const int each = (a.num_seqs + kThreads - 1) / kThreads;
   const int seq0 = min((int)threadIdx.x * each, a.num_seqs), seq1 = min(seq0 + each, a.num_seqs);
   int64_t mine = 0;
-  for (int i = seq0; i < seq1; ++i) mine += sequence_at(a, i).units(a.most_subs);
+  for (int i = seq0; i < seq1; ++i) {
+    const Sequence s = sequence_at(a, i);
+    if (each == 1) in_lds[i] = s;
+    mine += s.units(a.most_subs);
+  }
   int64_t before = wave_sum_up_to(mine);
   if (lane == 63) wave_units[wave] = before;
   if (threadIdx.x == 0) start_seq = -1;
@@ -191,7 +215,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
   if (first >= before && first < before + mine) {
     int64_t at = first - before;
     int i = seq0;
-    while (true) {
+    while (each > 1) {
       const int64_t u = sequence_at(a, i).units(a.most_subs);
       if (at < u) break;
       at -= u;
@@ -202,7 +226,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
   }
   __syncthreads();
   int seq = uniform(start_seq);
-  if (threadIdx.x == 0 && head == 0) a.cuts[share * kCut + kCutShares] = 0;
+  if (threadIdx.x == 0 && head == 0) a.cuts[share * kCut + kCutRows] = 0;
   if (seq < 0 || first >= total) return;
   int64_t in_seq = uniform64(start_unit);  // units of the sequence before the next
   const float k_scale = E4M3 ? a.k_scale[head] : 1.f, v_scale = E4M3 ? a.v_scale[head] : 1.f;
@@ -210,7 +234,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
   const char *const k_base = (const char*)a.k + part * kOwnBytes, *const v_base = (const char*)a.v + part * kOwnBytes;
 
   for (int64_t unit = first; unit < last;) {
-    Sequence s = sequence_at(a, seq);
+    Sequence s = each == 1 ? in_lds[seq] : sequence_at(a, seq);
     s = Sequence{uniform(s.len), uniform(s.rows), uniform(s.first_row)};
     if (s.rows == 0 || in_seq >= s.units(a.most_subs)) {
       ++seq;
@@ -232,17 +256,15 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
     const int seen = s.len - tokens + token + 1;  // keys that the row sees (none if <= 0)
     const int first_seen = s.len - tokens + a.by_group(row0) + 1;                               // of the first row,
     const int most_seen = max(0, s.len - tokens + a.by_group(min(row0 + kRows, s.rows) - 1) + 1);  // and of the last
-    // operand B of K Q^T, to LDS in the order in which the lanes read it: in step 2 t + u, half h has dimensions 32 t + 16 h + 8 u .. + 7 (in registers it would leave too few
-    // for the loads ahead)
-    {
-      const __bf16* const p = a.q + (int64_t)q_row * a.q_stride + (int64_t)q_head * D + 16 * half;
-      // (the waves of a sub share the work)
-      for (int n = team * kParts + part; n < D / 16; n += teams * kParts) {
-        const Loose8 x = *reinterpret_cast<const Loose8*>(p + (n >> 1) * 32 + (n & 1) * 8);
-        q[sub][n][lane] = live ? __builtin_bit_cast(bf16x8, x) : bf16x8{};
-      }
+    // operand B of K Q^T: in step 2 t + u, half h has dimensions 32 t + 16 h + 8 u .. + 7; the waves of a sub share the loads
+    constexpr int kLoads = D / 16 / (kSubs == 1 ? kWaves : 1);  // at most
+    bf16x8 own_q[kLoads];
+    const int sharers = teams * kParts, first_q = team * kParts + part;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int n = i * sharers + first_q;
+      if (n < D / 16) own_q[i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const Loose8*>(a.q + (int64_t)q_row * a.q_stride + (int64_t)q_head * D + 16 * half + (n >> 1) * 32 + (n & 1) * 8));
     }
-    __syncthreads();
     f32x16 acc[kDims] = {};
     float m = kFloor, l = 0.f;
 
@@ -317,6 +339,12 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
       load_tile(slot);
     });
     next = find(tile + kAhead * teams);
+    // queries to LDS, in the order in which the lanes read them (in registers they would leave too few for the loads ahead); the tiles' loads go on
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i)
+      if (i * sharers + first_q < D / 16) q[sub][i * sharers + first_q][lane] = live ? own_q[i] : bf16x8{};
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+    wg_barrier();
     // (waves that share a tile's dimensions all go on to the last tile of any, as they wait for each other)
     auto more = [&]() { return kParts == 1 ? tile < tile1 : tile - team < tile1; };
     auto step = [&](auto slot) {
@@ -344,8 +372,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
       for (int n = 0; n < kVChunks; ++n) {
         __bf16* const to = v_tile + Chunk(lane, n).in_lds;
         if constexpr (E4M3) {
-          *reinterpret_cast<bf16x8*>(to) = widen8(vr[S][n][0], vr[S][n][1]);
-          *reinterpret_cast<bf16x8*>(to + 8) = widen8(vr[S][n][2], vr[S][n][3]);
+          *reinterpret_cast<f16x8*>(to) = widen8_f16(vr[S][n][0], vr[S][n][1]);
+          *reinterpret_cast<f16x8*>(to + 8) = widen8_f16(vr[S][n][2], vr[S][n][3]);
         } else {
           *reinterpret_cast<u32x4*>(to) = vr[S][n];
         }
@@ -386,15 +414,15 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
       float top = score[0];
 #pragma unroll
       for (int e = 1; e < 16; ++e) top = fmaxf(top, score[e]);
-      top = fmaxf(m, max_halves(top) * scale);
+      top = max_halves(top) * scale;
       if (__any(top > m + kGrowth)) {
-        const float f = __builtin_amdgcn_exp2f(m - top);
+        const float to = fmaxf(m, top - kBelow), f = __builtin_amdgcn_exp2f(m - to);
         l *= f;
 #pragma unroll
         for (int t = 0; t < kDims; ++t)
 #pragma unroll
           for (int e = 0; e < 16; ++e) acc[t][e] *= f;
-        m = top;
+        m = to;
       }
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
@@ -418,26 +446,30 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
           for (int t = 0; t < kDims; ++t)
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-              const bf16x4 x = *reinterpret_cast<const bf16x4*>(v_tile + key * kPitch + 32 * t + 8 * g + 4 * half);
+              const Value* const x = (const Value*)v_tile + key * kPitch + 32 * t + 8 * g + 4 * half;
 #pragma unroll
-              for (int e = 0; e < 4; ++e)
-                acc[t][4 * g + e] += sees && !(fabsf((float)x[e]) < INFINITY) ? weight * (float)x[e] : 0.f;
+              for (int e = 0; e < 4; ++e) acc[t][4 * g + e] += sees && !(fabsf((float)x[e]) < INFINITY) ? weight * (float)x[e] : 0.f;
               __builtin_amdgcn_sched_barrier(0);
             }
           __builtin_amdgcn_wave_barrier();
           for (int i = lane; i < kOwn; i += 64)
-            if (!(fabsf((float)v_tile[key * kPitch + i]) < INFINITY)) v_tile[key * kPitch + i] = (__bf16)0.f;
+            if (!(fabsf((float)((Value*)v_tile)[key * kPitch + i]) < INFINITY)) ((Value*)v_tile)[key * kPitch + i] = (Value)0.f;
           __builtin_amdgcn_wave_barrier();
         }
       }
-      // weights as two terms, the values' sums
+      // the values' sums: weights as two bf16 terms, or one of float16
 #pragma unroll
       for (int st = 0; st < 2; ++st) {
         bf16x8 hi, lo;
+        f16x8 one;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          hi[e] = (__bf16)score[8 * st + e];
-          lo[e] = (__bf16)(score[8 * st + e] - (float)hi[e]);
+          if constexpr (E4M3) {
+            one[e] = (_Float16)score[8 * st + e];
+          } else {
+            hi[e] = (__bf16)score[8 * st + e];
+            lo[e] = (__bf16)(score[8 * st + e] - (float)hi[e]);
+          }
         }
         __builtin_amdgcn_sched_barrier(0);
         // lanes 4 e + c of a group of 16 address dimensions 4 c .. 4 c + 3 of its key e
@@ -445,9 +477,13 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
 #pragma unroll
         for (int t = 0; t < kDims; ++t) {
           const s16x4 x = lds_read_tr(from + 32 * t), y = lds_read_tr(from + 32 * t + 8 * kPitch);
-          const bf16x8 v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
-          acc[t] = mfma32(v, hi, acc[t]);
-          acc[t] = mfma32(v, lo, acc[t]);
+          const s16x8 v = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+          if constexpr (E4M3) {
+            acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, v), one, acc[t], 0, 0, 0);
+          } else {
+            acc[t] = mfma32(__builtin_bit_cast(bf16x8, v), hi, acc[t]);
+            acc[t] = mfma32(__builtin_bit_cast(bf16x8, v), lo, acc[t]);
+          }
         }
       }
       tile += teams;
@@ -537,8 +573,10 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
           }
         }
         if (lane == 0 && wave == 0 && head == 0 && block0 == 0) {
-          a.cuts[share * kCut + kCutSeq] = seq;
-          a.cuts[share * kCut + kCutBlock] = row_block;
+          const int row = row_block * subs * kRows;
+          a.cuts[share * kCut + kCutSeqRow] = s.first_row;
+          a.cuts[share * kCut + kCutRow] = row;
+          a.cuts[share * kCut + kCutRows] = min(subs * kRows, s.rows - row);
           a.cuts[share * kCut + kCutShares] = (int)((unit + key_blocks - 1) / size) - share + 1;
         }
       }
@@ -549,54 +587,93 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
   }
 }
 
-// Blocks of rows that were cut: the parts of one row, in the order of the keys, joined by a workgroup (each wave takes every fourth part).
+// Blocks of rows that were cut.  All their rows are dealt to the workgroups of a head; the parts of a row, in the order of the keys, are joined by a workgroup.
 template <int D>
-__global__ __launch_bounds__(kThreads) void join_kernel(const AttnArgs a, const int row_groups) {
+__global__ __launch_bounds__(kThreads) void join_kernel(const AttnArgs a, const int groups) {
   constexpr int kPer = (D + 63) / 64;
-  __shared__ float tops[kWaves], sums[kWaves], values[kWaves][D];
-  const int head = blockIdx.x % a.heads, at = blockIdx.x / a.heads, share = at / row_groups;
-  const int n = a.cuts[share * kCut + kCutShares];
-  if (n <= 1) return;
-  const int seq = a.cuts[share * kCut + kCutSeq], block = a.cuts[share * kCut + kCutBlock];
-  const Sequence s = sequence_at(a, seq);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int rows = kRows * s.subs(a.most_subs);
-  for (int in_block = at % row_groups; in_block < rows && block * rows + in_block < s.rows; in_block += row_groups) {
-    const int row = block * rows + in_block, col = in_block % kRows, token = a.by_group(row), q_row = s.first_row + token, q_head = head * a.group + row - token * a.group;
+  __shared__ float factors[kMostShares], reduced[2][kWaves], values[kWaves][D];
+  __shared__ int wave_rows[kWaves], found, in_found;
+  const int head = blockIdx.x % a.heads, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  constexpr int kEach = kMostShares / kThreads;
+  int rows[kEach], mine = 0;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int share = threadIdx.x * kEach + i;
+    rows[i] = share < a.shares ? a.cuts[share * kCut + kCutRows] : 0;
+    mine += rows[i];
+  }
+  int up_to = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(up_to, o);
+    if (lane >= o) up_to += y;
+  }
+  if (lane == 63) wave_rows[wave] = up_to;
+  __syncthreads();
+  int before = up_to - mine, total = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < wave) before += wave_rows[w];
+    total += wave_rows[w];
+  }
+  for (int job = blockIdx.x / a.heads; job < total; job += groups) {
+    {
+      int at = before;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        if (job >= at && job < at + rows[i]) {
+          found = threadIdx.x * kEach + i;
+          in_found = job - at;
+        }
+        at += rows[i];
+      }
+    }
+    __syncthreads();
+    const int share = found, in_block = in_found;
+    const int n = a.cuts[share * kCut + kCutShares], row = a.cuts[share * kCut + kCutRow] + in_block;
+    const int token = a.by_group(row), q_row = a.cuts[share * kCut + kCutSeqRow] + token, q_head = head * a.group + row - token * a.group, col = in_block % kRows;
     auto part_of = [&](int i) { return a.parts + (((int64_t)((share + i) * 2 + (i == 0)) * a.heads + head) * a.most_subs + in_block / kRows) * part_floats<D>(); };
-    float m = kFloor;
-    for (int i = wave; i < n; i += kWaves) m = fmaxf(m, part_of(i)[kRows * D + col]);
-    float l = 0.f, acc[kPer] = {};
-#pragma unroll 4
+    float ms[kEach], ls[kEach], top = kFloor;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int piece = threadIdx.x + i * kThreads;
+      ms[i] = piece < n ? part_of(piece)[kRows * D + col] : kFloor;
+      ls[i] = piece < n ? part_of(piece)[kRows * D + kRows + col] : 0.f;
+      top = fmaxf(top, ms[i]);
+    }
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+    if (lane == 0) reduced[0][wave] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(reduced[0][0], reduced[0][1]), fmaxf(reduced[0][2], reduced[0][3]));
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const float f = __builtin_amdgcn_exp2f(ms[i] - top);
+      factors[threadIdx.x + i * kThreads] = f;
+      sum += ls[i] * f;
+    }
+    sum = lanes_sum<64>(sum);
+    if (lane == 0) reduced[1][wave] = sum;
+    __syncthreads();
+    sum = (reduced[1][0] + reduced[1][1]) + (reduced[1][2] + reduced[1][3]);
+    float acc[kPer] = {};
+#pragma unroll 8
     for (int i = wave; i < n; i += kWaves) {
-      const float* const p = part_of(i);
-      const float f = __builtin_amdgcn_exp2f(p[kRows * D + col] - m);
-      l += p[kRows * D + kRows + col] * f;
+      const float* const p = part_of(i) + col * D;
+      const float f = factors[i];
 #pragma unroll
       for (int e = 0; e < kPer; ++e)
-        if (e * 64 + lane < D) acc[e] += p[col * D + e * 64 + lane] * f;
-    }
-    if (lane == 0) {
-      tops[wave] = m;
-      sums[wave] = l;
+        if (D % 64 == 0 || e * 64 + lane < D) acc[e] += p[e * 64 + lane] * f;
     }
 #pragma unroll
     for (int e = 0; e < kPer; ++e)
-      if (e * 64 + lane < D) values[wave][e * 64 + lane] = acc[e];
+      if (D % 64 == 0 || e * 64 + lane < D) values[wave][e * 64 + lane] = acc[e];
     __syncthreads();
-    float top = kFloor, sum = 0.f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, tops[w]);
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) sum += sums[w] * __builtin_amdgcn_exp2f(tops[w] - top);
     const bool some = sum > 0.f || sum != sum;
     const float inv = some ? (a.v_scale ? a.v_scale[head] : 1.f) / sum : 0.f;
-    for (int i = threadIdx.x; i < D; i += kThreads) {
-      float x = 0.f;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) x += values[w][i] * __builtin_amdgcn_exp2f(tops[w] - top);
-      a.o[(int64_t)q_row * a.o_stride + (int64_t)q_head * D + i] = (__bf16)(x * inv);
-    }
+    for (int i = threadIdx.x; i < D; i += kThreads)
+      a.o[(int64_t)q_row * a.o_stride + (int64_t)q_head * D + i] = (__bf16)(((values[0][i] + values[1][i]) + (values[2][i] + values[3][i])) * inv);
     if (a.lse && threadIdx.x == 0) a.lse[(int64_t)q_head * a.total_q + q_row] = some ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
     __syncthreads();
   }
@@ -620,7 +697,7 @@ int check_desc(const paged_attn_desc* d) {
 int count_shares(const paged_attn_desc* d) {
   const int64_t most_keys = (int64_t)d->max_pages * d->page_size, group = d->num_q_heads / d->num_kv_heads;
   const int64_t blocks = std::min<int64_t>((int64_t)d->num_seqs + d->total_q * group / kRows, std::max<int64_t>(d->total_q * group, 1)) * ((most_keys + kBlockKeys - 1) / kBlockKeys);
-  const int64_t fill = (2 * kCus + d->num_kv_heads - 1) / d->num_kv_heads;
+  const int64_t fill = (kMostShares + d->num_kv_heads - 1) / d->num_kv_heads;
   return (int)std::max<int64_t>(1, std::min<int64_t>(fill, (blocks + kLeastShare - 1) / kLeastShare));
 }
 int count_subs(const paged_attn_desc* d) {
@@ -684,10 +761,10 @@ extern "C" int paged_attn_fwd(const paged_attn_desc* d, const void* q, int64_t q
     else with_pages(std::false_type{});
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || shares == 1) return e;
-    // rows of a block that is cut: one to a workgroup, as long as that makes no more than 4096 of them
-    const int most = (int)std::min<int64_t>(kRows * count_subs(d), (int64_t)d->total_q * group);
-    const int row_groups = std::max(1, std::min(most, 4096 / (shares * heads)));
-    hipLaunchKernelGGL((join_kernel<D>), dim3((unsigned)(shares * heads * row_groups)), dim3(kThreads), 0, stream, a, row_groups);
+    // a workgroup for each row that may be cut, as long as that makes no more than eight of them to a compute unit
+    const int64_t rows = std::min<int64_t>((int64_t)d->total_q * group, (int64_t)(shares - 1) * kRows * a.most_subs);
+    const int groups = (int)std::max<int64_t>(1, std::min<int64_t>(rows, 8 * kCus / heads));
+    hipLaunchKernelGGL((join_kernel<D>), dim3((unsigned)(groups * heads)), dim3(kThreads), 0, stream, a, groups);
     return hipGetLastError();
   });
   return e == hipSuccess ? CHUNK_ATTN_OK : report_hip(e, "attention over a paged cache");

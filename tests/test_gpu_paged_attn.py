@@ -1,6 +1,6 @@
 """Attention over a paged cache against float64.  Tolerance: a result is rounded once (half a step of bf16, 2^-8 of it).  Before that, a score is a sum of d products in float32, off by at most
-(d + 8) 2^-24 of the sum of their sizes; the argument of an exponential, below 2^7 in size, is off by 2^-17 more, the weight's two bf16 terms by 2^-17 of it, and sums over L keys by L 2^-24 at
-most.  With e the sum of these, weights are off by the factor 1 + e, the values' sum by e times the weighted sum of their sizes, and the sum of weights that divides it by the same: 2 e."""
+(d + 8) 2^-24 of the sum of their sizes; the argument of an exponential, below 2^7 in size, is off by 2^-17 more, the weight's two bf16 terms by 2^-17 of it (with values of 8 bits, one term of float16: half a step, 2^-11), and sums over L
+keys by L 2^-24 at most.  With e the sum of these, weights are off by the factor 1 + e, the values' sum by e times the weighted sum of their sizes, and the sum of weights that divides it by the same: 2 e."""
 import numpy as np
 import pytest
 import torch
@@ -69,7 +69,8 @@ class Case:
                     assert not o[row].any() and (lse is None or np.all(lse[:, row] == -np.inf))
                     continue
                 e = (self.dim + 8) * 2.0 ** -24 * score + 2.0 ** -16 + keys * 2.0 ** -24
-                assert np.all(np.abs(o[row] - want) <= 2.0 ** -8 * np.abs(want) + 2 * e[:, None] * size), (row, float(np.abs(o[row] - want).max()))
+                term = 0.0 if self.kind == "bf16" else 2.0 ** -11
+                assert np.all(np.abs(o[row] - want) <= 2.0 ** -8 * np.abs(want) + (2 * e[:, None] + term) * size), (row, float(np.abs(o[row] - want).max()))
                 # (a float32 of the lse's size is off by 2^-24 of it)
                 assert lse is None or np.all(np.abs(lse[:, row] - want_lse) <= e + 2.0 ** -22 * np.abs(want_lse)), row
         last = self.q_start[-1]
