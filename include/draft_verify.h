@@ -7,7 +7,7 @@
  * max(0, p_a(x) - q_a(x)), or, if all are kept (a = count), from p_a(x): it is the lowest x of positive weight whose sum of weights up to and with it exceeds last_uniform * (sum of all), in float64; the
  * highest x of positive weight if none does.  Where no weight is positive it is drawn from p_a, and if nothing in p_a is positive either, it is -1.  Without draft
  * probabilities q_j is 1 at d_j and 0 elsewhere (a draft that does not draw).
- * A probability that is not finite, or a NaN, weighs nothing, and keeps no token.  A drafted token outside [0, vocab) is not kept.
+ * A probability that is not finite (or a difference of two that float32 does not hold) weighs nothing, and keeps no token.  A drafted token outside [0, vocab) is not kept.
  *
  * Tensors (DEVICE; the caller owns them):
  *   target       : row j of request r at (r * (max_drafts + 1) + j) * target_stride, vocab contiguous elements; float32 or bf16, aligned to their type

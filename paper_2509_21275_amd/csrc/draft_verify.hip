@@ -15,7 +15,7 @@ namespace chunk_attn {
 namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
-constexpr int kRun = 64 * 8, kGranule = 2 * kRun;  // a wave takes eight neighbouring weights to a lane
+constexpr int kRun = 64 * 8, kGranule = 2 * kRun;  // a wave takes eight neighbouring weights to a lane, twice
 
 template <class T>
 struct VerifyArgs {
@@ -25,10 +25,8 @@ struct VerifyArgs {
   const float *uniforms, *last_uniform;
   int32_t *accepted, *rejected, *out;
   double* sums;  // [batch][granules]
-  int32_t max_drafts, vocab, granules, each, groups;  // granules to a wave; workgroups to a request
+  int32_t max_drafts, vocab, granules, groups;  // workgroups to a request
 };
-
-__device__ __forceinline__ double weight_of(double x) { return x > 0.0 && x <= 1.7976931348623157e308 ? x : 0.0; }
 
 // The row that the last token is drawn from.
 template <class T>
@@ -36,17 +34,22 @@ struct Weights {
   const T *p, *q;  // q: null if all is drawn from p
   int without;     // a token that weighs nothing, or -1
   int vocab;
-  // Weights first .. first + 7 (behind the vocabulary: zeros).
-  __device__ void load(int first, double* w) const {
-    float x[8], y[8];
-    const int n = vocab - first;
+  // Probabilities first .. first + 7 (behind the vocabulary: zeros), such that x - y is their weight: both zero where that is not positive, or not finite.
+  // INSIDE: all of them are in the vocabulary (no branch stands between loads then).
+  template <bool INSIDE>
+  __device__ void load(int first, float* x, float* y) const {
+    const int n = INSIDE ? 8 : vocab - first;
     load_up_to_8(p + first, n, x);
-    if (q) load_up_to_8(q + first, n, y);
+    load_up_to_8((q ? q : p) + first, n, y);
+  }
+  __device__ void clear(int first, float* x, float* y) const {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      w[e] = weight_of(q ? (double)x[e] - (double)y[e] : (double)x[e]);
-      if (q && !(fabsf(x[e]) <= 3.402823466e38f && fabsf(y[e]) <= 3.402823466e38f)) w[e] = 0.0;
-      if (first + e == without) w[e] = 0.0;
+      y[e] = q ? y[e] : 0.f;
+      const float d = x[e] - y[e];  // (rounded, but of the right sign)
+      const bool some = d > 0.f && d <= 3.402823466e38f && first + e != without;
+      x[e] = some ? x[e] : 0.f;
+      y[e] = some ? y[e] : 0.f;
     }
   }
 };
@@ -80,7 +83,39 @@ __device__ __forceinline__ double wave_up_to(double x) {
   return x;
 }
 
-template <class T>
+// Sums of the granules first .. first + EACH - 1, by one wave.
+template <class T, int EACH, bool INSIDE>
+__device__ __forceinline__ void leave_sums(const VerifyArgs<T>& a, const Weights<T>& weights, int r, int first) {
+  const int lane = threadIdx.x & 63;
+  float x[EACH][2][8], y[EACH][2][8];
+#pragma unroll
+  for (int g = 0; g < EACH; ++g)
+#pragma unroll
+    for (int n = 0; n < 2; ++n) weights.template load<INSIDE>(INSIDE ? (first + g) * kGranule + n * kRun + lane * 8 : min((first + g) * kGranule + n * kRun + lane * 8, a.vocab), x[g][n], y[g][n]);
+  double sums[EACH];
+#pragma unroll
+  for (int g = 0; g < EACH; ++g) {
+    sums[g] = 0.0;
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      weights.clear((first + g) * kGranule + n * kRun + lane * 8, x[g][n], y[g][n]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        sums[g] += (double)x[g][n][e];
+        sums[g] -= (double)y[g][n][e];
+      }
+    }
+  }
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1)
+#pragma unroll
+    for (int g = 0; g < EACH; ++g) sums[g] += __shfl_xor(sums[g], o);
+#pragma unroll
+  for (int g = 0; g < EACH; ++g)
+    if (lane == 0 && first + g < a.granules) a.sums[(int64_t)r * a.granules + first + g] = sums[g];
+}
+
+template <class T, int EACH>
 __global__ __launch_bounds__(kThreads) void sums_kernel(const VerifyArgs<T> a) {
   __shared__ int kept_by_all;
   const int r = blockIdx.x / a.groups, group = blockIdx.x % a.groups, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -108,130 +143,136 @@ __global__ __launch_bounds__(kThreads) void sums_kernel(const VerifyArgs<T> a) {
   __syncthreads();
   const int kept = kept_by_all;
   const Weights<T> weights = weights_of(a, r, kept, kept < count);
-  const int first = (group * kWaves + wave) * a.each;
-  for (int g = first; g < min(first + a.each, a.granules); ++g) {
-    double sum = 0.0;
-#pragma unroll
-    for (int n = 0; n < kGranule / kRun; ++n) {
-      double w[8];
-      weights.load(g * kGranule + n * kRun + lane * 8, w);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) sum += w[e];
-    }
-    sum = wave_total(sum);
-    if (lane == 0) a.sums[(int64_t)r * a.granules + g] = sum;
-  }
+  // granules of a wave at once, so that their loads are under way together
+  const int first = (group * kWaves + wave) * EACH;
+  if (first >= a.granules) return;
+  if ((first + EACH) * kGranule <= a.vocab) leave_sums<T, EACH, true>(a, weights, r, first);
+  else leave_sums<T, EACH, false>(a, weights, r, first);
 }
 
 // One workgroup to a request.
 template <class T>
 __global__ __launch_bounds__(kThreads) void choose_kernel(const VerifyArgs<T> a) {
-  __shared__ double room[kWaves];
-  __shared__ int chosen, highest;
-  __shared__ double before_chosen;
+  __shared__ double room[kWaves], before_first[kWaves], before_last[kWaves];
+  __shared__ int first_past[kWaves], last_some[kWaves];
   const int r = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int count = count_of(a, r), kept = a.accepted[r];
   double* const sums = a.sums + (int64_t)r * a.granules;
   const int each = (a.granules + kThreads - 1) / kThreads, first = min((int)threadIdx.x * each, a.granules), last = min(first + each, a.granules);
+  // loads that depend on nothing, together
+  const int kept = a.accepted[r], count = count_of(a, r), drafted = lane < a.max_drafts ? a.tokens[(int64_t)r * a.max_drafts + lane] : -1;
+  const float uniform = a.last_uniform[r];
+  double mine = first < last ? sums[first] : 0.0;
+  for (int g = first + 1; g < last; ++g) mine += sums[g];
   Weights<T> weights = weights_of(a, r, kept, kept < count);
   double total = 0.0, before = 0.0;
   for (int again = 0;; ++again) {
-    double mine = 0.0;
-    for (int g = first; g < last; ++g) mine += sums[g];
     const double up_to = wave_up_to(mine);
     if (lane == 63) room[wave] = up_to;
     __syncthreads();
     before = up_to - mine;
     total = 0.0;
+#pragma unroll
     for (int w = 0; w < kWaves; ++w) {
       if (w < wave) before += room[w];
       total += room[w];
     }
-    __syncthreads();
     if (total > 0.0 || again || kept >= count) break;
     // the draft leaves nothing: from the target's row itself
     weights = weights_of(a, r, kept, false);
     for (int g = wave; g < a.granules; g += kWaves) {
       double sum = 0.0;
       for (int n = 0; n < kGranule / kRun; ++n) {
-        double w[8];
-        weights.load(g * kGranule + n * kRun + lane * 8, w);
-        for (int e = 0; e < 8; ++e) sum += w[e];
+        float x[8], y[8];
+        const int at = g * kGranule + n * kRun + lane * 8;
+        weights.template load<false>(min(at, a.vocab), x, y);
+        weights.clear(at, x, y);
+        for (int e = 0; e < 8; ++e) sum += (double)x[e];
       }
       sum = wave_total(sum);
       if (lane == 0) sums[g] = sum;
     }
     __syncthreads();
+    mine = 0.0;
+    for (int g = first; g < last; ++g) mine += sums[g];
   }
   // the first granule whose sum with those before it passes the share, and the highest with a weight
-  const double share = (double)a.last_uniform[r] * total;
-  if (threadIdx.x == 0) {
-    chosen = INT32_MAX;
-    highest = -1;
-  }
-  __syncthreads();
-  int mine = INT32_MAX, top = -1;
-  double at_mine = 0.0, at_top = 0.0;
-  {
-    double at = before;
-    for (int g = first; g < last; ++g) {
-      const double s = sums[g];
-      if (s > 0.0) {
-        top = g;
-        at_top = at;
-        if (mine == INT32_MAX && at + s > share) {
-          mine = g;
-          at_mine = at;
-        }
-      }
-      at += s;
-    }
-  }
-  if (mine != INT32_MAX) atomicMin(&chosen, mine);
-  if (top >= 0) atomicMax(&highest, top);
-  __syncthreads();
-  const bool passes = chosen != INT32_MAX;
-  const int granule = passes ? chosen : highest;
-  if (passes ? mine == granule : top == granule && top >= 0) before_chosen = passes ? at_mine : at_top;
-  __syncthreads();
-  if (wave == 0) {
-    int token = -1;
-    if (granule >= 0) {
-      double at = before_chosen;
-      int top_token = -1;
-      for (int n = 0; n < kGranule / kRun; ++n) {
-        double w[8], sum = 0.0;
-        const int x = granule * kGranule + n * kRun + lane * 8;
-        weights.load(x, w);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sum += w[e];
-        const double up_to = wave_up_to(sum);
-        double running = at + (up_to - sum);
-        int found = INT32_MAX;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          running += w[e];
-          if (w[e] > 0.0) {
-            top_token = x + e;
-            if (found == INT32_MAX && running > share) found = x + e;
-          }
-        }
-        at += __shfl(up_to, 63);
-        const unsigned long long who = __ballot(found != INT32_MAX);
-        if (who != 0) {
-          token = __shfl(found, __ffsll((long long)who) - 1);
-          break;
-        }
-      }
-      if (token < 0) {
-#pragma unroll
-        for (int o = 32; o >= 1; o >>= 1) top_token = max(top_token, __shfl_xor(top_token, o));
-        token = top_token;
+  const double share = (double)uniform * total;
+  int past = INT32_MAX, some = -1;
+  double at_past = 0.0, at_some = 0.0, at = before;
+  for (int g = first; g < last; ++g) {
+    const double s = each == 1 ? mine : sums[g];
+    if (s > 0.0) {
+      some = g;
+      at_some = at;
+      if (past == INT32_MAX && at + s > share) {
+        past = g;
+        at_past = at;
       }
     }
-    for (int j = lane; j <= a.max_drafts; j += 64)
-      a.out[(int64_t)r * (a.max_drafts + 1) + j] = j < kept ? a.tokens[(int64_t)r * a.max_drafts + j] : j == kept ? token : -1;
+    at += s;
   }
+  const unsigned long long who_past = __ballot(past != INT32_MAX), who_some = __ballot(some >= 0);
+  if (lane == (who_past ? __ffsll((long long)who_past) - 1 : 0)) {
+    first_past[wave] = past;
+    before_first[wave] = at_past;
+  }
+  if (lane == (who_some ? 63 - __clzll((long long)who_some) : 0)) {
+    last_some[wave] = some;
+    before_last[wave] = at_some;
+  }
+  __syncthreads();
+  if (wave != 0) return;
+  int granule = -1;
+  at = 0.0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w)
+    if (last_some[w] >= 0) {
+      granule = last_some[w];
+      at = before_last[w];
+    }
+#pragma unroll
+  for (int w = kWaves - 1; w >= 0; --w)
+    if (first_past[w] != INT32_MAX) {
+      granule = first_past[w];
+      at = before_first[w];
+    }
+  int token = -1, highest = -1;
+  if (granule >= 0) {
+    float x[2][8], y[2][8];
+#pragma unroll
+    for (int n = 0; n < 2; ++n) weights.template load<false>(min(granule * kGranule + n * kRun + lane * 8, a.vocab), x[n], y[n]);
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      const int base = granule * kGranule + n * kRun + lane * 8;
+      weights.clear(base, x[n], y[n]);
+      double sum = 0.0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum += (double)x[n][e] - (double)y[n][e];
+      const double up_to = wave_up_to(sum);
+      double running = at + (up_to - sum);
+      int found = INT32_MAX;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        running += (double)x[n][e] - (double)y[n][e];
+        if (x[n][e] > y[n][e]) {
+          highest = base + e;
+          if (found == INT32_MAX && running > share) found = base + e;
+        }
+      }
+      at += __shfl(up_to, 63);
+      const unsigned long long who = __ballot(found != INT32_MAX);
+      if (who != 0 && token < 0) token = __shfl(found, __ffsll((long long)who) - 1);
+    }
+    if (token < 0) {
+#pragma unroll
+      for (int o = 32; o >= 1; o >>= 1) highest = max(highest, __shfl_xor(highest, o));
+      token = highest;
+    }
+  }
+  // (64 drafts at most: a place for each lane, and one behind them)
+  int32_t* const out = a.out + (int64_t)r * (a.max_drafts + 1);
+  if (lane <= a.max_drafts) out[lane] = lane < kept ? drafted : lane == kept ? token : -1;
+  if (lane == 0 && a.max_drafts == 64) out[64] = kept == 64 ? token : -1;
 }
 
 int check_sizes(int32_t batch, int32_t max_drafts, int32_t vocab) {
@@ -244,10 +285,12 @@ bool aligned(const void* p, uintptr_t to) { return p && ((uintptr_t)p & (to - 1)
 template <class T>
 hipError_t launch(VerifyArgs<T> a, int batch, hipStream_t stream) {
   a.granules = count_granules(a.vocab);
-  // granules to a wave: one, or more (eight at most) where the chip is full with that
-  a.each = (int)std::max<int64_t>(1, std::min<int64_t>(8, (int64_t)batch * a.granules / (kCus * 32)));
-  a.groups = (a.granules + a.each * kWaves - 1) / (a.each * kWaves);
-  hipLaunchKernelGGL((sums_kernel<T>), dim3((unsigned)((int64_t)batch * a.groups)), dim3(kThreads), 0, stream, a);
+  // granules to a wave: one, or four where the chip is full with that
+  const bool many = (int64_t)batch * a.granules >= 4 * kCus * 16;
+  a.groups = (a.granules + (many ? 4 : 1) * kWaves - 1) / ((many ? 4 : 1) * kWaves);
+  const dim3 grid((unsigned)((int64_t)batch * a.groups));
+  if (many) hipLaunchKernelGGL((sums_kernel<T, 4>), grid, dim3(kThreads), 0, stream, a);
+  else hipLaunchKernelGGL((sums_kernel<T, 1>), grid, dim3(kThreads), 0, stream, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((choose_kernel<T>), dim3((unsigned)batch), dim3(kThreads), 0, stream, a);

@@ -29,7 +29,6 @@ constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr int kRows = 32;               // rows of a block
 constexpr int kTile = 32;               // keys of a tile
 constexpr int kBlockKeys = kTile * kWaves;
-constexpr int kLeastShare = 2;          // units of a share, at least
 constexpr int kMostShares = 2 * kCus;     // of a head
 constexpr float kFloor = -3e38f;        // of a running maximum: what is masked (-inf) stays below it, so that no difference of two infinities is formed
 // Weights are 2^(score - m) for an m that the largest score may exceed by kGrowth before it moves, to kBelow below that score (log2): weights that go into products as float16 (e4m3 values) then stay
@@ -210,7 +209,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
     if (w < wave) before += wave_units[w];
     total += wave_units[w];
   }
-  const int64_t size = uniform64(max((int64_t)kLeastShare, (total + a.shares - 1) / a.shares));
+  const int64_t size = uniform64(max((int64_t)1, (total + a.shares - 1) / a.shares));
   const int64_t first = share * size, last = uniform64(min(first + size, total));
   if (first >= before && first < before + mine) {
     int64_t at = first - before;
@@ -592,15 +591,17 @@ template <int D>
 __global__ __launch_bounds__(kThreads) void join_kernel(const AttnArgs a, const int groups) {
   constexpr int kPer = (D + 63) / 64;
   __shared__ float factors[kMostShares], reduced[2][kWaves], values[kWaves][D];
-  __shared__ int wave_rows[kWaves], found, in_found;
+  __shared__ int wave_rows[kWaves], found[kCut + 1];
   const int head = blockIdx.x % a.heads, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  constexpr int kEach = kMostShares / kThreads;
-  int rows[kEach], mine = 0;
+  constexpr int kEach = kMostShares / kThreads, kEarly = 4;
+  static_assert(kCut == 4);
+  int4 cuts[kEach];
+  int mine = 0;
 #pragma unroll
   for (int i = 0; i < kEach; ++i) {
     const int share = threadIdx.x * kEach + i;
-    rows[i] = share < a.shares ? a.cuts[share * kCut + kCutRows] : 0;
-    mine += rows[i];
+    cuts[i] = share < a.shares ? reinterpret_cast<const int4*>(a.cuts)[share] : int4{};
+    mine += cuts[i].z;
   }
   int up_to = mine;
 #pragma unroll
@@ -621,18 +622,27 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const AttnArgs a, const 
       int at = before;
 #pragma unroll
       for (int i = 0; i < kEach; ++i) {
-        if (job >= at && job < at + rows[i]) {
-          found = threadIdx.x * kEach + i;
-          in_found = job - at;
+        if (job >= at && job < at + cuts[i].z) {
+          found[kCutSeqRow] = cuts[i].x;
+          found[kCutRow] = cuts[i].y;
+          found[kCutRows] = job - at;  // (the row of the block)
+          found[kCutShares] = cuts[i].w;
+          found[kCut] = threadIdx.x * kEach + i;
         }
-        at += rows[i];
+        at += cuts[i].z;
       }
     }
     __syncthreads();
-    const int share = found, in_block = in_found;
-    const int n = a.cuts[share * kCut + kCutShares], row = a.cuts[share * kCut + kCutRow] + in_block;
-    const int token = a.by_group(row), q_row = a.cuts[share * kCut + kCutSeqRow] + token, q_head = head * a.group + row - token * a.group, col = in_block % kRows;
+    const int share = found[kCut], in_block = found[kCutRows], n = found[kCutShares], row = found[kCutRow] + in_block;
+    const int token = a.by_group(row), q_row = found[kCutSeqRow] + token, q_head = head * a.group + row - token * a.group, col = in_block % kRows;
     auto part_of = [&](int i) { return a.parts + (((int64_t)((share + i) * 2 + (i == 0)) * a.heads + head) * a.most_subs + in_block / kRows) * part_floats<D>(); };
+    float early[kEarly][kPer];  // the wave's first parts, on their way while the factors are found
+#pragma unroll
+    for (int j = 0; j < kEarly; ++j) {
+      const float* const p = part_of(min(wave + j * kWaves, n - 1)) + col * D;
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) early[j][e] = D % 64 == 0 || e * 64 + lane < D ? p[e * 64 + lane] : 0.f;
+    }
     float ms[kEach], ls[kEach], top = kFloor;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
@@ -658,8 +668,14 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const AttnArgs a, const 
     __syncthreads();
     sum = (reduced[1][0] + reduced[1][1]) + (reduced[1][2] + reduced[1][3]);
     float acc[kPer] = {};
+#pragma unroll
+    for (int j = 0; j < kEarly; ++j) {
+      const float f = wave + j * kWaves < n ? factors[wave + j * kWaves] : 0.f;
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) acc[e] += wave + j * kWaves < n ? early[j][e] * f : 0.f;
+    }
 #pragma unroll 8
-    for (int i = wave; i < n; i += kWaves) {
+    for (int i = wave + kEarly * kWaves; i < n; i += kWaves) {
       const float* const p = part_of(i) + col * D;
       const float f = factors[i];
 #pragma unroll
@@ -698,7 +714,7 @@ int count_shares(const paged_attn_desc* d) {
   const int64_t most_keys = (int64_t)d->max_pages * d->page_size, group = d->num_q_heads / d->num_kv_heads;
   const int64_t blocks = std::min<int64_t>((int64_t)d->num_seqs + d->total_q * group / kRows, std::max<int64_t>(d->total_q * group, 1)) * ((most_keys + kBlockKeys - 1) / kBlockKeys);
   const int64_t fill = (kMostShares + d->num_kv_heads - 1) / d->num_kv_heads;
-  return (int)std::max<int64_t>(1, std::min<int64_t>(fill, (blocks + kLeastShare - 1) / kLeastShare));
+  return (int)std::max<int64_t>(1, std::min<int64_t>(fill, blocks));
 }
 int count_subs(const paged_attn_desc* d) {
   const int64_t rows = (int64_t)d->total_q * (d->num_q_heads / d->num_kv_heads);

@@ -31,6 +31,7 @@ struct TableArgs {
   int32_t max_rows;
   // workspace: what the second launch goes by
   int32_t* sums;  // [kSums][n] and the totals behind them
+  Divide by_page{1};
 };
 // Of each request: pages before it, tokens before the call (extend: -1 if it is not served), pages that it had (truncate: that it keeps).
 enum { kPagesBefore, kOldLen, kHeld, kSums };
@@ -63,24 +64,29 @@ struct Request {
   int old_len, held, change, len, need;  // need: pages that it takes (extend, if it is served) or gives (truncate)
   bool fits;
 };
+__device__ __forceinline__ int pages_of(const TableArgs& a, int len) { return len > 0 ? a.by_page(len - 1) + 1 : 0; }
 template <bool EXTEND>
-__device__ __forceinline__ Request request_at(const TableArgs& a, int i) {
+__device__ __forceinline__ Request request_of(const TableArgs& a, int change, int kv_len, int held) {
   const int64_t most = (int64_t)a.max_pages * a.page_size;  // < 2^31
   Request r;
-  r.old_len = at_most(max(a.kv_len[i], 0), most);
-  r.held = min(max(a.held[i], 0), a.max_pages);
-  r.change = max(a.change[i], 0);
+  r.old_len = at_most(max(kv_len, 0), most);
+  r.held = min(max(held, 0), a.max_pages);
+  r.change = max(change, 0);
   if (EXTEND) {
     const int64_t len = (int64_t)r.old_len + r.change;
     r.fits = len <= most;
     r.len = r.fits ? (int)len : r.old_len;
-    r.need = r.fits ? max(0, (int)((len + a.page_size - 1) / a.page_size) - r.held) : 0;
+    r.need = r.fits ? max(0, pages_of(a, r.len) - r.held) : 0;
   } else {
     r.fits = true;
     r.len = max(r.old_len - r.change, 0);
-    r.need = r.held - min(r.held, (int)(((int64_t)r.len + a.page_size - 1) / a.page_size));
+    r.need = r.held - min(r.held, pages_of(a, r.len));
   }
   return r;
+}
+template <bool EXTEND>
+__device__ __forceinline__ Request request_at(const TableArgs& a, int i) {
+  return request_of<EXTEND>(a, a.change[i], a.kv_len[i], a.held[i]);
 }
 
 // Last i < n with sums[i] <= x, for sums[0] = 0 <= x.
@@ -94,32 +100,57 @@ __device__ __forceinline__ int find(const int32_t* sums, int n, int x) {
   return lo;
 }
 
-// Slots of rows, from the sums.
-__device__ __forceinline__ int64_t slot_of_row(const TableArgs& a, const int32_t* q_start, const int32_t* pages_before, const int32_t* old_lens, const int32_t* helds, int on_stack, int row) {
-  if (row >= q_start[a.n]) return -1;
-  const int i = find(q_start, a.n, row);
+// Slot of a row of request i, from the sums.
+__device__ __forceinline__ int64_t slot_of_row(const TableArgs& a, const int32_t* q_start, const int32_t* pages_before, const int32_t* old_lens, const int32_t* helds, int on_stack, int row, int i) {
   if (old_lens[i] < 0) return -1;
-  const int at = old_lens[i] + row - q_start[i], b = at / a.page_size;
+  const int at = old_lens[i] + row - q_start[i], b = a.by_page(at);
   const int page = b < helds[i] ? a.table[(int64_t)i * a.max_pages + b] : a.free_pages[on_stack - 1 - (pages_before[i] + b - helds[i])];
-  return page >= 0 && page < a.num_pages ? (int64_t)page * a.page_size + at % a.page_size : -1;
+  return page >= 0 && page < a.num_pages ? (int64_t)page * a.page_size + at - b * a.page_size : -1;
 }
-// One page that changes hands.
+// One page that changes hands, of request i.
 template <bool EXTEND>
-__device__ __forceinline__ void move_page(const TableArgs& a, const int32_t* pages_before, const int32_t* helds, int on_stack, int p) {
-  const int i = find(pages_before, a.n, p);
+__device__ __forceinline__ void move_page(const TableArgs& a, const int32_t* pages_before, const int32_t* helds, int on_stack, int p, int i) {
   int32_t* const entry = a.table + (int64_t)i * a.max_pages + helds[i] + p - pages_before[i];
   if (EXTEND) *entry = a.free_pages[on_stack - 1 - p];
   else if (on_stack + p < a.num_pages) a.free_pages[on_stack + p] = *entry;
 }
 
-// IN_ONE: at most kScanThreads requests and kInOne rows; everything is done here.
-template <bool EXTEND, bool IN_ONE>
+// Loads of four neighbouring numbers, from any address that suits one.
+struct __attribute__((packed, aligned(4))) LooseInts {
+  int x[4];
+};
+
+// IN_ONE: at most kScanThreads requests and kInOne rows; everything is done here.  EACH: requests of a thread (0: any number, read again wherever they are used).
+template <bool EXTEND, bool IN_ONE, int EACH>
 __global__ __launch_bounds__(kScanThreads) void tables_kernel(const TableArgs a) {
   __shared__ int64_t room[kScanThreads / 64];
   __shared__ int32_t in_lds[IN_ONE ? kSums + 1 : 1][IN_ONE ? kScanThreads + 1 : 1];
   __shared__ int moved;
-  const int each = IN_ONE ? 1 : (a.n + kScanThreads - 1) / kScanThreads;
+  static_assert(!IN_ONE || EACH == 1);
+  const int each = EACH ? EACH : (a.n + kScanThreads - 1) / kScanThreads;
   const int first = min((int)threadIdx.x * each, a.n), last = min(first + each, a.n);
+  Request held_back[EACH ? EACH : 1];
+  if constexpr (EACH == 4) {
+    if (last == first + EACH) {
+      const LooseInts change = *reinterpret_cast<const LooseInts*>(a.change + first), kv_len = *reinterpret_cast<const LooseInts*>(a.kv_len + first), held = *reinterpret_cast<const LooseInts*>(a.held + first);
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) held_back[i] = request_of<EXTEND>(a, change.x[i], kv_len.x[i], held.x[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) held_back[i] = first + i < last ? request_at<EXTEND>(a, first + i) : Request{};
+    }
+  } else if constexpr (EACH == 1) {
+    held_back[0] = first < last ? request_at<EXTEND>(a, first) : Request{};
+  }
+  auto each_request = [&](auto&& f) {
+    if constexpr (EACH > 0) {
+#pragma unroll
+      for (int i = 0; i < EACH; ++i)
+        if (first + i < last) f(first + i, held_back[i]);
+    } else {
+      for (int i = first; i < last; ++i) f(i, request_at<EXTEND>(a, i));
+    }
+  };
   const int on_stack = min(max(*a.num_free, 0), a.num_pages);
   int32_t* const pages_before = IN_ONE ? in_lds[kPagesBefore] : a.sums + (int64_t)kPagesBefore * a.n;
   int32_t* const old_lens = IN_ONE ? in_lds[kOldLen] : a.sums + (int64_t)kOldLen * a.n;
@@ -129,20 +160,18 @@ __global__ __launch_bounds__(kScanThreads) void tables_kernel(const TableArgs a)
   // rows first: who does not fit in them has no claim on pages
   int64_t rows = 0, pages = 0;
   if (EXTEND) {
-    for (int i = first; i < last; ++i) rows += max(a.change[i], 0);
+    each_request([&](int, const Request& r) { rows += r.change; });
     rows = sum_before(rows, room);
   }
   int64_t row = rows;
-  for (int i = first; i < last; ++i) {
-    const Request r = request_at<EXTEND>(a, i);
+  each_request([&](int, const Request& r) {
     row += r.change;
     if (!EXTEND || r.change == 0 || row <= a.max_rows) pages += r.need;
-  }
+  });
   pages = sum_before(pages, room);
   row = rows;
   int mine = 0;
-  for (int i = first; i < last; ++i) {
-    const Request r = request_at<EXTEND>(a, i);
+  each_request([&](int i, const Request& r) {
     const int64_t end = row + r.change;
     const bool in_rows = !EXTEND || r.change == 0 || end <= a.max_rows;
     const int need = in_rows ? r.need : 0;
@@ -165,7 +194,7 @@ __global__ __launch_bounds__(kScanThreads) void tables_kernel(const TableArgs a)
     row = end;
     a.kv_len_out[i] = served ? r.len : r.old_len;
     a.held_out[i] = EXTEND ? r.held + (served ? need : 0) : r.held - need;
-  }
+  });
   if (mine > 0) atomicMax(&moved, mine);
   __syncthreads();
   if (threadIdx.x == 0) {
@@ -177,19 +206,63 @@ __global__ __launch_bounds__(kScanThreads) void tables_kernel(const TableArgs a)
   }
   if constexpr (IN_ONE) {
     if (EXTEND)
-      for (int r = threadIdx.x; r < a.max_rows; r += kScanThreads) a.slots[r] = slot_of_row(a, starts, pages_before, old_lens, helds, on_stack, r);
-    for (int p = threadIdx.x; p < moved; p += kScanThreads) move_page<EXTEND>(a, pages_before, helds, on_stack, p);
+      for (int r = threadIdx.x; r < a.max_rows; r += kScanThreads) a.slots[r] = r < starts[a.n] ? slot_of_row(a, starts, pages_before, old_lens, helds, on_stack, r, find(starts, a.n, r)) : -1;
+    for (int p = threadIdx.x; p < moved; p += kScanThreads) move_page<EXTEND>(a, pages_before, helds, on_stack, p, find(pages_before, a.n, p));
   }
 }
 
+// Where a workgroup's neighbouring rows (or pages) begin to be found: the last i < n with sums[i] <= x, by one wave that looks at 64 places at a time, and the sums from there on in LDS.
+constexpr int kFillThreads = 256, kWindow = 1024;
+struct Window {
+  int32_t at[kWindow];
+  int first, count;
+};
+__device__ void open_window(Window& w, const int32_t* sums, int n, int x) {
+  if (threadIdx.x < 64) {
+    int lo = 0, size = n;  // the place is in lo .. lo + size - 1
+    while (size > 1) {
+      const int step = (size + 63) / 64, i = lo + (int)threadIdx.x * step;
+      const unsigned long long up_to = __ballot(i < lo + size && sums[min(i, n - 1)] <= x);  // (sums grow: the first places)
+      const int last = 63 - __clzll((long long)up_to);
+      size = min(step, size - last * step);
+      lo += last * step;
+    }
+    if (threadIdx.x == 0) w.first = lo;
+  }
+  __syncthreads();
+  const int first = w.first, count = min(kWindow, n - first);
+  for (int i = threadIdx.x; i < count; i += kFillThreads) w.at[i] = sums[first + i];
+  if (threadIdx.x == 0) w.count = count;
+  __syncthreads();
+}
+// The same for an x that is not smaller; rows of requests that have none may lie between, so that the window need not reach it.
+__device__ __forceinline__ int find_from(const Window& w, const int32_t* sums, int n, int x) {
+  if (w.first + w.count < n && x >= w.at[w.count - 1]) return find(sums, n, x);
+  return w.first + find(w.at, w.count, x);
+}
+
 template <bool EXTEND>
-__global__ __launch_bounds__(256) void fill_kernel(const TableArgs a) {
+__global__ __launch_bounds__(kFillThreads) void fill_kernel(const TableArgs a) {
+  __shared__ Window window;
   const int32_t *const pages_before = a.sums + (int64_t)kPagesBefore * a.n, *const old_lens = a.sums + (int64_t)kOldLen * a.n, *const helds = a.sums + (int64_t)kHeld * a.n;
   const int moved = a.sums[(int64_t)kSums * a.n + kMoved], on_stack = a.sums[(int64_t)kSums * a.n + kOnStack];
-  const int64_t step = (int64_t)gridDim.x * 256, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (EXTEND)
-    for (int64_t r = at; r < a.max_rows; r += step) a.slots[r] = slot_of_row(a, a.q_start, pages_before, old_lens, helds, on_stack, (int)r);
-  for (int64_t p = at; p < moved; p += step) move_page<EXTEND>(a, pages_before, helds, on_stack, (int)p);
+  const int64_t step = (int64_t)gridDim.x * kFillThreads;
+  if (EXTEND) {
+    const int rows = a.q_start[a.n];
+    for (int64_t r0 = (int64_t)blockIdx.x * kFillThreads; r0 < a.max_rows; r0 += step) {
+      if (r0 < rows) open_window(window, a.q_start, a.n, (int)r0);
+      const int64_t r = r0 + threadIdx.x;
+      if (r < a.max_rows) a.slots[r] = r < rows ? slot_of_row(a, a.q_start, pages_before, old_lens, helds, on_stack, (int)r, find_from(window, a.q_start, a.n, (int)r)) : -1;
+      __syncthreads();
+    }
+  }
+  // (pages with the last workgroups first: those with the fewest rows)
+  for (int64_t p0 = (int64_t)(gridDim.x - 1 - blockIdx.x) * kFillThreads; p0 < moved; p0 += step) {
+    open_window(window, pages_before, a.n, (int)p0);
+    const int64_t p = p0 + threadIdx.x;
+    if (p < moved) move_page<EXTEND>(a, pages_before, helds, on_stack, (int)p, find_from(window, pages_before, a.n, (int)p));
+    __syncthreads();
+  }
 }
 
 int check_desc(const paged_cache_desc* d) {
@@ -212,23 +285,26 @@ int run_tables(const paged_cache_desc* d, TableArgs a, void* workspace, size_t w
   a.page_size = d->page_size;
   a.num_pages = d->num_pages;
   a.sums = (int32_t*)workspace;
+  a.by_page = Divide(d->page_size);
   if (a.n <= kScanThreads && a.max_rows <= kInOne) {
-    hipLaunchKernelGGL((tables_kernel<EXTEND, true>), dim3(1), dim3(kScanThreads), 0, stream, a);
+    hipLaunchKernelGGL((tables_kernel<EXTEND, true, 1>), dim3(1), dim3(kScanThreads), 0, stream, a);
   } else {
-    hipLaunchKernelGGL((tables_kernel<EXTEND, false>), dim3(1), dim3(kScanThreads), 0, stream, a);
+    if (a.n <= 4 * kScanThreads) hipLaunchKernelGGL((tables_kernel<EXTEND, false, 4>), dim3(1), dim3(kScanThreads), 0, stream, a);
+    else hipLaunchKernelGGL((tables_kernel<EXTEND, false, 0>), dim3(1), dim3(kScanThreads), 0, stream, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return report_hip(e, what);
     // (a page or more to a thread's rows: pages that change hands are hardly ever more than rows, and few of the pool's)
     const int64_t threads = EXTEND ? std::max<int64_t>(a.max_rows, a.n) : std::min<int64_t>((int64_t)a.n * 4, a.num_pages);
-    hipLaunchKernelGGL((fill_kernel<EXTEND>), dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>((threads + 255) / 256, 4 * kCus))), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((fill_kernel<EXTEND>), dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>((threads + kFillThreads - 1) / kFillThreads, 4 * kCus))), dim3(kFillThreads), 0, stream, a);
   }
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? CHUNK_ATTN_OK : report_hip(e, what);
 }
 
 // ---- keys and values into the pages ----
-// Bound by memory: 16 elements to a thread and tensor, kAtOnce such pieces loaded before any is stored.  A workgroup takes neighbouring rows.
-constexpr int kWriteThreads = 256, kAtOnce = 2;
+// Bound by memory: a thread takes eight elements of a row, of both tensors (two or four such pieces to a thread are slower, 88 and 93 us for the 87 below).
+constexpr int kWriteThreads = 256;
+constexpr int64_t kStreamBytes = (int64_t)256 << 20;
 
 struct WriteArgs {
   const __bf16 *k, *v;
@@ -236,70 +312,70 @@ struct WriteArgs {
   const int64_t* slots;
   const float *k_scale, *v_scale;
   void *k_cache, *v_cache;
-  int64_t num_slots, pieces;  // pieces of 16 elements in all rows
+  int64_t num_slots, pieces;  // pieces of eight elements in all rows
   int32_t heads, head_pieces, row_pieces, page_size;
   Divide by_row, by_head, by_page;
 };
 
-struct __attribute__((packed, aligned(2))) Loose16 {
-  u32x4 w[2];
+// Division by a head's scale.  x / s as x y + r y with y the nearest to 1 / s and r = x - (x y) s, which a fused multiply and add gives exactly: the nearest to the quotient, where nothing leaves
+// float32's normal range (equal to the division for 4 * 10^8 drawn pairs, and a third of its time).
+struct Scale {
+  float s, y;
+  bool usual;  // the quotient of anything by s that 8 bits hold is far from the ends of float32's range
+  explicit __device__ Scale(float scale) : s(scale), y(1.f / scale), usual(scale > 0x1p-80f && scale < 0x1p80f) {}
+  __device__ float divides(float x) const {
+    if (!usual) return x / s;
+    const float q = x * y;
+    return fabsf(q) < 1024.f ? __builtin_fmaf(__builtin_fmaf(-s, q, x), y, q) : q;
+  }
 };
-
-__device__ __forceinline__ u32x4 to_e4m3(const Loose16& x, float scale) {
-  u32x4 r;
+__device__ __forceinline__ u32x2 to_e4m3(const u32x4& x, const Scale& scale) {
+  u32x2 r;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    unsigned word = 0;
+  for (int w = 0; w < 2; ++w) {
+    float c[4];
+    unsigned nans = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const unsigned two = x.w[w >> 1][(w & 1) * 2 + (e >> 1)];
-      const float f = __uint_as_float(e & 1 ? two & 0xffff0000u : two << 16) / scale;  // (true division: rounded once)
-      // |f| up to 448 by clamping; a NaN passes neither comparison
-      const float c = f > 448.f ? 448.f : f < -448.f ? -448.f : f;
-      const unsigned byte = f != f ? 0x7fu : (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(c, c, 0, false) & 0xffu;
-      word |= byte << (8 * e);
+      const unsigned two = x[2 * w + (e >> 1)];
+      const float f = scale.divides(__uint_as_float(e & 1 ? two & 0xffff0000u : two << 16));
+      c[e] = f > 448.f ? 448.f : f < -448.f ? -448.f : f;  // (a NaN passes neither comparison)
+      nans |= f != f ? 0x7fu << (8 * e) : 0u;
     }
-    r[w] = word;
+    int word = __builtin_amdgcn_cvt_pk_fp8_f32(c[0], c[1], 0, false);
+    word = __builtin_amdgcn_cvt_pk_fp8_f32(c[2], c[3], word, true);
+    r[w] = (unsigned)word | nans;
   }
   return r;
 }
 
-template <bool E4M3>
+typedef u32x4 __attribute__((aligned(2))) LooseWords;
+template <bool STREAM, class T>
+__device__ __forceinline__ void store_words(T* p, T x) {
+  if (STREAM) __builtin_nontemporal_store(x, p);
+  else *p = x;
+}
+
+// STREAM: past the caches, for calls of more bytes than the last-level cache holds (65536 rows of 8 heads of 128 to e4m3, 403 MB: 87 -> 84 us); what fits is kept for who reads it next.
+template <bool E4M3, bool STREAM>
 __global__ __launch_bounds__(kWriteThreads) void write_kernel(const WriteArgs a) {
-  Loose16 k[kAtOnce], v[kAtOnce];
-  int64_t to[kAtOnce];
-  int head[kAtOnce];
-  const int64_t first = (int64_t)blockIdx.x * (kWriteThreads * kAtOnce) + threadIdx.x;
-#pragma unroll
-  for (int n = 0; n < kAtOnce; ++n) {
-    const int64_t piece = first + n * kWriteThreads;
-    to[n] = -1;
-    head[n] = 0;
-    if (piece >= a.pieces) continue;
-    // (pieces < 2^36; rows < 2^31)
-    const int64_t row = a.by_row.wide(piece);
-    const int in_row = (int)(piece - row * a.row_pieces);
-    const int64_t slot = a.slots[row];
-    if (slot < 0 || slot >= a.num_slots) continue;
-    head[n] = a.by_head(in_row);
-    const int64_t page = a.by_page.wide(slot);
-    to[n] = ((page * a.heads + head[n]) * a.page_size + (slot - page * a.page_size)) * a.head_pieces + (in_row - head[n] * a.head_pieces);
-    k[n] = *reinterpret_cast<const Loose16*>(a.k + row * a.k_stride + in_row * 16);
-    v[n] = *reinterpret_cast<const Loose16*>(a.v + row * a.v_stride + in_row * 16);
-  }
-#pragma unroll
-  for (int n = 0; n < kAtOnce; ++n) {
-    if (to[n] < 0) continue;
-    if constexpr (E4M3) {
-      reinterpret_cast<u32x4*>(a.k_cache)[to[n]] = to_e4m3(k[n], a.k_scale[head[n]]);
-      reinterpret_cast<u32x4*>(a.v_cache)[to[n]] = to_e4m3(v[n], a.v_scale[head[n]]);
-    } else {
-      u32x4 *const pk = reinterpret_cast<u32x4*>(a.k_cache) + 2 * to[n], *const pv = reinterpret_cast<u32x4*>(a.v_cache) + 2 * to[n];
-      pk[0] = k[n].w[0];
-      pk[1] = k[n].w[1];
-      pv[0] = v[n].w[0];
-      pv[1] = v[n].w[1];
-    }
+  const int64_t piece = (int64_t)blockIdx.x * kWriteThreads + threadIdx.x;
+  if (piece >= a.pieces) return;
+  const int64_t row = a.by_row.wide(piece);
+  const int in_row = (int)(piece - row * a.row_pieces);
+  const int64_t slot = a.slots[row];
+  if (slot < 0 || slot >= a.num_slots) return;
+  const int head = a.by_head(in_row);
+  const int64_t page = a.by_page.wide(slot);
+  const int64_t to = ((page * a.heads + head) * a.page_size + (slot - page * a.page_size)) * a.head_pieces + (in_row - head * a.head_pieces);
+  const LooseWords *const pk = reinterpret_cast<const LooseWords*>(a.k + row * a.k_stride + in_row * 8), *const pv = reinterpret_cast<const LooseWords*>(a.v + row * a.v_stride + in_row * 8);
+  const u32x4 k = STREAM ? __builtin_nontemporal_load(pk) : *pk, v = STREAM ? __builtin_nontemporal_load(pv) : *pv;
+  if constexpr (E4M3) {
+    store_words<STREAM>(reinterpret_cast<u32x2*>(a.k_cache) + to, to_e4m3(k, Scale(a.k_scale[head])));
+    store_words<STREAM>(reinterpret_cast<u32x2*>(a.v_cache) + to, to_e4m3(v, Scale(a.v_scale[head])));
+  } else {
+    store_words<STREAM>(reinterpret_cast<u32x4*>(a.k_cache) + to, k);
+    store_words<STREAM>(reinterpret_cast<u32x4*>(a.v_cache) + to, v);
   }
 }
 
@@ -371,14 +447,16 @@ extern "C" int paged_cache_write(int32_t rows, int32_t num_kv_heads, int32_t hea
   if (!aligned(k, 2) || !aligned(v, 2) || k_stride < row_elements || v_stride < row_elements || !aligned(slots, 8) || !aligned(k_cache, 16) || !aligned(v_cache, 16) ||
       (cache_type == PAGED_CACHE_E4M3 && (!aligned(k_scale, 4) || !aligned(v_scale, 4))))
     return CHUNK_ATTN_INVALID_ARG;
-  const int row_pieces = (int)(row_elements / 16), head_pieces = head_dim / 16;
+  const int row_pieces = (int)(row_elements / 8), head_pieces = head_dim / 8;
   const int64_t pieces = (int64_t)rows * row_pieces;
   const WriteArgs a{(const __bf16*)k, (const __bf16*)v, k_stride, v_stride, slots, k_scale, v_scale, k_cache, v_cache, (int64_t)num_pages * page_size, pieces, num_kv_heads,
                     head_pieces, row_pieces, page_size, Divide(row_pieces), Divide(head_pieces), Divide(page_size)};
-  const int64_t groups = (pieces + kWriteThreads * kAtOnce - 1) / (kWriteThreads * kAtOnce);
+  const int64_t groups = (pieces + kWriteThreads - 1) / kWriteThreads;
   if (groups * kWriteThreads >= (int64_t)1 << 32) return CHUNK_ATTN_INVALID_ARG;
-  if (cache_type == PAGED_CACHE_E4M3) hipLaunchKernelGGL(write_kernel<true>, dim3((unsigned)groups), dim3(kWriteThreads), 0, (hipStream_t)hip_stream, a);
-  else hipLaunchKernelGGL(write_kernel<false>, dim3((unsigned)groups), dim3(kWriteThreads), 0, (hipStream_t)hip_stream, a);
+  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(kWriteThreads), 0, (hipStream_t)hip_stream, a); };
+  const bool e4m3 = cache_type == PAGED_CACHE_E4M3;
+  if (pieces * (e4m3 ? 48 : 64) > kStreamBytes) e4m3 ? launch(write_kernel<true, true>) : launch(write_kernel<false, true>);
+  else e4m3 ? launch(write_kernel<true, false>) : launch(write_kernel<false, false>);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? CHUNK_ATTN_OK : report_hip(e, "keys and values into pages");
 }
