@@ -8,6 +8,7 @@ import torch
 
 from . import ChunkAttnError
 
+_only_gpu = None
 BF16, F32, U8, I32 = torch.bfloat16, torch.float32, torch.uint8, torch.int32
 
 
@@ -50,6 +51,14 @@ def room(workspace):
 
 def call(function, tensors, stream, *args):
     """Calls a function of the library on the GPU that holds the tensors (which need not be the current one), on `stream` or that GPU's current one."""
+    global _only_gpu
+    if _only_gpu is None:
+        _only_gpu = torch.cuda.device_count() == 1
+    if _only_gpu:  # (all of them are on it)
+        rc = function(*args, torch._C._cuda_getCurrentRawStream(0) if stream is None else stream.cuda_stream)
+        if rc != 0:
+            raise ChunkAttnError(rc)
+        return
     devices = {t.get_device() for t in tensors if t is not None}
     if len(devices) > 1:
         raise ValueError("the tensors are on different GPUs")

@@ -38,26 +38,31 @@ enum { kPagesBefore, kOldLen, kHeld, kSums };
 // Behind them: pages that change hands, pages on the stack before the call.
 enum { kMoved, kOnStack, kTotals };
 
-__device__ __forceinline__ int64_t wave_scan(int64_t x) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int64_t y = __shfl_up(x, o);
-    if (lane >= o) x += y;
-  }
+// Sums that stay at the largest number once they are there: whatever the inputs are, what is below 2^32 - 1 is right, and nothing larger is used.
+__device__ __forceinline__ uint32_t add(uint32_t x, uint32_t y) { return __builtin_elementwise_add_sat(x, y); }
+// Sum over the lanes up to the own one: within rows of 16 lanes, then from row to row.
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
+  x = add(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, false));  // from 1, 2, 4 and 8 lanes before
+  x = add(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, false));
+  x = add(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, false));
+  x = add(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, false));
+  x = add(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false));  // the last lane of the row before, to rows 1 and 3
+  x = add(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false));  // lane 31 to rows 2 and 3
   return x;
 }
-// Sum over the threads before the own one; `room`: one number for each wave.
-__device__ __forceinline__ int64_t sum_before(int64_t x, int64_t* room) {
-  const int64_t up_to = wave_scan(x);
+// Sum over the threads before the own one; `room`: one number for each wave, used by no other sum.
+__device__ __forceinline__ uint32_t sum_before(uint32_t x, uint32_t* room) {
+  const uint32_t up_to = wave_scan(x);
+  uint32_t before = (uint32_t)__shfl_up((int)up_to, 1);
+  if ((threadIdx.x & 63) == 0) before = 0;
   if ((threadIdx.x & 63) == 63) room[threadIdx.x >> 6] = up_to;
   __syncthreads();
-  int64_t before = up_to - x;
-  for (int w = 0; w < (int)(threadIdx.x >> 6); ++w) before += room[w];
-  __syncthreads();
+  const int wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int w = 0; w < kScanThreads / 64; ++w) before = add(before, w < wave ? room[w] : 0);
   return before;
 }
-__device__ __forceinline__ int at_most(int64_t x, int64_t most) { return (int)(x < most ? x : most); }
+__device__ __forceinline__ int at_most(uint32_t x, int most) { return (int)min(x, (uint32_t)most); }
 
 // A request, its numbers brought into their ranges.
 struct Request {
@@ -67,15 +72,14 @@ struct Request {
 __device__ __forceinline__ int pages_of(const TableArgs& a, int len) { return len > 0 ? a.by_page(len - 1) + 1 : 0; }
 template <bool EXTEND>
 __device__ __forceinline__ Request request_of(const TableArgs& a, int change, int kv_len, int held) {
-  const int64_t most = (int64_t)a.max_pages * a.page_size;  // < 2^31
+  const int most = a.max_pages * a.page_size;  // < 2^31
   Request r;
-  r.old_len = at_most(max(kv_len, 0), most);
+  r.old_len = min(max(kv_len, 0), most);
   r.held = min(max(held, 0), a.max_pages);
   r.change = max(change, 0);
   if (EXTEND) {
-    const int64_t len = (int64_t)r.old_len + r.change;
-    r.fits = len <= most;
-    r.len = r.fits ? (int)len : r.old_len;
+    r.fits = r.change <= most - r.old_len;
+    r.len = r.fits ? r.old_len + r.change : r.old_len;
     r.need = r.fits ? max(0, pages_of(a, r.len) - r.held) : 0;
   } else {
     r.fits = true;
@@ -115,7 +119,11 @@ __device__ __forceinline__ void move_page(const TableArgs& a, const int32_t* pag
   else if (on_stack + p < a.num_pages) a.free_pages[on_stack + p] = *entry;
 }
 
-// Loads of four neighbouring numbers, from any address that suits one.
+// What becomes of a request (members as in the arrays they go to).
+struct Outcome {
+  int start, end, pages_before, old_len, held, granted, len_out, held_out;
+};
+// Four neighbouring numbers, from any address that suits one.
 struct __attribute__((packed, aligned(4))) LooseInts {
   int x[4];
 };
@@ -123,7 +131,7 @@ struct __attribute__((packed, aligned(4))) LooseInts {
 // IN_ONE: at most kScanThreads requests and kInOne rows; everything is done here.  EACH: requests of a thread (0: any number, read again wherever they are used).
 template <bool EXTEND, bool IN_ONE, int EACH>
 __global__ __launch_bounds__(kScanThreads) void tables_kernel(const TableArgs a) {
-  __shared__ int64_t room[kScanThreads / 64];
+  __shared__ uint32_t room[2][kScanThreads / 64];
   __shared__ int32_t in_lds[IN_ONE ? kSums + 1 : 1][IN_ONE ? kScanThreads + 1 : 1];
   __shared__ int moved;
   static_assert(!IN_ONE || EACH == 1);
@@ -156,49 +164,84 @@ __global__ __launch_bounds__(kScanThreads) void tables_kernel(const TableArgs a)
   int32_t* const old_lens = IN_ONE ? in_lds[kOldLen] : a.sums + (int64_t)kOldLen * a.n;
   int32_t* const helds = IN_ONE ? in_lds[kHeld] : a.sums + (int64_t)kHeld * a.n;
   int32_t* const starts = IN_ONE ? in_lds[kSums] : a.q_start;
-  if (threadIdx.x == 0) moved = 0;
+  auto leave = [&](int i, const Outcome& o) {
+    pages_before[i] = o.pages_before;
+    old_lens[i] = o.old_len;
+    helds[i] = o.held;
+    a.kv_len_out[i] = o.len_out;
+    a.held_out[i] = o.held_out;
+    if (EXTEND) {
+      starts[i] = o.start;
+      if (IN_ONE) a.q_start[i] = o.start;
+      if (i == a.n - 1) {
+        starts[a.n] = o.end;
+        if (IN_ONE) a.q_start[a.n] = o.end;
+      }
+      if (a.granted) a.granted[i] = o.granted;
+    }
+  };
+  if (threadIdx.x == 0) moved = 0;  // (before the sums' barrier)
   // rows first: who does not fit in them has no claim on pages
-  int64_t rows = 0, pages = 0;
+  uint32_t rows = 0, pages = 0;
   if (EXTEND) {
-    each_request([&](int, const Request& r) { rows += r.change; });
-    rows = sum_before(rows, room);
+    each_request([&](int, const Request& r) { rows = add(rows, r.change); });
+    rows = sum_before(rows, room[0]);
   }
-  int64_t row = rows;
+  uint32_t row = rows;
   each_request([&](int, const Request& r) {
-    row += r.change;
-    if (!EXTEND || r.change == 0 || row <= a.max_rows) pages += r.need;
+    row = add(row, r.change);
+    if (!EXTEND || r.change == 0 || row <= (uint32_t)a.max_rows) pages = add(pages, r.need);
   });
-  pages = sum_before(pages, room);
+  pages = sum_before(pages, room[1]);
   row = rows;
   int mine = 0;
+  Outcome outcome[EACH ? EACH : 1];
   each_request([&](int i, const Request& r) {
-    const int64_t end = row + r.change;
-    const bool in_rows = !EXTEND || r.change == 0 || end <= a.max_rows;
+    const uint32_t end = add(row, r.change);
+    const bool in_rows = !EXTEND || r.change == 0 || end <= (uint32_t)a.max_rows;
     const int need = in_rows ? r.need : 0;
-    const bool served = r.fits && in_rows && (!EXTEND || need == 0 || pages + need <= on_stack);
-    pages_before[i] = at_most(pages, INT32_MAX);
-    pages += need;
+    const bool served = r.fits && in_rows && (!EXTEND || need == 0 || add(pages, need) <= (uint32_t)on_stack);
+    Outcome o;
+    o.start = at_most(row, a.max_rows);
+    o.end = at_most(end, a.max_rows);
+    o.pages_before = at_most(pages, INT32_MAX);
+    pages = add(pages, need);
     if (served && need > 0) mine = at_most(pages, INT32_MAX);  // (the sums grow: those that are served are the first of those that need pages)
-    old_lens[i] = served ? r.old_len : -1;
-    helds[i] = EXTEND ? r.held : r.held - need;
-    if (EXTEND) {
-      const int start = at_most(row, a.max_rows);
-      starts[i] = start;
-      if (IN_ONE) a.q_start[i] = start;
-      if (i == a.n - 1) {
-        starts[a.n] = at_most(end, a.max_rows);
-        if (IN_ONE) a.q_start[a.n] = at_most(end, a.max_rows);
-      }
-      if (a.granted) a.granted[i] = served;
-    }
     row = end;
-    a.kv_len_out[i] = served ? r.len : r.old_len;
-    a.held_out[i] = EXTEND ? r.held + (served ? need : 0) : r.held - need;
+    o.old_len = served ? r.old_len : -1;
+    o.held = EXTEND ? r.held : r.held - need;
+    o.granted = served;
+    o.len_out = served ? r.len : r.old_len;
+    o.held_out = EXTEND ? r.held + (served ? need : 0) : r.held - need;
+    if constexpr (EACH > 0) outcome[i - first] = o;
+    else leave(i, o);
   });
+  if constexpr (EACH == 4) {
+    if (last == first + EACH) {
+      // four neighbouring numbers to a store
+      auto four = [&](int32_t* p, auto member) {
+        *reinterpret_cast<LooseInts*>(p + first) = LooseInts{{outcome[0].*member, outcome[1].*member, outcome[2].*member, outcome[3].*member}};
+      };
+      four(pages_before, &Outcome::pages_before);
+      four(old_lens, &Outcome::old_len);
+      four(helds, &Outcome::held);
+      four(a.kv_len_out, &Outcome::len_out);
+      four(a.held_out, &Outcome::held_out);
+      if (EXTEND) {
+        four(a.q_start, &Outcome::start);
+        if (a.granted) four(a.granted, &Outcome::granted);
+        if (last == a.n) a.q_start[a.n] = outcome[3].end;
+      }
+    } else {
+      each_request([&](int i, const Request&) { leave(i, outcome[i - first]); });
+    }
+  } else if constexpr (EACH == 1) {
+    each_request([&](int i, const Request&) { leave(i, outcome[0]); });
+  }
   if (mine > 0) atomicMax(&moved, mine);
   __syncthreads();
   if (threadIdx.x == 0) {
-    *a.num_free_out = EXTEND ? on_stack - moved : at_most((int64_t)on_stack + moved, a.num_pages);
+    *a.num_free_out = EXTEND ? on_stack - moved : at_most((uint32_t)on_stack + (uint32_t)moved, a.num_pages);
     if (!IN_ONE) {
       a.sums[(int64_t)kSums * a.n + kMoved] = moved;
       a.sums[(int64_t)kSums * a.n + kOnStack] = on_stack;
