@@ -17,6 +17,7 @@ namespace {
 // from the sums (slots of rows, entries of the table, entries of the stack) goes row by row and page by page, each of which finds its request by halving in the sums.  Few requests with few
 // rows: the same workgroup does that too, with the sums in LDS (one launch).  Else the sums go to the workspace and a second launch fills the chip.
 constexpr int kScanThreads = 1024;
+constexpr int kFillThreads = 256;
 constexpr int kInOne = 4096;  // rows that the one workgroup goes through itself
 
 struct TableArgs {
@@ -238,6 +239,15 @@ __global__ __launch_bounds__(kScanThreads) void tables_kernel(const TableArgs a)
   } else if constexpr (EACH == 1) {
     each_request([&](int i, const Request&) { leave(i, outcome[0]); });
   }
+  if constexpr (EXTEND && !IN_ONE) {
+    // fill_kernel's workgroups begin to look for their rows' requests where the first row's slot will be
+    row = rows;
+    each_request([&](int i, const Request& r) {
+      const int64_t end = min(add(row, r.change), (uint32_t)a.max_rows);
+      for (int64_t at = ((int64_t)row + kFillThreads - 1) / kFillThreads * kFillThreads; at < end; at += kFillThreads) a.slots[at] = i;
+      row = add(row, r.change);
+    });
+  }
   if (mine > 0) atomicMax(&moved, mine);
   __syncthreads();
   if (threadIdx.x == 0) {
@@ -254,57 +264,56 @@ __global__ __launch_bounds__(kScanThreads) void tables_kernel(const TableArgs a)
   }
 }
 
-// Where a workgroup's neighbouring rows (or pages) begin to be found: the last i < n with sums[i] <= x, by one wave that looks at 64 places at a time, and the sums from there on in LDS.
-constexpr int kFillThreads = 256, kWindow = 1024;
-struct Window {
-  int32_t at[kWindow];
-  int first, count;
-};
-__device__ void open_window(Window& w, const int32_t* sums, int n, int x) {
-  if (threadIdx.x < 64) {
-    int lo = 0, size = n;  // the place is in lo .. lo + size - 1
-    while (size > 1) {
-      const int step = (size + 63) / 64, i = lo + (int)threadIdx.x * step;
-      const unsigned long long up_to = __ballot(i < lo + size && sums[min(i, n - 1)] <= x);  // (sums grow: the first places)
-      const int last = 63 - __clzll((long long)up_to);
-      size = min(step, size - last * step);
-      lo += last * step;
-    }
-    if (threadIdx.x == 0) w.first = lo;
-  }
-  __syncthreads();
-  const int first = w.first, count = min(kWindow, n - first);
-  for (int i = threadIdx.x; i < count; i += kFillThreads) w.at[i] = sums[first + i];
-  if (threadIdx.x == 0) w.count = count;
-  __syncthreads();
-}
-// The same for an x that is not smaller; rows of requests that have none may lie between, so that the window need not reach it.
-__device__ __forceinline__ int find_from(const Window& w, const int32_t* sums, int n, int x) {
-  if (w.first + w.count < n && x >= w.at[w.count - 1]) return find(sums, n, x);
-  return w.first + find(w.at, w.count, x);
-}
-
+// The first `page_groups` workgroups: pages that change hands, a wave to a request.  The others: slots, kFillThreads neighbouring rows to a workgroup, whose requests are looked for among the sums from the
+// first row's request on, in LDS (rows of requests that have none may lie between, so that kWindow of them need not reach the last row).
+constexpr int kWindow = 1024;
 template <bool EXTEND>
-__global__ __launch_bounds__(kFillThreads) void fill_kernel(const TableArgs a) {
-  __shared__ Window window;
+__global__ __launch_bounds__(kFillThreads) void fill_kernel(const TableArgs a, const int page_groups) {
   const int32_t *const pages_before = a.sums + (int64_t)kPagesBefore * a.n, *const old_lens = a.sums + (int64_t)kOldLen * a.n, *const helds = a.sums + (int64_t)kHeld * a.n;
   const int moved = a.sums[(int64_t)kSums * a.n + kMoved], on_stack = a.sums[(int64_t)kSums * a.n + kOnStack];
-  const int64_t step = (int64_t)gridDim.x * kFillThreads;
-  if (EXTEND) {
+  if ((int)blockIdx.x < page_groups) {
+    const int i = __builtin_amdgcn_readfirstlane(blockIdx.x * (kFillThreads / 64) + (threadIdx.x >> 6)), lane = threadIdx.x & 63;
+    if (i >= a.n) return;
+    const int first = pages_before[i], held = helds[i], end = i + 1 < a.n ? pages_before[i + 1] : INT32_MAX;
+    // (extend: none of a request that is not served)
+    const int last = EXTEND ? first + (a.held_out[i] - held) : min(end, moved);
+    constexpr int kAtOnce = 4;
+    int32_t* const entries = a.table + (int64_t)i * a.max_pages + held;
+    for (int64_t p0 = first; p0 < last; p0 += 64 * kAtOnce) {
+      int32_t page[kAtOnce];
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) {
+        const int64_t p = p0 + k * 64 + lane;
+        page[k] = p >= last ? 0 : EXTEND ? a.free_pages[on_stack - 1 - p] : entries[p - first];
+      }
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) {
+        const int64_t p = p0 + k * 64 + lane;
+        if (p >= last) continue;
+        if (EXTEND) entries[p - first] = page[k];
+        else if (on_stack + p < a.num_pages) a.free_pages[on_stack + p] = page[k];
+      }
+    }
+    return;
+  }
+  if constexpr (EXTEND) {
+    __shared__ int32_t window[kWindow];
     const int rows = a.q_start[a.n];
-    for (int64_t r0 = (int64_t)blockIdx.x * kFillThreads; r0 < a.max_rows; r0 += step) {
-      if (r0 < rows) open_window(window, a.q_start, a.n, (int)r0);
+    for (int64_t r0 = (int64_t)(blockIdx.x - page_groups) * kFillThreads; r0 < a.max_rows; r0 += (int64_t)(gridDim.x - page_groups) * kFillThreads) {
       const int64_t r = r0 + threadIdx.x;
-      if (r < a.max_rows) a.slots[r] = r < rows ? slot_of_row(a, a.q_start, pages_before, old_lens, helds, on_stack, (int)r, find_from(window, a.q_start, a.n, (int)r)) : -1;
+      const int first = r0 < rows ? (int)a.slots[r0] : 0, count = min(kWindow, a.n - first);
+      for (int i = threadIdx.x; i < count; i += kFillThreads) window[i] = a.q_start[first + i];
+      __syncthreads();  // (and the first row's slot has been read)
+      if (r < a.max_rows) {
+        int64_t slot = -1;
+        if (r < rows) {
+          const bool behind = first + count < a.n && r >= window[count - 1];
+          slot = slot_of_row(a, a.q_start, pages_before, old_lens, helds, on_stack, (int)r, behind ? find(a.q_start, a.n, (int)r) : first + find(window, count, (int)r));
+        }
+        a.slots[r] = slot;
+      }
       __syncthreads();
     }
-  }
-  // (pages with the last workgroups first: those with the fewest rows)
-  for (int64_t p0 = (int64_t)(gridDim.x - 1 - blockIdx.x) * kFillThreads; p0 < moved; p0 += step) {
-    open_window(window, pages_before, a.n, (int)p0);
-    const int64_t p = p0 + threadIdx.x;
-    if (p < moved) move_page<EXTEND>(a, pages_before, helds, on_stack, (int)p, find_from(window, pages_before, a.n, (int)p));
-    __syncthreads();
   }
 }
 
@@ -336,9 +345,9 @@ int run_tables(const paged_cache_desc* d, TableArgs a, void* workspace, size_t w
     else hipLaunchKernelGGL((tables_kernel<EXTEND, false, 0>), dim3(1), dim3(kScanThreads), 0, stream, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return report_hip(e, what);
-    // (a page or more to a thread's rows: pages that change hands are hardly ever more than rows, and few of the pool's)
-    const int64_t threads = EXTEND ? std::max<int64_t>(a.max_rows, a.n) : std::min<int64_t>((int64_t)a.n * 4, a.num_pages);
-    hipLaunchKernelGGL((fill_kernel<EXTEND>), dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>((threads + kFillThreads - 1) / kFillThreads, 4 * kCus))), dim3(kFillThreads), 0, stream, a);
+    const int page_groups = (a.n + kFillThreads / 64 - 1) / (kFillThreads / 64);
+    const int row_groups = EXTEND ? (int)std::min<int64_t>(((int64_t)a.max_rows + kFillThreads - 1) / kFillThreads, 4 * kCus) : 0;
+    hipLaunchKernelGGL((fill_kernel<EXTEND>), dim3((unsigned)(page_groups + row_groups)), dim3(kFillThreads), 0, stream, a, page_groups);
   }
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? CHUNK_ATTN_OK : report_hip(e, what);
