@@ -40,6 +40,13 @@ def whole(t, dtype, shape, name):
     return t.data_ptr()
 
 
+def given(t, dtype, shape, name):
+    """The same for a tensor that has to be there."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.shape == shape and t.is_contiguous()):
+        _refuse(name, dtype, shape, "contiguous ")
+    return t.data_ptr()
+
+
 def room(workspace):
     """Address and size of a workspace; (None, 0) for None."""
     if workspace is None:

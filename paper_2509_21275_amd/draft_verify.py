@@ -4,7 +4,7 @@ from __future__ import annotations
 import ctypes
 
 from . import ChunkAttnError, _lib
-from ._args import BF16, F32, I32, call, room, torch, whole
+from ._args import BF16, F32, I32, call, given, room, torch, whole
 
 _bound = False
 
@@ -57,12 +57,9 @@ def draft_verify(target, draft, tokens, count, uniforms, last_uniform, accepted,
         _bind()
     if not (isinstance(target, torch.Tensor) and target.dim() == 3 and target.shape[1] >= 1 and target.dtype in (F32, BF16)):
         raise ValueError("target: expected a float32 or bf16 tensor of 3 dimensions")
-    for t, name in ((tokens, "tokens"), (uniforms, "uniforms"), (last_uniform, "last_uniform"), (accepted, "accepted"), (out, "out"), (workspace, "workspace")):
-        if t is None:
-            raise ValueError(f"{name}: expected a tensor")
     n, places, V = target.shape
     K = places - 1
     call(_lib.draft_verify, (target, draft, tokens, count, uniforms, last_uniform, accepted, rejected, out, workspace), stream, n, K, V, 1 if target.dtype == F32 else 0,
-         *_probabilities(target, (n, places, V), target.dtype, "target"), *_probabilities(draft, (n, K, V), target.dtype, "draft"), whole(tokens, I32, (n, K), "tokens"),
-         whole(count, I32, (n,), "count"), whole(uniforms, F32, (n, K), "uniforms"), whole(last_uniform, F32, (n,), "last_uniform"), whole(accepted, I32, (n,), "accepted"),
-         whole(rejected, I32, (n,), "rejected"), whole(out, I32, (n, K + 1), "out"), *room(workspace))
+         *_probabilities(target, (n, places, V), target.dtype, "target"), *_probabilities(draft, (n, K, V), target.dtype, "draft"), given(tokens, I32, (n, K), "tokens"),
+         whole(count, I32, (n,), "count"), given(uniforms, F32, (n, K), "uniforms"), given(last_uniform, F32, (n,), "last_uniform"), given(accepted, I32, (n,), "accepted"),
+         whole(rejected, I32, (n,), "rejected"), given(out, I32, (n, K + 1), "out"), *room(workspace))

@@ -4,7 +4,7 @@ from __future__ import annotations
 import ctypes
 
 from . import ChunkAttnError, _lib
-from ._args import BF16, F32, I32, call, room, rows, torch, whole
+from ._args import BF16, F32, I32, call, given, room, rows, torch, whole
 from .paged_cache import CACHE_TYPES
 
 _bound = False
@@ -59,15 +59,11 @@ def alloc_workspace(desc, device="cuda"):
 def paged_attn_fwd(desc, q, k_cache, v_cache, table, kv_len, q_start, o, lse, workspace, k_scale=None, v_scale=None, stream=None) -> None:
     """Attention of q [total_q, num_q_heads, head_dim] over the pages of each sequence (table [num_seqs, max_pages], kv_len [num_seqs], q_start [num_seqs + 1], all int32);
     writes o like q and, unless it is None, lse [num_q_heads, total_q] float32.  k_scale, v_scale [num_kv_heads] float32 for cache_type "e4m3"."""
-    for t, name in ((q, "q"), (k_cache, "k_cache"), (v_cache, "v_cache"), (table, "table"), (kv_len, "kv_len"), (q_start, "q_start"), (o, "o"), (workspace, "workspace")):
-        if t is None:
-            raise ValueError(f"{name}: expected a tensor")
     H, Hk, d, n = desc.num_q_heads, desc.num_kv_heads, desc.head_dim, desc.num_seqs
     dtype = desc._dtype
-    if dtype != BF16 and (k_scale is None or v_scale is None):
-        raise ValueError("k_scale, v_scale: expected tensors")
+    scale = whole if dtype == BF16 else given
     qs, cs = (desc.total_q, H, d), (desc.num_pages, Hk, desc.page_size, d)
     call(_lib.paged_attn_fwd, (q, k_cache, v_cache, k_scale, v_scale, table, kv_len, q_start, o, lse, workspace), stream, ctypes.byref(desc), *rows(q, BF16, qs, (d, 1), "q"),
-         whole(k_cache, dtype, cs, "k_cache"), whole(v_cache, dtype, cs, "v_cache"), whole(k_scale, F32, (Hk,), "k_scale"), whole(v_scale, F32, (Hk,), "v_scale"),
-         whole(table, I32, (n, desc.max_pages), "table"), whole(kv_len, I32, (n,), "kv_len"), whole(q_start, I32, (n + 1,), "q_start"), *rows(o, BF16, qs, (d, 1), "o"),
+         given(k_cache, dtype, cs, "k_cache"), given(v_cache, dtype, cs, "v_cache"), scale(k_scale, F32, (Hk,), "k_scale"), scale(v_scale, F32, (Hk,), "v_scale"),
+         given(table, I32, (n, desc.max_pages), "table"), given(kv_len, I32, (n,), "kv_len"), given(q_start, I32, (n + 1,), "q_start"), *rows(o, BF16, qs, (d, 1), "o"),
          whole(lse, F32, (H, desc.total_q), "lse"), *room(workspace))

@@ -4,7 +4,7 @@ from __future__ import annotations
 import ctypes
 
 from . import ChunkAttnError, _lib
-from ._args import BF16, F32, I32, call, room, rows, torch, whole
+from ._args import BF16, F32, I32, call, given, room, rows, torch, whole
 
 _bound = False
 E4M3, I64 = torch.float8_e4m3fn, torch.int64
@@ -56,37 +56,27 @@ def alloc_workspace(desc, device="cuda"):
     return torch.empty(max(paged_cache_workspace_bytes(desc), 256), dtype=torch.uint8, device=device)
 
 
-def _must(*named):
-    for t, name in named:
-        if t is None:
-            raise ValueError(f"{name}: expected a tensor")
-
-
 def paged_cache_extend(desc, new_tokens, kv_len, held, table, free_pages, num_free, kv_len_out, held_out, num_free_out, q_start, slots, granted, workspace,
                        stream=None) -> None:
     """Pages and slots for new_tokens [num_requests] tokens of each request; writes the state behind the call (kv_len_out, held_out, num_free_out, which may be the inputs, and new
     entries of table), q_start [num_requests + 1], slots [rows] int64 (its length is the most rows there are) and, unless it is None, granted [num_requests]."""
     n, one = (desc.num_requests,), (1,)
-    _must((new_tokens, "new_tokens"), (kv_len, "kv_len"), (held, "held"), (table, "table"), (free_pages, "free_pages"), (num_free, "num_free"), (kv_len_out, "kv_len_out"),
-          (held_out, "held_out"), (num_free_out, "num_free_out"), (q_start, "q_start"), (slots, "slots"))
     if not (isinstance(slots, torch.Tensor) and slots.dim() == 1):
         raise ValueError("slots: expected a tensor of one dimension")
     call(_lib.paged_cache_extend, (new_tokens, kv_len, held, table, free_pages, num_free, kv_len_out, held_out, num_free_out, q_start, slots, granted, workspace), stream,
-         ctypes.byref(desc), whole(new_tokens, I32, n, "new_tokens"), whole(kv_len, I32, n, "kv_len"), whole(held, I32, n, "held"),
-         whole(table, I32, (desc.num_requests, desc.max_pages), "table"), whole(free_pages, I32, (desc.num_pages,), "free_pages"), whole(num_free, I32, one, "num_free"),
-         whole(kv_len_out, I32, n, "kv_len_out"), whole(held_out, I32, n, "held_out"), whole(num_free_out, I32, one, "num_free_out"),
-         whole(q_start, I32, (desc.num_requests + 1,), "q_start"), whole(slots, I64, slots.shape, "slots"), slots.shape[0], whole(granted, I32, n, "granted"), *room(workspace))
+         ctypes.byref(desc), given(new_tokens, I32, n, "new_tokens"), given(kv_len, I32, n, "kv_len"), given(held, I32, n, "held"),
+         given(table, I32, (desc.num_requests, desc.max_pages), "table"), given(free_pages, I32, (desc.num_pages,), "free_pages"), given(num_free, I32, one, "num_free"),
+         given(kv_len_out, I32, n, "kv_len_out"), given(held_out, I32, n, "held_out"), given(num_free_out, I32, one, "num_free_out"),
+         given(q_start, I32, (desc.num_requests + 1,), "q_start"), given(slots, I64, slots.shape, "slots"), slots.shape[0], whole(granted, I32, n, "granted"), *room(workspace))
 
 
 def paged_cache_truncate(desc, drop, kv_len, held, table, free_pages, num_free, kv_len_out, held_out, num_free_out, workspace, stream=None) -> None:
     """Takes drop [num_requests] tokens off the end of each request and puts pages that hold none of those left back on the stack; *_out may be the inputs."""
     n, one = (desc.num_requests,), (1,)
-    _must((drop, "drop"), (kv_len, "kv_len"), (held, "held"), (table, "table"), (free_pages, "free_pages"), (num_free, "num_free"), (kv_len_out, "kv_len_out"),
-          (held_out, "held_out"), (num_free_out, "num_free_out"))
     call(_lib.paged_cache_truncate, (drop, kv_len, held, table, free_pages, num_free, kv_len_out, held_out, num_free_out, workspace), stream, ctypes.byref(desc),
-         whole(drop, I32, n, "drop"), whole(kv_len, I32, n, "kv_len"), whole(held, I32, n, "held"), whole(table, I32, (desc.num_requests, desc.max_pages), "table"),
-         whole(free_pages, I32, (desc.num_pages,), "free_pages"), whole(num_free, I32, one, "num_free"), whole(kv_len_out, I32, n, "kv_len_out"),
-         whole(held_out, I32, n, "held_out"), whole(num_free_out, I32, one, "num_free_out"), *room(workspace))
+         given(drop, I32, n, "drop"), given(kv_len, I32, n, "kv_len"), given(held, I32, n, "held"), given(table, I32, (desc.num_requests, desc.max_pages), "table"),
+         given(free_pages, I32, (desc.num_pages,), "free_pages"), given(num_free, I32, one, "num_free"), given(kv_len_out, I32, n, "kv_len_out"),
+         given(held_out, I32, n, "held_out"), given(num_free_out, I32, one, "num_free_out"), *room(workspace))
 
 
 def paged_cache_write(k, v, slots, k_cache, v_cache, k_scale=None, v_scale=None, stream=None) -> None:
@@ -100,9 +90,8 @@ def paged_cache_write(k, v, slots, k_cache, v_cache, k_scale=None, v_scale=None,
     n, H, d = k.shape
     pages, page = k_cache.shape[0], k_cache.shape[2]
     dtype = E4M3 if k_cache.dtype == E4M3 else BF16
-    if dtype == E4M3:
-        _must((k_scale, "k_scale"), (v_scale, "v_scale"))
+    scale = given if dtype == E4M3 else whole
     cs, ks = (pages, H, page, d), (n, H, d)
     call(_lib.paged_cache_write, (k, v, slots, k_cache, v_cache, k_scale, v_scale), stream, n, H, d, page, pages, 1 if dtype == E4M3 else 0, *rows(k, BF16, ks, (d, 1), "k"),
-         *rows(v, BF16, ks, (d, 1), "v"), whole(slots, I64, (n,), "slots"), whole(k_scale, F32, (H,), "k_scale"), whole(v_scale, F32, (H,), "v_scale"),
-         whole(k_cache, dtype, cs, "k_cache"), whole(v_cache, dtype, cs, "v_cache"))
+         *rows(v, BF16, ks, (d, 1), "v"), given(slots, I64, (n,), "slots"), scale(k_scale, F32, (H,), "k_scale"), scale(v_scale, F32, (H,), "v_scale"),
+         given(k_cache, dtype, cs, "k_cache"), given(v_cache, dtype, cs, "v_cache"))
