@@ -39,7 +39,9 @@ typedef struct {
   int32_t total_q;      /* rows of q and o, >= 0 (0: nothing to do); total_q * num_q_heads < 2^31 */
   int32_t page_size;    /* 1 .. PAGED_CACHE_MAX_PAGE_SIZE */
   int32_t num_pages;    /* pages of the pool; num_pages * num_kv_heads * page_size < 2^31 */
-  int32_t max_pages;    /* entries of a row of the table; max_pages * page_size <= 2^30 */
+  /* entries of a row of the table; max_pages * page_size <= 2^30, and with the rows of all sequences, R = total_q * num_q_heads / num_kv_heads:
+   * (num_seqs + R / 32) * max_pages * page_size <= 2^37 */
+  int32_t max_pages;
   int32_t cache_type;   /* PAGED_CACHE_BF16 or PAGED_CACHE_E4M3 */
   float softmax_scale;  /* finite, > 0; normally 1/sqrt(head_dim) */
 } paged_attn_desc;

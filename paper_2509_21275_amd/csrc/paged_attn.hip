@@ -50,7 +50,7 @@ struct AttnArgs {
   int32_t num_seqs, total_q, heads, group, page_size, num_pages, max_pages, shares;
   int32_t most_subs;  // groups of rows that walk over the keys together, at most
   float scale_log2;
-  Divide by_page, by_group;
+  Divide by_page, by_group, by_shares;
 };
 // First row of q of its sequence, its first row of the sequence's, how many rows, and in how many shares it lies.
 enum { kCutSeqRow, kCutRow, kCutRows, kCutShares, kCut };
@@ -71,7 +71,7 @@ struct Sequence {
     return (rows + n - 1) / n;
   }
   __device__ int key_blocks() const { return max(1, (int)(((unsigned)len + kBlockKeys - 1) / kBlockKeys)); }
-  __device__ int64_t units(int most) const { return (int64_t)row_blocks(most) * key_blocks(); }
+  __device__ int units(int most) const { return row_blocks(most) * key_blocks(); }  // < 2^30 (check_desc)
 };
 __device__ __forceinline__ Sequence sequence_at(const AttnArgs& a, int i) {
   Sequence s;
@@ -82,20 +82,8 @@ __device__ __forceinline__ Sequence sequence_at(const AttnArgs& a, int i) {
   return s;
 }
 
-__device__ __forceinline__ int64_t wave_sum_up_to(int64_t x) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int64_t y = __shfl_up(x, o);
-    if (lane >= o) x += y;
-  }
-  return x;
-}
-
 // A value that all lanes of a wave have, as one the compiler knows to be so.
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ int64_t uniform64(int64_t x) { return (int64_t)(((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32) | (uint32_t)uniform((int)x)); }
-
 // The lowest n bits (none if n < 0, all if n > 31).
 __device__ __forceinline__ unsigned first_bits(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1; }
 
@@ -175,15 +163,23 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
       in_lds = (kEven ? lane / kRowChunks * kPitch + n * (kRowsApart * kPitch) : row * kPitch) + in_row * (16 / kBytes);
     }
   };
-  __shared__ __attribute__((aligned(16))) __bf16 tiles[kWaves][kTile * kPitch];
-  __shared__ bf16x8 q[kSubs][D / 16][64];
-  __shared__ f32x4 partial[kParts == 2 ? kWaves : 1][4][64];  // scores of a wave's dimensions
+  struct Walk {
+    __bf16 tiles[kWaves][kTile * kPitch];
+    bf16x8 q[kSubs][D / 16][64];
+    f32x4 partial[kParts == 2 ? kWaves : 1][kParts == 2 ? 4 : 1][kParts == 2 ? 64 : 1];  // scores of a wave's dimensions
+  };
+  __shared__ union __attribute__((aligned(16))) Pool {
+    Walk walk;
+    f32x4 values[kWaves][kDims * 4][64];  // the waves' results, when they are put together
+    __device__ Pool() {}
+  } pool;
+  auto& tiles = pool.walk.tiles;
+  auto& q = pool.walk.q;
+  auto& partial = pool.walk.partial;
   __shared__ float maxima[kWaves][kRows], sums[kWaves][kRows];
-  __shared__ int64_t wave_units[kWaves];
-  __shared__ int64_t start_unit;
-  __shared__ int start_seq;
+  __shared__ uint32_t wave_units[kWaves];
+  __shared__ int start_seq, start_unit;
   __shared__ Sequence in_lds[kThreads];  // where there are no more than threads
-  static_assert(sizeof(tiles) >= 2 * kRows * kOwn * 4, "two waves' values find room");
 
   const int head = blockIdx.x % a.heads, share = blockIdx.x / a.heads;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
@@ -192,30 +188,31 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
   // ---- the share: units first .. last - 1 of all ----
   const int each = (a.num_seqs + kThreads - 1) / kThreads;
   const int seq0 = min((int)threadIdx.x * each, a.num_seqs), seq1 = min(seq0 + each, a.num_seqs);
-  int64_t mine = 0;
+  // (sums that stay at their largest: starts of rows that do not increase may make them too large, and the share is then of some of the units)
+  uint32_t mine = 0;
   for (int i = seq0; i < seq1; ++i) {
     const Sequence s = sequence_at(a, i);
     if (each == 1) in_lds[i] = s;
-    mine += s.units(a.most_subs);
+    mine = sum_at_most(mine, s.units(a.most_subs));
   }
-  int64_t before = wave_sum_up_to(mine);
-  if (lane == 63) wave_units[wave] = before;
+  const uint32_t up_to = wave_sum_up_to(mine);
+  uint32_t before = (uint32_t)__shfl_up((int)up_to, 1);
+  if (lane == 0) before = 0;
+  if (lane == 63) wave_units[wave] = up_to;
   if (threadIdx.x == 0) start_seq = -1;
-  before -= mine;
   __syncthreads();
-  int64_t total = 0;
+  uint32_t all = 0;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
-    if (w < wave) before += wave_units[w];
-    total += wave_units[w];
+    if (w < wave) before = sum_at_most(before, wave_units[w]);
+    all = sum_at_most(all, wave_units[w]);
   }
-  const int64_t size = uniform64(max((int64_t)1, (total + a.shares - 1) / a.shares));
-  const int64_t first = share * size, last = uniform64(min(first + size, total));
-  if (first >= before && first < before + mine) {
-    int64_t at = first - before;
-    int i = seq0;
+  const int total = uniform((int)min(all, 1u << 30)), size = max(1, a.by_shares(total + a.shares - 1));
+  const int first = (int)min((int64_t)share * size, (int64_t)total), last = min(first + size, total);
+  if ((uint32_t)first >= before && (uint32_t)first < sum_at_most(before, mine)) {
+    int at = first - (int)before, i = seq0;
     while (each > 1) {
-      const int64_t u = sequence_at(a, i).units(a.most_subs);
+      const int u = sequence_at(a, i).units(a.most_subs);
       if (at < u) break;
       at -= u;
       ++i;
@@ -224,15 +221,14 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
     start_unit = at;
   }
   __syncthreads();
-  int seq = uniform(start_seq);
+  int seq = uniform(start_seq), in_seq = uniform(start_unit);  // units of the sequence before the next
   if (threadIdx.x == 0 && head == 0) a.cuts[share * kCut + kCutRows] = 0;
   if (seq < 0 || first >= total) return;
-  int64_t in_seq = uniform64(start_unit);  // units of the sequence before the next
   const float k_scale = E4M3 ? a.k_scale[head] : 1.f, v_scale = E4M3 ? a.v_scale[head] : 1.f;
   const float scale = a.scale_log2 * k_scale;
   const char *const k_base = (const char*)a.k + part * kOwnBytes, *const v_base = (const char*)a.v + part * kOwnBytes;
 
-  for (int64_t unit = first; unit < last;) {
+  for (int unit = first; unit < last;) {
     Sequence s = each == 1 ? in_lds[seq] : sequence_at(a, seq);
     s = Sequence{uniform(s.len), uniform(s.rows), uniform(s.first_row)};
     if (s.rows == 0 || in_seq >= s.units(a.most_subs)) {
@@ -241,8 +237,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
       continue;
     }
     const int key_blocks = s.key_blocks();
-    const int row_block = (int)(in_seq / key_blocks), block0 = (int)(in_seq - (int64_t)row_block * key_blocks);
-    const int block1 = (int)min((int64_t)key_blocks, block0 + (last - unit));
+    const int row_block = in_seq < key_blocks ? 0 : (int)((unsigned)in_seq / (unsigned)key_blocks), block0 = in_seq - row_block * key_blocks;
+    const int block1 = min(key_blocks, block0 + (last - unit));
     // rows of this lane's column
     // Waves: `part` of the dimensions, `sub` of the block's rows, and `team`, which takes every teams-th tile.  (Waves of one team load the same tile at about the same time, so that it
     // comes from memory once.)
@@ -513,72 +509,40 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
 #pragma unroll
     for (int t = 0; t < kDims; ++t)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) acc[t][e] *= f;
-    f32x4* const given = reinterpret_cast<f32x4*>(&tiles[0][0]);
-    auto give = [&](int to) {
-#pragma unroll
-      for (int t = 0; t < kDims; ++t)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) given[(to * kDims * 4 + t * 4 + g) * 64 + lane] = f32x4{acc[t][4 * g], acc[t][4 * g + 1], acc[t][4 * g + 2], acc[t][4 * g + 3]};
-    };
-    auto take = [&](int from) {
-#pragma unroll
-      for (int t = 0; t < kDims; ++t)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const f32x4 x = given[(from * kDims * 4 + t * 4 + g) * 64 + lane];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[t][4 * g + e] += x[e];
-        }
-    };
-    if (teams >= 2) {
-      if (wave >= 2) give(wave - 2);
-      __syncthreads();
-      if (wave < 2) take(wave);
-    }
-    if (teams == 4) {
-      __syncthreads();
-      if (wave == 1) give(0);
-      __syncthreads();
-      if (wave == 0) take(0);
-    }
-    if (team == 0) {
-      if (block0 == 0 && block1 == key_blocks) {
-        if (live) {
-          const float inv = sum > 0.f || sum != sum ? v_scale / sum : 0.f;
-          __bf16* const to = a.o + (int64_t)q_row * a.o_stride + (int64_t)q_head * D + part * kOwn + 4 * half;
-#pragma unroll
-          for (int t = 0; t < kDims; ++t)
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-              struct __attribute__((packed, aligned(2))) Loose4 {
-                bf16x4 x;
-              };
-              reinterpret_cast<Loose4*>(to + 32 * t + 8 * g)->x = pack4(acc[t][4 * g] * inv, acc[t][4 * g + 1] * inv, acc[t][4 * g + 2] * inv, acc[t][4 * g + 3] * inv);
-            }
-          if (a.lse && half == 0 && part == 0) a.lse[(int64_t)q_head * a.total_q + q_row] = sum > 0.f || sum != sum ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
-        }
-      } else {
-        float* const into = a.parts + (((int64_t)(share * 2 + (block0 == 0)) * a.heads + head) * a.most_subs + sub) * part_floats<D>();
-        if (live) {
-#pragma unroll
-          for (int t = 0; t < kDims; ++t)
-#pragma unroll
-            for (int g = 0; g < 4; ++g)
-              *reinterpret_cast<f32x4*>(into + col * D + part * kOwn + 32 * t + 8 * g + 4 * half) = f32x4{acc[t][4 * g], acc[t][4 * g + 1], acc[t][4 * g + 2], acc[t][4 * g + 3]};
-          if (half == 0 && part == 0) {
-            into[kRows * D + col] = top;
-            into[kRows * D + kRows + col] = sum;
-          }
-        }
-        if (lane == 0 && wave == 0 && head == 0 && block0 == 0) {
-          const int row = row_block * subs * kRows;
-          a.cuts[share * kCut + kCutSeqRow] = s.first_row;
-          a.cuts[share * kCut + kCutRow] = row;
-          a.cuts[share * kCut + kCutRows] = min(subs * kRows, s.rows - row);
-          a.cuts[share * kCut + kCutShares] = (int)((unit + key_blocks - 1) / size) - share + 1;
+      for (int g = 0; g < 4; ++g) pool.values[wave][4 * t + g][lane] = f32x4{acc[t][4 * g] * f, acc[t][4 * g + 1] * f, acc[t][4 * g + 2] * f, acc[t][4 * g + 3] * f};
+    __syncthreads();
+    // quarter u of the lane's row: dimensions 8 u + 4 half .. + 3 of the wave's; each team's wave sums up every teams-th
+    const bool cut = block0 != 0 || block1 != key_blocks, some = sum > 0.f || sum != sum;
+    float* const into = a.parts + (((int64_t)(share * 2 + (block0 == 0)) * a.heads + head) * a.most_subs + sub) * part_floats<D>();
+    if (live) {
+      const float inv = some ? v_scale / sum : 0.f;
+      __bf16* const to = a.o + (int64_t)q_row * a.o_stride + (int64_t)q_head * D + part * kOwn + 4 * half;
+      float* const to_part = into + col * D + part * kOwn + 4 * half;
+#pragma unroll 4
+      for (int u = team; u < 4 * kDims; u += teams) {
+        f32x4 x = pool.values[sub * kParts + part][u][lane];
+        for (int w = 1; w < teams; ++w) x += pool.values[(w * subs + sub) * kParts + part][u][lane];
+        struct __attribute__((packed, aligned(2))) Loose4 {
+          bf16x4 x;
+        };
+        if (cut) *reinterpret_cast<f32x4*>(to_part + 8 * u) = x;
+        else reinterpret_cast<Loose4*>(to + 8 * u)->x = pack4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
+      }
+      if (team == 0 && part == 0 && half == 0) {
+        if (cut) {
+          into[kRows * D + col] = top;
+          into[kRows * D + kRows + col] = sum;
+        } else if (a.lse) {
+          a.lse[(int64_t)q_head * a.total_q + q_row] = some ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
         }
       }
+    }
+    if (cut && block0 == 0 && threadIdx.x == 0 && head == 0) {
+      const int row = row_block * subs * kRows;
+      a.cuts[share * kCut + kCutSeqRow] = s.first_row;
+      a.cuts[share * kCut + kCutRow] = row;
+      a.cuts[share * kCut + kCutRows] = min(subs * kRows, s.rows - row);
+      a.cuts[share * kCut + kCutShares] = (int)((unsigned)(unit + key_blocks - 1) / (unsigned)size) - share + 1;
     }
     __syncthreads();
     unit += block1 - block0;
@@ -696,6 +660,11 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const AttnArgs a, const 
 }
 
 // ---- host ----
+// Units of a key/value head, at most.
+int64_t most_units(const paged_attn_desc* d) {
+  const int64_t rows = (int64_t)d->total_q * (d->num_q_heads / d->num_kv_heads);
+  return std::min((int64_t)d->num_seqs + rows / kRows, std::max<int64_t>(rows, 1)) * (((int64_t)d->max_pages * d->page_size + kBlockKeys - 1) / kBlockKeys);
+}
 int check_desc(const paged_attn_desc* d) {
   if (!d || d->num_q_heads < 1 || d->num_kv_heads < 1 || d->num_seqs < 1 || d->total_q < 0 || d->page_size < 1 || d->num_pages < 1 || d->max_pages < 1 ||
       (d->cache_type != PAGED_CACHE_BF16 && d->cache_type != PAGED_CACHE_E4M3) || !finite_number(d->softmax_scale) || d->softmax_scale <= 0.f)
@@ -705,16 +674,14 @@ int check_desc(const paged_attn_desc* d) {
     return CHUNK_ATTN_UNSUPPORTED;
   // (products of three are formed of factors below 2^31 and 2^30)
   if ((int64_t)d->total_q * d->num_q_heads > INT32_MAX || (int64_t)d->max_pages * d->page_size > 1 << 30 ||
-      (int64_t)d->num_pages * d->page_size > INT32_MAX / d->num_kv_heads)
+      (int64_t)d->num_pages * d->page_size > INT32_MAX / d->num_kv_heads || most_units(d) > 1 << 30)
     return CHUNK_ATTN_INVALID_ARG;
   return CHUNK_ATTN_OK;
 }
 // Workgroups for each key/value head: two to a compute unit, and no more than there can be shares.
 int count_shares(const paged_attn_desc* d) {
-  const int64_t most_keys = (int64_t)d->max_pages * d->page_size, group = d->num_q_heads / d->num_kv_heads;
-  const int64_t blocks = std::min<int64_t>((int64_t)d->num_seqs + d->total_q * group / kRows, std::max<int64_t>(d->total_q * group, 1)) * ((most_keys + kBlockKeys - 1) / kBlockKeys);
   const int64_t fill = (kMostShares + d->num_kv_heads - 1) / d->num_kv_heads;
-  return (int)std::max<int64_t>(1, std::min<int64_t>(fill, blocks));
+  return (int)std::max<int64_t>(1, std::min(fill, most_units(d)));
 }
 int count_subs(const paged_attn_desc* d) {
   const int64_t rows = (int64_t)d->total_q * (d->num_q_heads / d->num_kv_heads);
@@ -763,7 +730,7 @@ extern "C" int paged_attn_fwd(const paged_attn_desc* d, const void* q, int64_t q
   const int heads = d->num_kv_heads, group = d->num_q_heads / heads, shares = count_shares(d);
   const AttnArgs a{(const __bf16*)q, q_stride, k_cache, v_cache, e4m3 ? k_scale : nullptr, e4m3 ? v_scale : nullptr, table, kv_len, q_start, (__bf16*)o, o_stride, lse,
                    (float*)workspace, (int32_t*)((char*)workspace + part_bytes(d)), d->num_seqs, d->total_q, heads, group, d->page_size, d->num_pages, d->max_pages, shares, count_subs(d),
-                   d->softmax_scale * kLog2e, Divide(d->page_size), Divide(group)};
+                   d->softmax_scale * kLog2e, Divide(d->page_size), Divide(group), Divide(shares)};
   const hipStream_t stream = (hipStream_t)hip_stream;
   const hipError_t e = by_dim(d->head_dim, [&](auto dim) {
     constexpr int D = decltype(dim)::value;

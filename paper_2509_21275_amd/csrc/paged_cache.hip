@@ -39,28 +39,16 @@ enum { kPagesBefore, kOldLen, kHeld, kSums };
 // Behind them: pages that change hands, pages on the stack before the call.
 enum { kMoved, kOnStack, kTotals };
 
-// Sums that stay at the largest number once they are there: whatever the inputs are, what is below 2^32 - 1 is right, and nothing larger is used.
-__device__ __forceinline__ uint32_t add(uint32_t x, uint32_t y) { return __builtin_elementwise_add_sat(x, y); }
-// Sum over the lanes up to the own one: within rows of 16 lanes, then from row to row.
-__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
-  x = add(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, false));  // from 1, 2, 4 and 8 lanes before
-  x = add(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, false));
-  x = add(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, false));
-  x = add(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, false));
-  x = add(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false));  // the last lane of the row before, to rows 1 and 3
-  x = add(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false));  // lane 31 to rows 2 and 3
-  return x;
-}
 // Sum over the threads before the own one; `room`: one number for each wave, used by no other sum.
 __device__ __forceinline__ uint32_t sum_before(uint32_t x, uint32_t* room) {
-  const uint32_t up_to = wave_scan(x);
+  const uint32_t up_to = wave_sum_up_to(x);
   uint32_t before = (uint32_t)__shfl_up((int)up_to, 1);
   if ((threadIdx.x & 63) == 0) before = 0;
   if ((threadIdx.x & 63) == 63) room[threadIdx.x >> 6] = up_to;
   __syncthreads();
   const int wave = threadIdx.x >> 6;
 #pragma unroll
-  for (int w = 0; w < kScanThreads / 64; ++w) before = add(before, w < wave ? room[w] : 0);
+  for (int w = 0; w < kScanThreads / 64; ++w) before = sum_at_most(before, w < wave ? room[w] : 0);
   return before;
 }
 __device__ __forceinline__ int at_most(uint32_t x, int most) { return (int)min(x, (uint32_t)most); }
@@ -185,28 +173,28 @@ __global__ __launch_bounds__(kScanThreads) void tables_kernel(const TableArgs a)
   // rows first: who does not fit in them has no claim on pages
   uint32_t rows = 0, pages = 0;
   if (EXTEND) {
-    each_request([&](int, const Request& r) { rows = add(rows, r.change); });
+    each_request([&](int, const Request& r) { rows = sum_at_most(rows, r.change); });
     rows = sum_before(rows, room[0]);
   }
   uint32_t row = rows;
   each_request([&](int, const Request& r) {
-    row = add(row, r.change);
-    if (!EXTEND || r.change == 0 || row <= (uint32_t)a.max_rows) pages = add(pages, r.need);
+    row = sum_at_most(row, r.change);
+    if (!EXTEND || r.change == 0 || row <= (uint32_t)a.max_rows) pages = sum_at_most(pages, r.need);
   });
   pages = sum_before(pages, room[1]);
   row = rows;
   int mine = 0;
   Outcome outcome[EACH ? EACH : 1];
   each_request([&](int i, const Request& r) {
-    const uint32_t end = add(row, r.change);
+    const uint32_t end = sum_at_most(row, r.change);
     const bool in_rows = !EXTEND || r.change == 0 || end <= (uint32_t)a.max_rows;
     const int need = in_rows ? r.need : 0;
-    const bool served = r.fits && in_rows && (!EXTEND || need == 0 || add(pages, need) <= (uint32_t)on_stack);
+    const bool served = r.fits && in_rows && (!EXTEND || need == 0 || sum_at_most(pages, need) <= (uint32_t)on_stack);
     Outcome o;
     o.start = at_most(row, a.max_rows);
     o.end = at_most(end, a.max_rows);
     o.pages_before = at_most(pages, INT32_MAX);
-    pages = add(pages, need);
+    pages = sum_at_most(pages, need);
     if (served && need > 0) mine = at_most(pages, INT32_MAX);  // (the sums grow: those that are served are the first of those that need pages)
     row = end;
     o.old_len = served ? r.old_len : -1;
@@ -243,9 +231,9 @@ __global__ __launch_bounds__(kScanThreads) void tables_kernel(const TableArgs a)
     // fill_kernel's workgroups begin to look for their rows' requests where the first row's slot will be
     row = rows;
     each_request([&](int i, const Request& r) {
-      const int64_t end = min(add(row, r.change), (uint32_t)a.max_rows);
+      const int64_t end = min(sum_at_most(row, r.change), (uint32_t)a.max_rows);
       for (int64_t at = ((int64_t)row + kFillThreads - 1) / kFillThreads * kFillThreads; at < end; at += kFillThreads) a.slots[at] = i;
-      row = add(row, r.change);
+      row = sum_at_most(row, r.change);
     });
   }
   if (mine > 0) atomicMax(&moved, mine);
