@@ -34,7 +34,7 @@ extern "C" {
 #define DRAFT_VERIFY_MAX_DRAFTS 64
 #define DRAFT_VERIFY_MAX_VOCAB (1 << 24)
 
-/* batch >= 0, max_drafts 0 .. DRAFT_VERIFY_MAX_DRAFTS and vocab 1 .. DRAFT_VERIFY_MAX_VOCAB (above: CHUNK_ATTN_UNSUPPORTED), batch * vocab < 2^38. */
+/* batch 0 .. 2^23 - 1, max_drafts 0 .. DRAFT_VERIFY_MAX_DRAFTS and vocab 1 .. DRAFT_VERIFY_MAX_VOCAB (above: CHUNK_ATTN_UNSUPPORTED), batch * vocab < 2^36. */
 int draft_verify_workspace_bytes(int32_t batch, int32_t max_drafts, int32_t vocab, size_t* bytes);
 
 int draft_verify(int32_t batch, int32_t max_drafts, int32_t vocab, int32_t probabilities_are_f32, const void* target, int64_t target_stride, const void* draft,

@@ -276,7 +276,7 @@ __global__ __launch_bounds__(kThreads) void choose_kernel(const VerifyArgs<T> a)
 }
 
 int check_sizes(int32_t batch, int32_t max_drafts, int32_t vocab) {
-  if (batch < 0 || max_drafts < 0 || vocab < 1 || (int64_t)batch * vocab >= (int64_t)1 << 38) return CHUNK_ATTN_INVALID_ARG;
+  if (batch < 0 || max_drafts < 0 || vocab < 1 || batch >= 1 << 23 || (int64_t)batch * vocab >= (int64_t)1 << 36) return CHUNK_ATTN_INVALID_ARG;  // (threads of a launch: below 2^32)
   return max_drafts > DRAFT_VERIFY_MAX_DRAFTS || vocab > DRAFT_VERIFY_MAX_VOCAB ? CHUNK_ATTN_UNSUPPORTED : CHUNK_ATTN_OK;
 }
 int count_granules(int32_t vocab) { return (vocab + kGranule - 1) / kGranule; }

@@ -62,13 +62,14 @@ template <int D>
 constexpr int part_floats() { return kRows * (D + 2); }
 
 // Sequence i, its numbers brought into their ranges.
+static_assert(kRows == 1 << 5);
 struct Sequence {
   int len, rows, first_row;  // tokens; rows of a key/value head; first row of q
-  // groups of kRows rows that walk over the keys together: 1, 2 or 4 (`most` at most)
-  __device__ int subs(int most) const { return rows <= kRows ? 1 : rows <= 2 * kRows ? min(2, most) : most; }
+  // groups of kRows rows that walk over the keys together: 1, 2 or 4 (`most` at most), as the logarithm
+  __device__ int log_subs(int most) const { return rows <= kRows || most == 1 ? 0 : rows <= 2 * kRows ? 1 : 2; }
   __device__ int row_blocks(int most) const {
-    const int n = kRows * subs(most);
-    return (rows + n - 1) / n;
+    const int log = 5 + log_subs(most);
+    return (rows + (1 << log) - 1) >> log;
   }
   __device__ int key_blocks() const { return max(1, (int)(((unsigned)len + kBlockKeys - 1) / kBlockKeys)); }
   __device__ int units(int most) const { return row_blocks(most) * key_blocks(); }  // < 2^30 (check_desc)
@@ -84,6 +85,12 @@ __device__ __forceinline__ Sequence sequence_at(const AttnArgs& a, int i) {
 
 // A value that all lanes of a wave have, as one the compiler knows to be so.
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+// A barrier that what this wave wrote to LDS is there before, but that waits for no loads from memory.
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+  wg_barrier();
+}
 // The lowest n bits (none if n < 0, all if n > 31).
 __device__ __forceinline__ unsigned first_bits(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1; }
 
@@ -242,12 +249,12 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
     // rows of this lane's column
     // Waves: `part` of the dimensions, `sub` of the block's rows, and `team`, which takes every teams-th tile.  (Waves of one team load the same tile at about the same time, so that it
     // comes from memory once.)
-    const int subs = s.subs(a.most_subs), sub = wave / kParts % subs, team = wave / kParts / subs, teams = kWaves / kParts / subs;
+    const int log_subs = s.log_subs(a.most_subs), subs = 1 << log_subs, sub = wave / kParts & (subs - 1), team = wave / kParts >> log_subs, teams = kWaves / kParts >> log_subs;
     const int row0 = min((row_block * subs + sub) * kRows, s.rows - 1);
     const int row = (row_block * subs + sub) * kRows + col;
     const bool live = row < s.rows;
     const int token = a.by_group(min(row, s.rows - 1)), q_row = s.first_row + token, q_head = head * a.group + min(row, s.rows - 1) - token * a.group;
-    const int tokens = s.rows / a.group;
+    const int tokens = a.by_group(s.rows);
     const int seen = s.len - tokens + token + 1;  // keys that the row sees (none if <= 0)
     const int first_seen = s.len - tokens + a.by_group(row0) + 1;                               // of the first row,
     const int most_seen = max(0, s.len - tokens + a.by_group(min(row0 + kRows, s.rows) - 1) + 1);  // and of the last
@@ -329,17 +336,15 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
     };
     __bf16* const v_tile = tiles[wave];
     int tile = block0 * kWaves + team;
-    static_for<0, kAhead>([&](auto slot) {
-      places[decltype(slot)::value] = find(tile + decltype(slot)::value * teams);
-      load_tile(slot);
-    });
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) places[i] = find(tile + i * teams);
     next = find(tile + kAhead * teams);
+    static_for<0, kAhead>([&](auto slot) { load_tile(slot); });
     // queries to LDS, in the order in which the lanes read them (in registers they would leave too few for the loads ahead); the tiles' loads go on
 #pragma unroll
     for (int i = 0; i < kLoads; ++i)
       if (i * sharers + first_q < D / 16) q[sub][i * sharers + first_q][lane] = live ? own_q[i] : bf16x8{};
-    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
-    wg_barrier();
+    lds_barrier();
     // (waves that share a tile's dimensions all go on to the last tile of any, as they wait for each other)
     auto more = [&]() { return kParts == 1 ? tile < tile1 : tile - team < tile1; };
     auto step = [&](auto slot) {
@@ -391,8 +396,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
         wg_barrier();  // (the last tile's have been read: their sums were used)
 #pragma unroll
         for (int g = 0; g < 4; ++g) partial[wave][g][lane] = f32x4{score[4 * g], score[4 * g + 1], score[4 * g + 2], score[4 * g + 3]};
-        __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): what this wave wrote is there; its loads go on
-        wg_barrier();
+        lds_barrier();
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
           const f32x4 x = partial[wave ^ 1][g][lane];
@@ -501,10 +505,10 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
     float top = kFloor, sum = 0.f;
 #pragma unroll
     for (int w = 0; w < kWaves; w += kParts)
-      if (w / kParts % subs == sub) top = fmaxf(top, maxima[w][col]);
+      if ((w / kParts & (subs - 1)) == sub) top = fmaxf(top, maxima[w][col]);
 #pragma unroll
     for (int w = 0; w < kWaves; w += kParts)
-      if (w / kParts % subs == sub) sum += sums[w][col] * __builtin_amdgcn_exp2f(maxima[w][col] - top);
+      if ((w / kParts & (subs - 1)) == sub) sum += sums[w][col] * __builtin_amdgcn_exp2f(maxima[w][col] - top);
     const float f = __builtin_amdgcn_exp2f(m - top);
 #pragma unroll
     for (int t = 0; t < kDims; ++t)
@@ -518,16 +522,24 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
       const float inv = some ? v_scale / sum : 0.f;
       __bf16* const to = a.o + (int64_t)q_row * a.o_stride + (int64_t)q_head * D + part * kOwn + 4 * half;
       float* const to_part = into + col * D + part * kOwn + 4 * half;
-#pragma unroll 4
-      for (int u = team; u < 4 * kDims; u += teams) {
-        f32x4 x = pool.values[sub * kParts + part][u][lane];
-        for (int w = 1; w < teams; ++w) x += pool.values[(w * subs + sub) * kParts + part][u][lane];
-        struct __attribute__((packed, aligned(2))) Loose4 {
-          bf16x4 x;
-        };
-        if (cut) *reinterpret_cast<f32x4*>(to_part + 8 * u) = x;
-        else reinterpret_cast<Loose4*>(to + 8 * u)->x = pack4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
-      }
+      auto put = [&](auto number) {
+        constexpr int TEAMS = decltype(number)::value;
+#pragma unroll
+        for (int i = 0; i < 4 * kDims / TEAMS; ++i) {
+          const int u = i * TEAMS + team;
+          f32x4 x = pool.values[sub * kParts + part][u][lane];
+#pragma unroll
+          for (int w = 1; w < TEAMS; ++w) x += pool.values[(w * subs + sub) * kParts + part][u][lane];
+          struct __attribute__((packed, aligned(2))) Loose4 {
+            bf16x4 x;
+          };
+          if (cut) *reinterpret_cast<f32x4*>(to_part + 8 * u) = x;
+          else reinterpret_cast<Loose4*>(to + 8 * u)->x = pack4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
+        }
+      };
+      if (teams == 4) put(std::integral_constant<int, 4>{});
+      else if (teams == 2) put(std::integral_constant<int, 2>{});
+      else put(std::integral_constant<int, 1>{});
       if (team == 0 && part == 0 && half == 0) {
         if (cut) {
           into[kRows * D + col] = top;

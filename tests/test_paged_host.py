@@ -122,7 +122,7 @@ def test_verify_refusals(ca):
 
     for kw in (dict(batch=-1), dict(K=-1), dict(V=0), dict(target=None), dict(target=P + 2), dict(ts=999), dict(draft=P + 2), dict(ds=0), dict(tokens=None), dict(tokens=P + 2),
                dict(count=P + 1), dict(u=None), dict(u=P + 2), dict(last=None), dict(last=P + 1), dict(accepted=None), dict(accepted=P + 2), dict(rejected=P + 1), dict(out=None),
-               dict(out=P + 2), dict(ws=None), dict(ws=P + 8), dict(f32=0, target=P + 1), dict(batch=2**20, V=2**18)):
+               dict(out=P + 2), dict(ws=None), dict(ws=P + 8), dict(f32=0, target=P + 1), dict(batch=2**20, V=2**18), dict(batch=2**23, V=10)):
         assert run(**kw) == ca.INVALID_ARG, kw
     assert run(K=65) == ca.UNSUPPORTED and run(V=2**24 + 1, ts=2**25, ds=2**25) == ca.UNSUPPORTED
     assert run(size=size - 1) == ca.WORKSPACE_TOO_SMALL and run(batch=0, target=None, ws=None) == ca.OK
