@@ -158,7 +158,6 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
   constexpr int kRowBytes = D * kBytes, kOwnBytes = kOwn * kBytes;
   constexpr int kRowChunks = kOwnBytes / 16, kVChunks = kRowChunks / 2;  // 16-byte chunks of a wave's part of a row; of a tile, for each lane
   using Value = std::conditional_t<E4M3, _Float16, __bf16>;  // of V in LDS
-  constexpr int kAhead = E4M3 ? 2 : 1;                  // tiles that are loaded ahead
   constexpr bool kEven = 64 % kRowChunks == 0;          // a wave's 16-byte loads are whole rows
   constexpr int kRowsApart = kEven ? 64 / kRowChunks : 0;
   // The n-th 16 bytes of a tile's V that a lane has: key, place in the row, place in LDS.
@@ -273,8 +272,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
     // ---- the walk ----
     const int tile1 = min(block1 * kWaves, (int)(((unsigned)most_seen + kTile - 1) / kTile));
     const int32_t* const pages = a.table + (int64_t)seq * a.max_pages;
-    u32x4 kr[kAhead][kDims * kBytes], vr[kAhead][kVChunks];
-    Place<HALVES> places[kAhead], next;
+    u32x4 kr[kDims * kBytes], vr[kVChunks];
+    Place<HALVES> at, next;
     auto find = [&](int tile) {
       Place<HALVES> r;
       if constexpr (HALVES) {
@@ -292,9 +291,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
       return r;
     };
     // Starts the loads of a tile; afterwards at.there says which of its keys there are.
-    auto load_tile = [&](auto slot) {
-      constexpr int S = decltype(slot)::value;
-      Place<HALVES>& at = places[S];
+    auto load_tile = [&]() {
       if constexpr (HALVES) {
         int rows[2];
         bool ok[2];
@@ -309,14 +306,14 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
 #pragma unroll
         for (int t = 0; t < kDims; ++t)
 #pragma unroll
-          for (int u = 0; u < kBytes; ++u) kr[S][t * kBytes + u] = load16(p + t * (32 * kBytes) + u * 16);
+          for (int u = 0; u < kBytes; ++u) kr[t * kBytes + u] = load16(p + t * (32 * kBytes) + u * 16);
         const char* const from[2] = {v_base + (int64_t)rows[0] * kRowBytes, v_base + (int64_t)rows[1] * kRowBytes};
 #pragma unroll
         for (int n = 0; n < kVChunks; ++n) {
           // (where a wave's loads are whole rows, the n-th is of one half)
           const Chunk c(lane, n);
-          if constexpr (kEven && kRowsApart <= 16) vr[S][n] = load16(from[n * kRowsApart / 16] + (unsigned)(lane / kRowChunks * kRowBytes + c.in_row * 16) + (n * kRowsApart % 16) * kRowBytes);
-          else vr[S][n] = load16((c.row & 16 ? from[1] : from[0]) + (c.row & 15) * kRowBytes + c.in_row * 16);
+          if constexpr (kEven && kRowsApart <= 16) vr[n] = load16(from[n * kRowsApart / 16] + (unsigned)(lane / kRowChunks * kRowBytes + c.in_row * 16) + (n * kRowsApart % 16) * kRowBytes);
+          else vr[n] = load16((c.row & 16 ? from[1] : from[0]) + (c.row & 15) * kRowBytes + c.in_row * 16);
         }
       } else {
         const bool ok = at.number >= 0 && at.number < a.num_pages;
@@ -326,20 +323,19 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
 #pragma unroll
         for (int t = 0; t < kDims; ++t)
 #pragma unroll
-          for (int u = 0; u < kBytes; ++u) kr[S][t * kBytes + u] = load16(p + t * (32 * kBytes) + u * 16);
+          for (int u = 0; u < kBytes; ++u) kr[t * kBytes + u] = load16(p + t * (32 * kBytes) + u * 16);
 #pragma unroll
         for (int n = 0; n < kVChunks; ++n) {
           const Chunk c(lane, n);
-          vr[S][n] = load16(v_base + (int64_t)__shfl(row, c.row) * kRowBytes + c.in_row * 16);
+          vr[n] = load16(v_base + (int64_t)__shfl(row, c.row) * kRowBytes + c.in_row * 16);
         }
       }
     };
     __bf16* const v_tile = tiles[wave];
     int tile = block0 * kWaves + team;
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) places[i] = find(tile + i * teams);
-    next = find(tile + kAhead * teams);
-    static_for<0, kAhead>([&](auto slot) { load_tile(slot); });
+    at = find(tile);
+    next = find(tile + teams);
+    load_tile();
     // queries to LDS, in the order in which the lanes read them (in registers they would leave too few for the loads ahead); the tiles' loads go on
 #pragma unroll
     for (int i = 0; i < kLoads; ++i)
@@ -347,9 +343,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
     lds_barrier();
     // (waves that share a tile's dimensions all go on to the last tile of any, as they wait for each other)
     auto more = [&]() { return kParts == 1 ? tile < tile1 : tile - team < tile1; };
-    auto step = [&](auto slot) {
-      constexpr int S = decltype(slot)::value;
-      Place<HALVES>& at = places[S];
+    auto step = [&]() {
       // bit k: key k of the tile is there and seen by a row of the block; is seen by this lane's row
       const unsigned keys = at.there & first_bits(most_seen - tile * kTile), visible = at.there & first_bits(seen - tile * kTile);
       const bool border = (tile + 1) * kTile > first_seen || at.there != 0xffffffffu;
@@ -363,8 +357,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
           const int row = kEven ? n * kRowsApart : Chunk(lane, n).row;  // (less first_row)
           const bool there = mine & (1u << row);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) vr[S][n][e] = there ? vr[S][n][e] : 0;
-          odd |= some_not_finite<E4M3>(vr[S][n]) ? 1u << row : 0u;
+          for (int e = 0; e < 4; ++e) vr[n][e] = there ? vr[n][e] : 0;
+          odd |= some_not_finite<E4M3>(vr[n]) ? 1u << row : 0u;
         }
         odd <<= first_row;
       }
@@ -372,10 +366,10 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
       for (int n = 0; n < kVChunks; ++n) {
         __bf16* const to = v_tile + Chunk(lane, n).in_lds;
         if constexpr (E4M3) {
-          *reinterpret_cast<f16x8*>(to) = widen8_f16(vr[S][n][0], vr[S][n][1]);
-          *reinterpret_cast<f16x8*>(to + 8) = widen8_f16(vr[S][n][2], vr[S][n][3]);
+          *reinterpret_cast<f16x8*>(to) = widen8_f16(vr[n][0], vr[n][1]);
+          *reinterpret_cast<f16x8*>(to + 8) = widen8_f16(vr[n][2], vr[n][3]);
         } else {
-          *reinterpret_cast<u32x4*>(to) = vr[S][n];
+          *reinterpret_cast<u32x4*>(to) = vr[n];
         }
       }
       // scores
@@ -383,14 +377,14 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
 #pragma unroll
       for (int n = 0; n < 2 * kDims; ++n) {
         bf16x8 x;
-        if constexpr (E4M3) x = n & 1 ? widen8(kr[S][n >> 1][2], kr[S][n >> 1][3]) : widen8(kr[S][n >> 1][0], kr[S][n >> 1][1]);
-        else x = __builtin_bit_cast(bf16x8, kr[S][n]);
+        if constexpr (E4M3) x = n & 1 ? widen8(kr[n >> 1][2], kr[n >> 1][3]) : widen8(kr[n >> 1][0], kr[n >> 1][1]);
+        else x = __builtin_bit_cast(bf16x8, kr[n]);
         score = mfma32(x, q[sub][part * 2 * kDims + n][lane], score);
       }
       // the next tile, and the page of the one after it (behind the last one: loads that nobody waits for, of a row that is there)
       at = next;
-      load_tile(slot);
-      next = find(tile + (kAhead + 1) * teams);
+      load_tile();
+      next = find(tile + 2 * teams);
       __builtin_amdgcn_sched_barrier(0);
       if constexpr (kParts == 2) {  // the other half of the dimensions
         wg_barrier();  // (the last tile's have been read: their sums were used)
@@ -487,13 +481,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
       }
       tile += teams;
     };
-    while (more()) {
-      step(std::integral_constant<int, 0>{});
-      if constexpr (kAhead == 2) {
-        if (!more()) break;
-        step(std::integral_constant<int, kAhead - 1>{});
-      }
-    }
+    while (more()) step();
 
     // ---- the waves' results together ----
     l = sum_halves(l);
