@@ -42,9 +42,12 @@ def whole(t, dtype, shape, name):
 
 def given(t, dtype, shape, name):
     """The same for a tensor that has to be there."""
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.shape == shape and t.is_contiguous()):
-        _refuse(name, dtype, shape, "contiguous ")
-    return t.data_ptr()
+    try:
+        if t.is_cuda and t.dtype is dtype and t.shape == shape and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:  # (not a tensor)
+        pass
+    _refuse(name, dtype, shape, "contiguous ")
 
 
 def room(workspace):

@@ -342,8 +342,10 @@ int run_tables(const paged_cache_desc* d, TableArgs a, void* workspace, size_t w
 }
 
 // ---- keys and values into the pages ----
-// Bound by memory: a thread takes eight elements of a row, of both tensors (two or four such pieces to a thread are slower, 88 and 93 us for the 87 below).
-constexpr int kWriteThreads = 256;
+// Bound by memory, as long as the vector work is kept small: with true divisions, and what belongs to a head found anew for each row, the vector units were busy for 97 % of the time.  A thread takes eight
+// elements of one place in a row, of both tensors, of ROWS rows that are `apart` rows from each other: one; two to e4m3 where the chip is full with that.  65536 rows of 8 heads of 128 out of wider rows, us,
+// one / two / four: e4m3 108 / 77 (5.2 TB/s) / 79, bf16 103 / 104 / 105; 16384 rows 30 / 20 / 21 and 27.6 / 29 / 31.
+constexpr int kWriteThreads = 256, kManyRows = 2;
 constexpr int64_t kStreamBytes = (int64_t)256 << 20;
 
 struct WriteArgs {
@@ -352,39 +354,46 @@ struct WriteArgs {
   const int64_t* slots;
   const float *k_scale, *v_scale;
   void *k_cache, *v_cache;
-  int64_t num_slots, pieces;  // pieces of eight elements in all rows
-  int32_t heads, head_pieces, row_pieces, page_size;
+  int64_t num_slots, pieces;  // pieces of eight elements in `apart` rows
+  int32_t rows, apart, heads, head_pieces, row_pieces, page_size;
   Divide by_row, by_head, by_page;
 };
 
-// Division by a head's scale.  x / s as x y + r y with y the nearest to 1 / s and r = x - (x y) s, which a fused multiply and add gives exactly: the nearest to the quotient, where nothing leaves
-// float32's normal range (equal to the division for 4 * 10^8 drawn pairs, and a third of its time).
+// Division by a head's scale.  x / s as q + r y with y the nearest to 1 / s, q = x y and r = x - q s, which a fused multiply and add gives exactly: the nearest to the quotient, where nothing
+// leaves float32's normal range (equal to the division for 4 * 10^8 drawn pairs).  Quotients past 1024 only have to stay past 448: q is kept to 1024, so that nothing becomes infinite less infinite.
 struct Scale {
   float s, y;
   bool usual;  // the quotient of anything by s that 8 bits hold is far from the ends of float32's range
   explicit __device__ Scale(float scale) : s(scale), y(1.f / scale), usual(scale > 0x1p-80f && scale < 0x1p80f) {}
   __device__ float divides(float x) const {
-    if (!usual) return x / s;
-    const float q = x * y;
-    return fabsf(q) < 1024.f ? __builtin_fmaf(__builtin_fmaf(-s, q, x), y, q) : q;
+    const float q = __builtin_amdgcn_fmed3f(x * y, -1024.f, 1024.f);
+    return __builtin_fmaf(__builtin_fmaf(-s, q, x), y, q);
   }
 };
+__device__ __forceinline__ float element(const u32x4& x, int e) { return __uint_as_float(e & 1 ? x[e >> 1] & 0xffff0000u : x[e >> 1] << 16); }
+// Eight bf16 numbers over the scale as e4m3.
 __device__ __forceinline__ u32x2 to_e4m3(const u32x4& x, const Scale& scale) {
+  unsigned special = 0;  // infinities and NaN: their exponents are ones, which overflow into the bit above
+#pragma unroll
+  for (int w = 0; w < 4; ++w) special |= ((x[w] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+  float c[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) c[e] = __builtin_amdgcn_fmed3f(scale.divides(element(x, e)), -448.f, 448.f);
+  unsigned nans[2] = {0, 0};
+  if (special != 0 || !scale.usual) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float f = element(x, e) / scale.s;
+      c[e] = f > 448.f ? 448.f : f < -448.f ? -448.f : f;
+      nans[e >> 2] |= f != f ? 0x7fu << (8 * (e & 3)) : 0u;
+    }
+  }
   u32x2 r;
 #pragma unroll
   for (int w = 0; w < 2; ++w) {
-    float c[4];
-    unsigned nans = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const unsigned two = x[2 * w + (e >> 1)];
-      const float f = scale.divides(__uint_as_float(e & 1 ? two & 0xffff0000u : two << 16));
-      c[e] = f > 448.f ? 448.f : f < -448.f ? -448.f : f;  // (a NaN passes neither comparison)
-      nans |= f != f ? 0x7fu << (8 * e) : 0u;
-    }
-    int word = __builtin_amdgcn_cvt_pk_fp8_f32(c[0], c[1], 0, false);
-    word = __builtin_amdgcn_cvt_pk_fp8_f32(c[2], c[3], word, true);
-    r[w] = (unsigned)word | nans;
+    int word = __builtin_amdgcn_cvt_pk_fp8_f32(c[4 * w], c[4 * w + 1], 0, false);
+    word = __builtin_amdgcn_cvt_pk_fp8_f32(c[4 * w + 2], c[4 * w + 3], word, true);
+    r[w] = (unsigned)word | nans[w];
   }
   return r;
 }
@@ -396,26 +405,42 @@ __device__ __forceinline__ void store_words(T* p, T x) {
   else *p = x;
 }
 
-// STREAM: past the caches, for calls of more bytes than the last-level cache holds (65536 rows of 8 heads of 128 to e4m3, 403 MB: 87 -> 84 us); what fits is kept for who reads it next.
-template <bool E4M3, bool STREAM>
+// STREAM: past the caches, for calls of more bytes than the last-level cache holds (87 -> 84 us before the vector work was cut); what fits is kept for who reads it next.
+template <bool E4M3, bool STREAM, int ROWS>
 __global__ __launch_bounds__(kWriteThreads) void write_kernel(const WriteArgs a) {
-  const int64_t piece = (int64_t)blockIdx.x * kWriteThreads + threadIdx.x;
-  if (piece >= a.pieces) return;
-  const int64_t row = a.by_row.wide(piece);
-  const int in_row = (int)(piece - row * a.row_pieces);
-  const int64_t slot = a.slots[row];
-  if (slot < 0 || slot >= a.num_slots) return;
-  const int head = a.by_head(in_row);
-  const int64_t page = a.by_page.wide(slot);
-  const int64_t to = ((page * a.heads + head) * a.page_size + (slot - page * a.page_size)) * a.head_pieces + (in_row - head * a.head_pieces);
-  const LooseWords *const pk = reinterpret_cast<const LooseWords*>(a.k + row * a.k_stride + in_row * 8), *const pv = reinterpret_cast<const LooseWords*>(a.v + row * a.v_stride + in_row * 8);
-  const u32x4 k = STREAM ? __builtin_nontemporal_load(pk) : *pk, v = STREAM ? __builtin_nontemporal_load(pv) : *pv;
-  if constexpr (E4M3) {
-    store_words<STREAM>(reinterpret_cast<u32x2*>(a.k_cache) + to, to_e4m3(k, Scale(a.k_scale[head])));
-    store_words<STREAM>(reinterpret_cast<u32x2*>(a.v_cache) + to, to_e4m3(v, Scale(a.v_scale[head])));
-  } else {
-    store_words<STREAM>(reinterpret_cast<u32x4*>(a.k_cache) + to, k);
-    store_words<STREAM>(reinterpret_cast<u32x4*>(a.v_cache) + to, v);
+  // (the workgroup's first row and piece: scalar work)
+  const int64_t piece0 = (int64_t)blockIdx.x * kWriteThreads, row0 = a.by_row.wide(piece0);
+  if (piece0 + threadIdx.x >= a.pieces) return;
+  const int ahead = (int)(piece0 - row0 * a.row_pieces) + threadIdx.x, rows_ahead = a.by_row(ahead), in_row = ahead - rows_ahead * a.row_pieces;
+  const int row = (int)row0 + rows_ahead, head = a.by_head(in_row);
+  u32x4 k[ROWS], v[ROWS];
+  int64_t slot[ROWS];
+#pragma unroll
+  for (int n = 0; n < ROWS; ++n) {
+    const int64_t at = row + (int64_t)n * a.apart;
+    slot[n] = ROWS == 1 || at < a.rows ? a.slots[at] : -1;
+  }
+#pragma unroll
+  for (int n = 0; n < ROWS; ++n) {
+    const int64_t at = row + (int64_t)n * a.apart;
+    if (ROWS > 1 && at >= a.rows) continue;
+    const LooseWords *const pk = reinterpret_cast<const LooseWords*>(a.k + at * a.k_stride + in_row * 8), *const pv = reinterpret_cast<const LooseWords*>(a.v + at * a.v_stride + in_row * 8);
+    k[n] = STREAM ? __builtin_nontemporal_load(pk) : *pk;
+    v[n] = STREAM ? __builtin_nontemporal_load(pv) : *pv;
+  }
+  const Scale k_scale(E4M3 ? a.k_scale[head] : 1.f), v_scale(E4M3 ? a.v_scale[head] : 1.f);
+#pragma unroll
+  for (int n = 0; n < ROWS; ++n) {
+    if (slot[n] < 0 || slot[n] >= a.num_slots) continue;
+    const int64_t page = a.by_page.wide(slot[n]);
+    const int64_t to = ((page * a.heads + head) * a.page_size + (slot[n] - page * a.page_size)) * a.head_pieces + (in_row - head * a.head_pieces);
+    if constexpr (E4M3) {
+      store_words<STREAM>(reinterpret_cast<u32x2*>(a.k_cache) + to, to_e4m3(k[n], k_scale));
+      store_words<STREAM>(reinterpret_cast<u32x2*>(a.v_cache) + to, to_e4m3(v[n], v_scale));
+    } else {
+      store_words<STREAM>(reinterpret_cast<u32x4*>(a.k_cache) + to, k[n]);
+      store_words<STREAM>(reinterpret_cast<u32x4*>(a.v_cache) + to, v[n]);
+    }
   }
 }
 
@@ -488,15 +513,17 @@ extern "C" int paged_cache_write(int32_t rows, int32_t num_kv_heads, int32_t hea
       (cache_type == PAGED_CACHE_E4M3 && (!aligned(k_scale, 4) || !aligned(v_scale, 4))))
     return CHUNK_ATTN_INVALID_ARG;
   const int row_pieces = (int)(row_elements / 8), head_pieces = head_dim / 8;
-  const int64_t pieces = (int64_t)rows * row_pieces;
-  const WriteArgs a{(const __bf16*)k, (const __bf16*)v, k_stride, v_stride, slots, k_scale, v_scale, k_cache, v_cache, (int64_t)num_pages * page_size, pieces, num_kv_heads,
-                    head_pieces, row_pieces, page_size, Divide(row_pieces), Divide(head_pieces), Divide(page_size)};
-  const int64_t groups = (pieces + kWriteThreads - 1) / kWriteThreads;
+  const bool e4m3 = cache_type == PAGED_CACHE_E4M3, stream = (int64_t)rows * row_pieces * (e4m3 ? 48 : 64) > kStreamBytes;
+  const bool many = e4m3 && (int64_t)rows * row_pieces >= (int64_t)kManyRows * kCus * 2048;
+  const int apart = many ? (rows + kManyRows - 1) / kManyRows : rows;
+  const int64_t pieces = (int64_t)apart * row_pieces, groups = (pieces + kWriteThreads - 1) / kWriteThreads;
   if (groups * kWriteThreads >= (int64_t)1 << 32) return CHUNK_ATTN_INVALID_ARG;
+  const WriteArgs a{(const __bf16*)k, (const __bf16*)v, k_stride, v_stride, slots, k_scale, v_scale, k_cache, v_cache, (int64_t)num_pages * page_size, pieces, rows, apart, num_kv_heads,
+                    head_pieces, row_pieces, page_size, Divide(row_pieces), Divide(head_pieces), Divide(page_size)};
   auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(kWriteThreads), 0, (hipStream_t)hip_stream, a); };
-  const bool e4m3 = cache_type == PAGED_CACHE_E4M3;
-  if (pieces * (e4m3 ? 48 : 64) > kStreamBytes) e4m3 ? launch(write_kernel<true, true>) : launch(write_kernel<false, true>);
-  else e4m3 ? launch(write_kernel<true, false>) : launch(write_kernel<false, false>);
+  if (many) stream ? launch(write_kernel<true, true, kManyRows>) : launch(write_kernel<true, false, kManyRows>);
+  else if (e4m3) launch(write_kernel<true, false, 1>);
+  else stream ? launch(write_kernel<false, true, 1>) : launch(write_kernel<false, false, 1>);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? CHUNK_ATTN_OK : report_hip(e, "keys and values into pages");
 }

@@ -108,7 +108,8 @@ def test_state_out_of_its_ranges(n):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "e4m3"])
-@pytest.mark.parametrize("rows,heads,dim,page,pad", [(1, 1, 64, 1, 0), (3, 2, 96, 7, 1), (257, 8, 128, 16, 0), (500, 3, 256, 48, 5), (1000, 5, 64, 64, 128), (70, 16, 128, 256, 8)])
+@pytest.mark.parametrize("rows,heads,dim,page,pad", [(1, 1, 64, 1, 0), (3, 2, 96, 7, 1), (257, 8, 128, 16, 0), (500, 3, 256, 48, 5), (1000, 5, 64, 64, 128), (70, 16, 128, 256, 8),
+                                                       (9001, 8, 128, 16, 4), (44001, 8, 128, 64, 0)])  # (two rows to a thread; past the caches)
 def test_write(rows, heads, dim, page, pad, kind):
     """Copies are equal; what is held in 8 bits is the nearest to the quotient in float32 (ties to even), as a cast gives it."""
     from paper_2509_21275_amd import paged_cache as pc
