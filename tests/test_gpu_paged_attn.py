@@ -153,6 +153,34 @@ def test_scores_of_any_size(dim):
         c.check(o, lse)
 
 
+@pytest.mark.parametrize("dim,kind", [(64, "bf16"), (128, "e4m3"), (256, "bf16")])
+def test_a_row_is_its_own(dim, kind):
+    """Queries that are not finite, or large, leave the other rows as they were, bit for bit."""
+    c = Case([700, 130, 40], [3, 5, 2], 8, 2, dim, 16, kind)
+    o, lse = c.run()
+    c.check(o, lse)
+    rows = [1, 4, 9]
+    for value in (float("nan"), float("inf"), 1000.0):
+        kept = c.q.clone()
+        c.q[rows, :4, ::3] = value
+        got, got_lse = c.run()
+        others = torch.ones(c.total, 8, dtype=torch.bool, device="cuda")
+        others[rows, :4] = False
+        assert torch.equal(got[others], o[others]) and torch.equal(got_lse.T[others], lse.T[others])
+        if value != value:
+            assert not bool(torch.isfinite(got[rows, :4]).any())
+        c.q.copy_(kept)
+
+
+def test_sequences_that_share_pages():
+    """Two sequences with the same first pages, as behind a common prompt, and one table row twice."""
+    c = Case([400, 300, 250], [1, 2, 1], 8, 2, 128, 16)
+    c.table[1, :12] = c.table[0, :12]
+    c.table[2] = c.table[0]
+    o, lse = c.run()
+    c.check(o, lse)
+
+
 def test_pages_that_are_none():
     """Tokens on a page whose number is none are masked; lengths past the table count as its own."""
     c = Case([300, 64, 20, 16], [2, 1, 1, 1], 4, 2, 128, 16)

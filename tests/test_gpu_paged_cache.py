@@ -107,6 +107,19 @@ def test_state_out_of_its_ranges(n):
         assert np.array_equal(x.cpu().numpy(), np.atleast_1d(y))
 
 
+@pytest.mark.parametrize("n", [8, 1500, 4500])
+def test_more_tokens_than_32_bits_count(n):
+    """Requests for 2^31 - 1 tokens each: what comes before them is served, nothing overflows."""
+    width, page, spare = 6, 16, 3 * n
+    rng, kv_len, held, table, stack, pages = state(n, width, page, spare, n, longest=40)
+    new = rng.integers(0, 5, n)
+    new[n // 2::3] = 2**31 - 1
+    for max_rows in (int(new[:n // 2].sum()) + 7, 3000):
+        want = orc.extend(page, pages, new, kv_len, held, table, stack, spare, max_rows)
+        got = extend(n, width, page, pages, new, kv_len, held, table, stack, spare, max_rows, False)
+        assert all(np.array_equal(a, np.atleast_1d(b)) for a, b in zip(got, want))
+
+
 @pytest.mark.parametrize("kind", ["bf16", "e4m3"])
 @pytest.mark.parametrize("rows,heads,dim,page,pad", [(1, 1, 64, 1, 0), (3, 2, 96, 7, 1), (257, 8, 128, 16, 0), (500, 3, 256, 48, 5), (1000, 5, 64, 64, 128), (70, 16, 128, 256, 8),
                                                        (9001, 8, 128, 16, 4), (44001, 8, 128, 64, 0)])  # (two rows to a thread; past the caches)
