@@ -102,12 +102,12 @@ __device__ __forceinline__ int64_t slot_of_row(const TableArgs& a, const int32_t
   const int page = b < helds[i] ? a.table[(int64_t)i * a.max_pages + b] : a.free_pages[on_stack - 1 - (pages_before[i] + b - helds[i])];
   return page >= 0 && page < a.num_pages ? (int64_t)page * a.page_size + at - b * a.page_size : -1;
 }
-// One page that changes hands, of request i.
+// One page that changes hands, of request i (truncate: one for which the stack has room).
 template <bool EXTEND>
 __device__ __forceinline__ void move_page(const TableArgs& a, const int32_t* pages_before, const int32_t* helds, int on_stack, int p, int i) {
   int32_t* const entry = a.table + (int64_t)i * a.max_pages + helds[i] + p - pages_before[i];
   if (EXTEND) *entry = a.free_pages[on_stack - 1 - p];
-  else if (on_stack + p < a.num_pages) a.free_pages[on_stack + p] = *entry;
+  else a.free_pages[on_stack + p] = *entry;
 }
 
 // What becomes of a request (members as in the arrays they go to).
@@ -250,7 +250,9 @@ __global__ __launch_bounds__(kScanThreads) void tables_kernel(const TableArgs a)
   if constexpr (IN_ONE) {
     if (EXTEND)
       for (int r = threadIdx.x; r < a.max_rows; r += kScanThreads) a.slots[r] = r < starts[a.n] ? slot_of_row(a, starts, pages_before, old_lens, helds, on_stack, r, find(starts, a.n, r)) : -1;
-    for (int p = threadIdx.x; p < moved; p += kScanThreads) move_page<EXTEND>(a, pages_before, helds, on_stack, p, find(pages_before, a.n, p));
+    // (unsigned: `moved` may be the largest int, and the next p past it)
+    const uint32_t moves = (uint32_t)(EXTEND ? moved : min(moved, a.num_pages - on_stack));
+    for (uint32_t p = threadIdx.x; p < moves; p += kScanThreads) move_page<EXTEND>(a, pages_before, helds, on_stack, (int)p, find(pages_before, a.n, (int)p));
   }
 }
 

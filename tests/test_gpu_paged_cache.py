@@ -120,6 +120,26 @@ def test_more_tokens_than_32_bits_count(n):
         assert all(np.array_equal(a, np.atleast_1d(b)) for a, b in zip(got, want))
 
 
+@pytest.mark.parametrize("pages,on_stack", [(16, 8), (8, 8), (3, 0)])
+def test_more_pages_given_back_than_32_bits_count(pages, on_stack):
+    """A request that says it holds 2^31 - 1 pages, most of them given back more than once: as many as the stack has room for go onto it, and nothing is written behind it."""
+    from paper_2509_21275_amd import paged_cache as pc
+    most = 2**31 - 1
+    desc = pc.make_desc(1, most, 1, pages)
+    table = torch.empty((1, most), dtype=I32, device="cuda")
+    table[0, :32] = torch.arange(100, 132, device="cuda")
+    room = torch.full((64,), -7, dtype=I32, device="cuda")
+    stack = room[16:16 + pages]
+    a = [gpu(x) for x in ([most], [0], [most])]
+    free = gpu([on_stack])
+    print(pages, on_stack, flush=True)
+    pc.paged_cache_truncate(desc, *a, table, stack, free, a[1], a[2], free, pc.alloc_workspace(desc))
+    torch.cuda.synchronize()
+    want = np.full(64, -7)
+    want[16 + on_stack:16 + pages] = np.arange(100, 100 + pages - on_stack)
+    assert np.array_equal(room.cpu().numpy(), want) and [int(t) for t in (a[1], a[2], free)] == [0, 0, pages]
+
+
 @pytest.mark.parametrize("kind", ["bf16", "e4m3"])
 @pytest.mark.parametrize("rows,heads,dim,page,pad", [(1, 1, 64, 1, 0), (3, 2, 96, 7, 1), (257, 8, 128, 16, 0), (500, 3, 256, 48, 5), (1000, 5, 64, 64, 128), (70, 16, 128, 256, 8),
                                                        (9001, 8, 128, 16, 4), (44001, 8, 128, 64, 0)])  # (two rows to a thread; past the caches)
