@@ -14,9 +14,9 @@
  * What kv_len, q_start and table hold is not known to the host, so nothing in them is an error: lengths count as at most max_pages * page_size, rows outside [0, total_q) as not there, and
  * tokens on a page whose number is none, which no row sees, as masked.  What lies in the cache where a row sees nothing (other rows of a page, tokens behind it) does not reach it, whatever it is.
  *
- * Any number of new tokens is right; many of them (hundreds) read a sequence's keys and values once for every 32 rows of a key/value head, and are faster with
- * chunk_attn_fwd.  Scores, softmax and sums are float32; weights go into the products with values as two bf16 terms; a result is rounded once.  Results do not depend on timing; the walk over the keys is
- * cut where the lengths of all sequences say, so a sequence's last bits may depend on the others' lengths.
+ * Any number of new tokens is right; many of them (hundreds) read a sequence's keys and values once for every 128 rows of a key/value head (32 for head dimension 256), and are
+ * faster with chunk_attn_fwd.  Scores, softmax and sums are float32; weights go into the products with values as two bf16 terms, with e4m3 values as one float16 term; a result is rounded once.
+ * Results do not depend on timing; the walk over the keys is cut where the lengths of all sequences say, so a sequence's last bits may depend on the others' lengths.
  *
  * The calls are asynchronous on `hip_stream`, keep nothing, allocate nothing and may be captured into a graph: lengths and tables are read on the device, so a replay follows them.  Scratch space
  * is the caller's `workspace` (DEVICE memory, 256-byte aligned, of paged_attn_workspace_bytes; its contents need not survive, and calls that may run at the same time need one each).  Outputs may overlap nothing else.

@@ -93,6 +93,9 @@ def test_attention_refusals(ca):
         assert pa.paged_attn_validate(desc(**kw)) == ca.INVALID_ARG, kw
     for kw in (dict(head_dim=80), dict(head_dim=32), dict(num_q_heads=9), dict(num_q_heads=32768), dict(num_seqs=65537), dict(page_size=65537)):
         assert pa.paged_attn_validate(desc(**kw)) == ca.UNSUPPORTED, kw
+    # 4096 sequences, a row to each, of up to 2^25 tokens: 2^30 blocks of 128 keys
+    most = dict(num_q_heads=2, num_seqs=4096, total_q=4096)
+    assert pa.paged_attn_validate(desc(max_pages=2**21, **most)) == ca.OK and pa.paged_attn_validate(desc(max_pages=2**21 + 1, **most)) == ca.INVALID_ARG
     bad = desc()
     bad.cache_type = 2
     assert pa.paged_attn_validate(bad) == ca.INVALID_ARG and ca._lib.paged_attn_validate(None) == ca.INVALID_ARG
