@@ -9,12 +9,12 @@
 // A wave's tile: K from memory into the registers of the product K Q^T (no LDS: a key is read by one wave, once), V in whole rows through registers into LDS, from where it is read transposed; both are
 // loaded one tile ahead (two ahead was slower).  Q lies in LDS, in the order in which lanes read it: in registers it left the compiler too few for the loads ahead (64 sequences of 3900 keys on average,
 // 32/8 heads of 128: 259 -> 198 us).  Head dimension 256 would need 128 registers for the output and as many for a tile: there two waves share a tile, each with half of the dimensions, and add up
-// their halves of the scores through LDS (32 sequences with up to 8 drafts, 16/4 heads: 293 -> 146 us).  More than 32 rows: the waves of a workgroup divide into groups of rows that load the same tile.
+// their halves of the scores through LDS (32 sequences with up to 8 drafts, 16/4 heads: 293 -> 146 us then, 131 now).  More than 32 rows: the waves of a workgroup divide into groups of rows that load the same tile.
 //
 // Bound by memory: one token of 32/8 heads takes four operations for each byte of the cache, 32 rows 32.  Weights go into the product with V as two bf16 terms (one would leave the output with
-// 2.4e-3 of itself in place of 1.7e-3), for e4m3 values, which float16 has, as one float16 term (2^-11).  Measured: 64 sequences as above 195 us, 5.4 TB/s; 8 of 32768 keys 197, 5.45; 8 of 131072
-// keys of 8 bits 369, 5.8; one of 131072 keys of 8 bits with 40 rows 75, 3.6 TB/s: there vector units (48 % of the time) and matrix units (27 %) take turns.  What is short: a launch with one block of
-// 60 keys takes 8 us, of which 2 until the first loads, 2.5 for them, 1 for the tile, 2 to put results together; cutting adds a launch of 3.5 us.
+// 2.4e-3 of itself in place of 1.7e-3), for e4m3 values, which float16 has, as one float16 term (2^-11).  Measured: 64 sequences as above 194 us, 5.4 TB/s; 8 of 32768 keys 197, 5.45; 8 of 131072
+// keys of 8 bits 369, 5.8; one of 131072 keys of 8 bits with 40 rows 74, 3.6 TB/s: there vector units (48 % of the time) and matrix units (27 %) take turns.  What is short: a launch with one block of
+// 60 keys takes 8 us, of which 2 until the first loads, 2.5 for them, 1 for the tile, 2 to put results together; cutting adds a launch of 4 us.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
