@@ -365,7 +365,8 @@ struct WriteArgs {
 };
 
 // Division by a head's scale.  x / s as q + r y with y the nearest to 1 / s, q = x y and r = x - q s, which a fused multiply and add gives exactly: the nearest to the quotient, where nothing
-// leaves float32's normal range (equal to the division for 4 * 10^8 drawn pairs).  Quotients past 1024 only have to stay past 448: q is kept to 1024, so that nothing becomes infinite less infinite.
+// leaves float32's normal range (equal to the division for 4 * 10^8 drawn pairs), but for -0, which comes out as 0 (the remainder is 0, and -0 + 0 = 0): to_e4m3 puts the sign back.
+// Quotients past 1024 only have to stay past 448: q is kept to 1024, so that nothing becomes infinite less infinite.
 struct Scale {
   float s, y;
   bool usual;  // the quotient of anything by s that 8 bits hold is far from the ends of float32's range
@@ -384,13 +385,17 @@ __device__ __forceinline__ u32x2 to_e4m3(const u32x4& x, const Scale& scale) {
   float c[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) c[e] = __builtin_amdgcn_fmed3f(scale.divides(element(x, e)), -448.f, 448.f);
-  unsigned nans[2] = {0, 0};
+  // set in a byte of the result: its sign, which is the number's (a scale is positive); where quotients are divided truly, NaN
+  unsigned bits[2];
+#pragma unroll
+  for (int w = 0; w < 2; ++w) bits[w] = __builtin_amdgcn_perm(x[2 * w + 1], x[2 * w], 0x07050301) & 0x80808080u;
   if (special != 0 || !scale.usual) {
+    bits[0] = bits[1] = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const float f = element(x, e) / scale.s;
       c[e] = f > 448.f ? 448.f : f < -448.f ? -448.f : f;
-      nans[e >> 2] |= f != f ? 0x7fu << (8 * (e & 3)) : 0u;
+      bits[e >> 2] |= f != f ? 0x7fu << (8 * (e & 3)) : 0u;
     }
   }
   u32x2 r;
@@ -398,7 +403,7 @@ __device__ __forceinline__ u32x2 to_e4m3(const u32x4& x, const Scale& scale) {
   for (int w = 0; w < 2; ++w) {
     int word = __builtin_amdgcn_cvt_pk_fp8_f32(c[4 * w], c[4 * w + 1], 0, false);
     word = __builtin_amdgcn_cvt_pk_fp8_f32(c[4 * w + 2], c[4 * w + 3], word, true);
-    r[w] = (unsigned)word | nans[w];
+    r[w] = (unsigned)word | bits[w];
   }
   return r;
 }

@@ -180,6 +180,37 @@ def test_write(rows, heads, dim, page, pad, kind):
             assert torch.equal(c, w)
 
 
+@pytest.mark.parametrize("rows,heads,dim,page,pad", [(1, 5, 64, 1, 0), (3, 5, 96, 7, 1), (700, 5, 256, 16, 0), (9001, 8, 128, 16, 4)])  # (the last: two rows to a thread)
+def test_special_values_to_8_bits(rows, heads, dim, page, pad):
+    """Zeros of both signs, ties, the smallest steps, what 8 bits do not reach, each among eight finite neighbours and beside infinities and NaN, in rows all of which are written; scales near and past the ends of
+    float32.  What is held is the nearest to the quotient in float32 (ties to even) with its sign, as a cast gives it, whatever the neighbours are."""
+    from paper_2509_21275_amd import paged_cache as pc
+    finite = torch.tensor([0.0, -0.0, 1.0625, -1.0625, 1.1875, 17.0, -19.0, 0.30078125, 448.0, 464.0, -465.0, 480.0, 1e30, -1e30, -0.0, 0.0, 2.0**-9, 2.0**-10, 3 * 2.0**-10, -(2.0**-10), -(2.0**-11),
+                           -5 * 2.0**-10, 1e-38, -1e-38, -0.0, -0.0, -0.0, -0.0, -0.0, -0.0, -0.0, -0.0])
+    beside = finite.clone()
+    beside[0::8] = torch.tensor([float("inf"), float("nan"), -float("inf"), float("inf")])
+    line = torch.cat((finite, beside)).repeat(heads * dim // 64 + 1)[:heads * dim]
+    x = (line[None] * (1.0 - 2.0 * (torch.arange(rows) % 2))[:, None]).to(BF16)  # (every other row with the other signs)
+    wide = torch.zeros((rows, heads * dim + pad), dtype=BF16)
+    wide[:, :heads * dim] = x
+    x = x.unflatten(1, (heads, dim))
+    k = wide.cuda()[:, :heads * dim].unflatten(1, (heads, dim))
+    scales = [torch.tensor((list(s) * heads)[:heads]) for s in ((1.0, 0.37, 2.0**-100, 2.0**100, 1.7), (2.0**-79, 2.0**79, 3.0, 2.0**-140, 0.25))]
+    pages = -(-rows // page) + 1
+    slots = torch.randperm(pages * page, generator=torch.Generator().manual_seed(rows))[:rows]
+    assert bool(((slots >= 0) & (slots < pages * page)).all())
+    caches = [torch.ones((pages, heads, page, dim), device="cuda").to(E4M3) for _ in range(2)]
+    print(rows, heads, dim, page, pad, flush=True)
+    pc.paged_cache_write(k, k, slots.cuda(), *caches, *(s.cuda() for s in scales))
+    torch.cuda.synchronize()
+    for c, s in zip(caches, scales):
+        w = torch.ones((pages, heads, page, dim)).to(E4M3).view(torch.uint8)
+        w[slots // page, :, slots % page] = (x.float() / s[:, None]).clamp(-448, 448).to(E4M3).view(torch.uint8)
+        c, nan = c.cpu().view(torch.uint8), w & 0x7f == 0x7f
+        assert bool(nan.any()) and bool((w == 0x80).any())
+        assert torch.equal(c & 0x7f == 0x7f, nan) and torch.equal(c[~nan], w[~nan])
+
+
 def test_write_past_offsets_of_32_bits():
     """Pages past the first 2^32 elements, and rows more than 2^31 elements behind the first."""
     from paper_2509_21275_amd import paged_cache as pc
