@@ -12,9 +12,10 @@
  * Tensors (DEVICE; the caller owns them):
  *   target       : row j of request r at (r * (max_drafts + 1) + j) * target_stride, vocab contiguous elements; float32 or bf16, aligned to their type
  *   draft        : row j of request r at (r * max_drafts + j) * draft_stride, of the same type; or null
- *   tokens       : [batch][max_drafts] int32;  count: [batch] int32, counted as 0 .. max_drafts at most, or null (max_drafts each)
+ *   tokens       : [batch][max_drafts] int32;  count: [batch] int32, counted as 0 .. max_drafts at most, or null: max_drafts each, where that many drafted tokens of every request are in the cache
  *   uniforms     : [batch][max_drafts] float32;  last_uniform: [batch] float32; both in [0, 1)
- *   accepted     : [batch] int32, tokens kept;  rejected: [batch] int32, count - accepted, or null: what paged_cache_truncate takes off again
+ *   accepted     : [batch] int32, tokens kept;  rejected: [batch] int32, count - accepted, or null: what paged_cache_truncate takes off again.  Of a request with nothing new,
+ *                  or that paged_cache_extend did not serve (`granted` 0), no drafted token is in the cache: its count has to be 0, so that nothing is taken off it, and its row of `out` means nothing
  *   out          : [batch][max_drafts + 1] int32: the tokens kept, the one that follows them, then -1
  * Rows of probabilities that the result does not depend on are not read, but for one number of each drafted token.
  *

@@ -4,7 +4,7 @@
  *
  * Sequence i has kv_len[i] tokens in the cache, of which its last n = q_start[i + 1] - q_start[i] are new: rows q_start[i] .. q_start[i + 1] - 1 of q.  New token j attends to tokens
  * t = 0 .. kv_len - n + j of its own sequence and to nothing else.  The result is exact softmax attention, O = softmax(scale * Q K^T + mask) V; a row that sees no token (kv_len < n)
- * has o = 0 and lse = -inf.  Query head h uses key/value head h / (num_q_heads / num_kv_heads).
+ * has o = 0 and lse = -inf; rows of a request that paged_cache_extend did not serve take its last cached tokens for new ones, and mean nothing.  Query head h uses key/value head h / (num_q_heads / num_kv_heads).
  *
  * Tensors (DEVICE; the caller owns them):
  *   q, o     : bf16, row r, head h at r * stride + h * head_dim (strides in elements, >= num_q_heads * head_dim; 2-byte aligned); rows behind q_start[num_seqs] are not read, and left as they are

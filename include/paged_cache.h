@@ -16,7 +16,8 @@
  * the slots of its tokens -1.
  *
  * A step of a server: paged_cache_extend for the tokens that come in, paged_cache_write for their keys and values in every layer, attention over the cache (paged_attn.h),
- * and, where drafted tokens were rejected or requests end, paged_cache_truncate.
+ * and, where drafted tokens were rejected or requests end, paged_cache_truncate.  A request that paged_cache_extend did not serve (`granted` 0) is as it was, and its last cached tokens are none of this
+ * step's: nothing may be dropped for the step, so with drafts it is verified with a count of 0, (new - 1) * granted (draft_verify.h); its rows are in q_start all the same, and what is computed from them means nothing.
  *
  * The calls are asynchronous on `hip_stream`, keep nothing, allocate nothing and may be captured into a graph.  Results do not depend on timing.  Scratch space is the caller's `workspace` (DEVICE
  * memory, 256-byte aligned, of paged_cache_workspace_bytes; its contents need not survive, and calls that may run at the same time need one each).

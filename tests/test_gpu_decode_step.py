@@ -187,3 +187,122 @@ def test_a_pool_that_runs_out():
             assert np.array_equal(x.cpu().numpy(), y), step
         assert free[:b[3]].tolist() == b[2][:b[3]].tolist()
     assert refused > 10
+
+
+class Refusing(Decoder):
+    """The same where the pool may run out: a request that is not served, or has nothing new, has no drafts in the cache, and nothing is taken off it."""
+
+    def __init__(self, *args, **kw):
+        super().__init__(*args, **kw)
+        self.count, self.idle = torch.zeros(self.n, dtype=I32, device="cuda"), set()
+
+    def feed(self, last):
+        """Rows of requests that have ended are not there: those of the others follow each other."""
+        super().feed(last)
+        at = [i * (1 + self.K) + j for i in range(self.n) if i not in self.idle for j in range(1 + self.K)]
+        for x in (self.q, self.k, self.v):
+            x[:len(at)] = x[at].clone()
+
+    def choose(self):
+        from paper_2509_21275_amd import draft_verify as dv
+        from paper_2509_21275_amd import paged_cache as pc
+        torch.mul(self.new - 1, self.granted, out=self.count)
+        dv.draft_verify(self.target, self.draft, self.tokens, self.count, self.u, self.last_u, self.accepted, self.rejected, self.out, self.ws[2])
+        pc.paged_cache_truncate(self.cdesc, self.rejected, self.kv_len, self.held, self.table, self.free, self.num_free, self.kv_len, self.held, self.num_free, self.ws[0])
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+def test_decoding_where_some_are_refused(kind):
+    """What a refused request has in the cache stays, and it goes on from there when others have ended."""
+    from paper_2509_21275_amd import paged_cache as pc
+    n, drafts, page = 6, 3, 4
+    d = Refusing(n, drafts, page, kind, seed=11, width=60)
+    d.prefill()
+    d.num_free.fill_(9)  # a step takes up to n of them
+    torch.cuda.synchronize()
+    texts, refused, again = [list(p) for p in d.prompts], set(), set()
+    idle = d.idle
+    for step in range(24):
+        d.feed([t[-1] for t in texts])
+        d.forward()
+        torch.cuda.synchronize()
+        granted = d.granted.tolist()
+        served = [i for i in range(n) if granted[i] and i not in idle]
+        waiting = [i for i in range(n) if not granted[i]]
+        refused |= set(waiting)
+        again |= refused & set(served)
+        assert d.kv_len.tolist() == [0 if i in idle else len(t) + drafts if granted[i] else len(t) - 1 for i, t in enumerate(texts)]
+        starts = d.q_start.tolist()
+        for i in served:  # (in float64: a few rows)
+            whole = torch.tensor(texts[i] + d.tokens[i].tolist(), device="cuda")
+            k, v = d.k_of[whole].double(), d.v_of[whole].double()
+            if kind == "e4m3":
+                s = float(d.scale[0])
+                k, v = ((x / s).float().clamp(-448, 448).to(E4M3).double() * s for x in (k, v))
+            for j in range(1 + drafts):
+                row, seen = starts[i] + j, len(texts[i]) + j
+                x = torch.matmul(d.q[row].double().view(d.kv_heads, -1, d.dim), k[:seen].permute(1, 2, 0).contiguous()) * d.dim ** -0.5
+                want = torch.matmul(torch.softmax(x, -1), v[:seen].transpose(0, 1).contiguous()).reshape(d.heads, d.dim)
+                # half a step of bf16, and 2^-11 of values below 5
+                assert float((d.o[row].double() - want).abs().max()) < 2.0 ** -8 * 5 + 2.0 ** -11 * 5, (step, i, j)
+        d.target.copy_(torch.softmax(d.o.float().flatten(1) @ d.head, -1).view(n, drafts + 1, d.vocab))
+        if idle:  # (their rows are not there, so that those of the others lie further ahead)
+            at = torch.tensor([starts[i] for i in range(n)], device="cuda")
+            rows = (at[:, None] + torch.arange(drafts + 1, device="cuda")).clamp(max=n * (drafts + 1) - 1)
+            d.target.copy_(d.target.flatten(0, 1)[rows])
+        before = [x.clone() for x in (d.kv_len, d.held, d.table)]
+        d.choose()
+        torch.cuda.synchronize()
+        for i in waiting:
+            assert d.rejected[i] == 0 and all(torch.equal(x[i], y[i]) for x, y in zip((d.kv_len, d.held, d.table), before)), (step, i)
+        target, draft = d.target.double().cpu().numpy(), d.draft.double().cpu().numpy()
+        for i in served:
+            kept, out = orc.verify(target[i], draft[i], d.tokens[i].tolist(), drafts, d.u[i].tolist(), float(d.last_u[i]))
+            assert d.accepted[i] == kept and d.out[i].tolist() == out, (step, i)
+            texts[i] += out[:kept + 1]
+        assert all(d.kv_len[i] == len(texts[i]) - 1 for i in range(n) if i not in idle)
+        if len(waiting) > 1 and len(idle) < 3:  # one of those that were served ends
+            i = served[0]
+            idle.add(i)
+            drop = torch.zeros_like(d.rejected)
+            drop[i] = 2**31 - 1
+            d.new[i] = 0
+            pc.paged_cache_truncate(d.cdesc, drop, d.kv_len, d.held, d.table, d.free, d.num_free, d.kv_len, d.held, d.num_free, d.ws[0])
+            torch.cuda.synchronize()
+    assert refused and again
+
+
+def test_the_step_of_the_readme():
+    """The lines themselves, on a pool that two of six requests find empty, and with one that has nothing new: what these have in the cache stays."""
+    from pathlib import Path
+    text = (Path(__file__).parent.parent / "README.md").read_text()
+    lines = [b.split("```")[0] for b in text.split("```python") if "paged_cache as pc" in b]
+    assert len(lines) == 1
+    g = torch.Generator().manual_seed(1)
+    n, drafts, vocab, page, width, pages = 6, 3, 100, 16, 8, 40
+    kv_len, new = [32, 20, 16, 48, 5, 30], [4, 4, 4, 4, 4, 0]
+    held = [-(-t // page) for t in kv_len]
+    table = torch.full((n, width), -1, dtype=I32)
+    at = 0
+    for i, h in enumerate(held):
+        table[i, :h] = torch.arange(at, at + h)
+        at += h
+    ints = lambda x: torch.tensor(x, dtype=I32, device="cuda")  # noqa: E731
+    z = lambda *s, dtype=I32: torch.zeros(s, dtype=dtype, device="cuda")  # noqa: E731
+    rows = n * (1 + drafts)
+    bf16 = lambda *s: torch.randn(s, generator=g).to(BF16).cuda()  # noqa: E731
+    free = torch.zeros(pages, dtype=I32)
+    free[:1] = at  # one page: request 0 gets it, 2 and 3 find none
+    names = dict(torch=torch, num_requests=n, max_pages=width, page_size=page, num_pages=pages, drafts=drafts, vocab=vocab, total_q=rows, new_tokens=ints(new), kv_len=ints(kv_len),
+                 held=ints(held), table=table.cuda(), free_pages=free.cuda(), num_free=ints([1]), q_start=z(n + 1), slots=z(rows, dtype=I64), granted=z(n), count=z(n), k=bf16(rows, 8, 128),
+                 v=bf16(rows, 8, 128), k_cache=bf16(pages, 8, page, 128), v_cache=bf16(pages, 8, page, 128), q=bf16(rows, 32, 128), o=bf16(rows, 32, 128), lse=torch.zeros((32, rows), device="cuda"),
+                 target=torch.softmax(torch.randn((n, drafts + 1, vocab), generator=g), -1).cuda(), draft=torch.softmax(torch.randn((n, drafts, vocab), generator=g), -1).cuda(),
+                 tokens=torch.randint(0, vocab, (n, drafts), generator=g).to(I32).cuda(), uniforms=torch.full((n, drafts), 0.99, device="cuda"), last_uniform=torch.rand(n, generator=g).cuda(),
+                 accepted=z(n), rejected=z(n), out=z(n, drafts + 1))
+    exec(lines[0], names)
+    torch.cuda.synchronize()
+    assert names["granted"].tolist() == [1, 1, 0, 0, 1, 1]
+    accepted = names["accepted"].tolist()
+    assert min(accepted) < drafts  # (a draft falls somewhere)
+    want = [t + 1 + a if m and ok else t for t, m, a, ok in zip(kv_len, new, accepted, names["granted"].tolist())]
+    assert names["kv_len"].tolist() == want and names["held"].tolist() == [-(-t // page) for t in want]
