@@ -24,6 +24,7 @@
 #include "kernels.hpp"
 #include "operators.hpp"
 #include "paged.hpp"
+#include "paged_shares.hpp"
 #include "tiles.hpp"
 
 namespace chunk_attn {
@@ -85,8 +86,9 @@ __device__ __forceinline__ Sequence sequence_at(const AttnArgs& a, int i) {
   Sequence s;
   const int most = a.max_pages * a.page_size;
   s.len = min(max(a.kv_len[i], 0), most);
-  s.first_row = max(a.q_start[i], 0);
-  s.rows = max(min(a.q_start[i + 1], a.total_q) - s.first_row, 0) * a.group;
+  const Rows r = rows_between(a.q_start[i], a.q_start[i + 1], a.total_q);
+  s.first_row = r.first;
+  s.rows = r.count * a.group;
   return s;
 }
 

@@ -208,6 +208,21 @@ def test_starts_of_rows_out_of_range():
     assert bool(torch.isfinite(o).all())
 
 
+@pytest.mark.parametrize("heads,kv_heads,dim", [(4, 2, 64), (8, 1, 256)])
+def test_starts_of_rows_farther_apart_than_32_bits_count(heads, kv_heads, dim):
+    """The largest and the smallest int next to each other: from the one down to the other there are no rows, up from the smallest there are all."""
+    c = Case([50, 60, 70, 5], [1, 1, 1, 1], heads, kv_heads, dim, 16)
+    most, least, total = 2**31 - 1, -(2**31), c.total
+    for starts, has_all in (([most, least, -1, least, least], None), ([most, least, most, least, -7], 1), ([total, least, total, -1, -1], 1), ([least, most - 5, least, least + 1, least], 0)):
+        c.q_start = starts
+        o, lse = c.run()
+        if has_all is None:
+            assert bool((o == 7.0).all()) and bool((lse == 7.0).all())
+        else:
+            c.q_start = [0] * (has_all + 1) + [total] * (4 - has_all)
+            c.check(o, lse)
+
+
 def test_pool_past_offsets_of_32_bits():
     """Pages past the first 2^32 elements of the pool."""
     heads, dim, page = 8, 128, 64

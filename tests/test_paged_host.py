@@ -3,6 +3,8 @@ has nothing to do, before any launch), and the oracles against closed forms."""
 import ctypes
 import os
 import re
+import shutil
+import subprocess
 
 import numpy as np
 import pytest
@@ -176,3 +178,13 @@ def test_oracle_of_the_verification_draws_as_the_target():
                 kept, out = orc.verify(p, q, [d], 1, [(i + 0.5) / m], (j + 0.5) / m)
                 got[out[0]] += q[0, d] / m / m
     assert np.allclose(got, p[0])
+
+
+# ---- the division of the attention's work ----
+@pytest.mark.skipif(shutil.which("g++") is None, reason="needs g++")
+def test_division_of_work_in_any_numbers(tmp_path):
+    exe = str(tmp_path / "paged_shares")
+    r = subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", os.path.join(ROOT, "tests", "native", "paged_shares.cpp"), "-o", exe], capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-2000:]
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and r.stdout.strip() == "ok", r.stdout[-2000:]
