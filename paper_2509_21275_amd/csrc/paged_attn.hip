@@ -552,7 +552,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnArgs a) {
       a.cuts[share * kCut + kCutSeqRow] = s.first_row;
       a.cuts[share * kCut + kCutRow] = row;
       a.cuts[share * kCut + kCutRows] = min(subs * kRows, s.rows - row);
-      a.cuts[share * kCut + kCutShares] = (int)((unsigned)(unit + key_blocks - 1) / (unsigned)size) - share + 1;
+      a.cuts[share * kCut + kCutShares] = shares_of_block(unit, key_blocks, size, total);
     }
     __syncthreads();
     unit += block1 - block0;

@@ -13,4 +13,11 @@ constexpr Rows rows_between(int32_t start, int32_t end, int32_t total) {
   return Rows{first, last - first};
 }
 
+// In how many shares of `size` units each, of `total` units in all, a block's units lie, from the share that its first unit is in.  (Sums of units stay at a largest number, which a block may reach
+// past where starts of rows do not increase: what lies behind it is in no share.)
+constexpr int32_t shares_of_block(int32_t first, int32_t units, int32_t size, int32_t total) {
+  const int32_t last = units < total - first ? first + units - 1 : total - 1;
+  return (int32_t)((uint32_t)last / (uint32_t)size - (uint32_t)first / (uint32_t)size) + 1;
+}
+
 }  // namespace chunk_attn
