@@ -65,6 +65,8 @@ int paged_cache_extend(const paged_cache_desc* desc, const int32_t* new_tokens, 
 /*
  * Tokens off the end of requests: drop [num_requests] (negative: 0; kv_len or more: all, the request has ended).  Pages that hold none of the tokens left go back on the stack, in
  * the order of the requests and of their tables; those that would not fit the stack (pages given back twice) are lost.  The table is read, and stays as it is.  *_out as above.
+ * It knows no holders: a page that several requests hold goes onto the stack once for each that gives it back, and then to two others.  Requests that share pages (full ones, of a common prompt: the
+ * attention reads them as any) are therefore dropped down to the shared tokens and no further, where the caller sets their kv_len and held to 0; the last holder gives the shared pages back.
  */
 int paged_cache_truncate(const paged_cache_desc* desc, const int32_t* drop, const int32_t* kv_len, const int32_t* held, const int32_t* table, int32_t* free_pages,
                          const int32_t* num_free, int32_t* kv_len_out, int32_t* held_out, int32_t* num_free_out, void* workspace, size_t workspace_bytes,

@@ -120,6 +120,32 @@ def test_more_tokens_than_32_bits_count(n):
         assert all(np.array_equal(a, np.atleast_1d(b)) for a, b in zip(got, want))
 
 
+def test_requests_that_share_a_prompt():
+    """Samples of one prompt, with its full pages in all their tables: each that ends is dropped down to them, the last one altogether; every page goes back once."""
+    from paper_2509_21275_amd import paged_cache as pc
+    n, width, page, pages, full = 4, 8, 4, 30, 3
+    desc = pc.make_desc(n, width, page, pages)
+    ws, q_start, slots = pc.alloc_workspace(desc), gpu(np.zeros(n + 1)), torch.zeros(100, dtype=I64, device="cuda")
+    kv_len, held, table, free, num_free = (gpu(x) for x in (np.zeros(n), np.zeros(n), np.zeros((n, width)), np.arange(pages), [pages]))
+    pc.paged_cache_extend(desc, gpu([full * page, 0, 0, 0]), kv_len, held, table, free, num_free, kv_len, held, num_free, q_start, slots, None, ws)
+    table[1:, :full] = table[0, :full]
+    kv_len.fill_(full * page)
+    held.fill_(full)
+    for _ in range(3):
+        pc.paged_cache_extend(desc, gpu([1, 3, 5, 0]), kv_len, held, table, free, num_free, kv_len, held, num_free, q_start, slots, None, ws)
+    torch.cuda.synchronize()
+    assert kv_len.tolist() == [15, 21, 27, 12] and held.tolist() == [4, 6, 7, 3] and int(num_free) == pages - 3 - 1 - 3 - 4
+    for i in (2, 0, 3, 1):
+        drop = torch.zeros(n, dtype=I32, device="cuda")
+        drop[i] = 2**31 - 1 if i == 1 else int(kv_len[i]) - full * page
+        pc.paged_cache_truncate(desc, drop, kv_len, held, table, free, num_free, kv_len, held, num_free, ws)
+        kv_len[i], held[i] = 0, 0
+        stack = free[:int(num_free)].tolist()
+        owned = {p for j in range(n) for p in table[j, :int(held[j])].tolist()}
+        assert len(set(stack)) == len(stack) and not owned & set(stack) and len(owned) + len(stack) == pages
+    assert int(num_free) == pages
+
+
 @pytest.mark.parametrize("pages,on_stack", [(16, 8), (8, 8), (3, 0)])
 def test_more_pages_given_back_than_32_bits_count(pages, on_stack):
     """A request that says it holds 2^31 - 1 pages, most of them given back more than once: as many as the stack has room for go onto it, and nothing is written behind it."""
