@@ -85,36 +85,27 @@ __device__ __forceinline__ double wave_up_to(double x) {
   return x;
 }
 
-// Sums of the granules first .. first + EACH - 1, by one wave.
-template <class T, int EACH, bool INSIDE>
-__device__ __forceinline__ void leave_sums(const VerifyArgs<T>& a, const Weights<T>& weights, int r, int first) {
+// Sum of a granule, by one wave.
+template <class T, bool INSIDE>
+__device__ __forceinline__ void leave_sum(const VerifyArgs<T>& a, const Weights<T>& weights, int r, int granule) {
   const int lane = threadIdx.x & 63;
-  float x[EACH][2][8], y[EACH][2][8];
+  float x[2][8], y[2][8];
 #pragma unroll
-  for (int g = 0; g < EACH; ++g)
+  for (int n = 0; n < 2; ++n) weights.template load<INSIDE>(INSIDE ? granule * kGranule + n * kRun + lane * 8 : min(granule * kGranule + n * kRun + lane * 8, a.vocab), x[n], y[n]);
+  double sum = 0.0;
 #pragma unroll
-    for (int n = 0; n < 2; ++n) weights.template load<INSIDE>(INSIDE ? (first + g) * kGranule + n * kRun + lane * 8 : min((first + g) * kGranule + n * kRun + lane * 8, a.vocab), x[g][n], y[g][n]);
-  double sums[EACH];
+  for (int n = 0; n < 2; ++n) {
+    weights.clear(granule * kGranule + n * kRun + lane * 8, x[n], y[n]);
 #pragma unroll
-  for (int g = 0; g < EACH; ++g) {
-    sums[g] = 0.0;
-#pragma unroll
-    for (int n = 0; n < 2; ++n) {
-      weights.clear((first + g) * kGranule + n * kRun + lane * 8, x[g][n], y[g][n]);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) sums[g] += (double)x[g][n][e] - (double)y[g][n][e];
-    }
+    for (int e = 0; e < 8; ++e) sum += (double)x[n][e] - (double)y[n][e];
   }
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1)
-#pragma unroll
-    for (int g = 0; g < EACH; ++g) sums[g] += __shfl_xor(sums[g], o);
-#pragma unroll
-  for (int g = 0; g < EACH; ++g)
-    if (lane == 0 && first + g < a.granules) a.sums[(int64_t)r * a.granules + first + g] = sums[g];
+  sum = wave_total(sum);
+  if (lane == 0) a.sums[(int64_t)r * a.granules + granule] = sum;
 }
 
-template <class T, int EACH>
+// A wave takes one granule (more only where a launch would have too many threads).  Four at once, so that more loads are under way, was slower but for large batches of bf16 rows that are a multiple of them: one / four, us, 512 requests of 32000 27.2 / 29.6 (float32)
+// and 20.1 / 25.2 (bf16), 900 of 50257 bf16 45 / 53, 256 of 131072 45.0 / 46.5 (float32) and 29.3 / 30.2 (bf16), 100 of 262144 bf16 24.9 / 25.6; 512 and 1000 of 131072 bf16 52.4 / 50.5 and 89.6 / 82.9.
+template <class T>
 __global__ __launch_bounds__(kThreads) void sums_kernel(const VerifyArgs<T> a) {
   __shared__ int kept_by_all;
   const int r = blockIdx.x / a.groups, group = blockIdx.x % a.groups, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -142,11 +133,10 @@ __global__ __launch_bounds__(kThreads) void sums_kernel(const VerifyArgs<T> a) {
   __syncthreads();
   const int kept = kept_by_all;
   const Weights<T> weights = weights_of(a, r, kept, kept < count);
-  // granules of a wave at once, so that their loads are under way together
-  const int first = (group * kWaves + wave) * EACH;
-  if (first >= a.granules) return;
-  if ((first + EACH) * kGranule <= a.vocab) leave_sums<T, EACH, true>(a, weights, r, first);
-  else leave_sums<T, EACH, false>(a, weights, r, first);
+  for (int granule = group * kWaves + wave; granule < a.granules; granule += a.groups * kWaves) {
+    if ((granule + 1) * kGranule <= a.vocab) leave_sum<T, true>(a, weights, r, granule);
+    else leave_sum<T, false>(a, weights, r, granule);
+  }
 }
 
 // One workgroup to a request.
@@ -275,7 +265,7 @@ __global__ __launch_bounds__(kThreads) void choose_kernel(const VerifyArgs<T> a)
 }
 
 int check_sizes(int32_t batch, int32_t max_drafts, int32_t vocab) {
-  if (batch < 0 || max_drafts < 0 || vocab < 1 || batch >= 1 << 23 || (int64_t)batch * vocab >= (int64_t)1 << 36) return CHUNK_ATTN_INVALID_ARG;  // (threads of a launch: below 2^32)
+  if (batch < 0 || max_drafts < 0 || vocab < 1 || batch >= 1 << 23 || (int64_t)batch * vocab >= (int64_t)1 << 36) return CHUNK_ATTN_INVALID_ARG;
   return max_drafts > DRAFT_VERIFY_MAX_DRAFTS || vocab > DRAFT_VERIFY_MAX_VOCAB ? CHUNK_ATTN_UNSUPPORTED : CHUNK_ATTN_OK;
 }
 int count_granules(int32_t vocab) { return (vocab + kGranule - 1) / kGranule; }
@@ -284,12 +274,8 @@ bool aligned(const void* p, uintptr_t to) { return p && ((uintptr_t)p & (to - 1)
 template <class T>
 hipError_t launch(VerifyArgs<T> a, int batch, hipStream_t stream) {
   a.granules = count_granules(a.vocab);
-  // granules to a wave: one, or four where the chip is full with that
-  const bool many = (int64_t)batch * a.granules >= 4 * kCus * 16;
-  a.groups = (a.granules + (many ? 4 : 1) * kWaves - 1) / ((many ? 4 : 1) * kWaves);
-  const dim3 grid((unsigned)((int64_t)batch * a.groups));
-  if (many) hipLaunchKernelGGL((sums_kernel<T, 4>), grid, dim3(kThreads), 0, stream, a);
-  else hipLaunchKernelGGL((sums_kernel<T, 1>), grid, dim3(kThreads), 0, stream, a);
+  a.groups = std::min((a.granules + kWaves - 1) / kWaves, ((1 << 24) - 1) / batch);  // (threads of a launch: below 2^32)
+  hipLaunchKernelGGL((sums_kernel<T>), dim3((unsigned)((int64_t)batch * a.groups)), dim3(kThreads), 0, stream, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((choose_kernel<T>), dim3((unsigned)batch), dim3(kThreads), 0, stream, a);

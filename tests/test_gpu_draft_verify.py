@@ -134,6 +134,26 @@ def test_rows_past_offsets_of_32_bits():
     check(*far, tokens, None, u, last)
 
 
+def test_more_rows_than_a_launch_has_workgroups_for():
+    """5.6 million requests of 8193 tokens (92 GB): three workgroups to each would be more threads than a launch can have.  All weight on one token, or on two."""
+    from paper_2509_21275_amd import draft_verify as dv
+    n, V = (1 << 24) // 3 + 1, 8193
+    if torch.cuda.mem_get_info()[0] < 130e9:
+        pytest.skip("needs 130 GB")
+    first = torch.randint(0, V - 1, (n,), device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))
+    second = torch.where(torch.arange(n, device="cuda") % 2 == 0, V - 1, first)
+    target = torch.zeros((n, 1, V), dtype=BF16, device="cuda")
+    for at in (first, second):
+        target.view(-1)[torch.arange(n, device="cuda") * V + at] = 0.5
+    last = torch.rand(n, device="cuda", generator=torch.Generator(device="cuda").manual_seed(2))
+    accepted, out = torch.full((n,), -9, dtype=I32, device="cuda"), torch.full((n, 1), -9, dtype=I32, device="cuda")
+    none, nothing = torch.zeros((n, 0), dtype=I32, device="cuda"), torch.zeros((n, 0), device="cuda")
+    print("92 GB of probabilities", flush=True)
+    dv.draft_verify(target, None, none, None, nothing, last, accepted, None, out, dv.alloc_workspace(n, 0, V))
+    torch.cuda.synchronize()
+    assert not accepted.any() and torch.equal(out[:, 0].long(), torch.where(last < 0.5, first, second))
+
+
 def test_replayed_graph():
     from paper_2509_21275_amd import draft_verify as dv
     n, K, V = 50, 4, 20000
