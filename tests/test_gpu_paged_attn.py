@@ -105,6 +105,17 @@ def test_against_float64(name, lens, new, heads, kv_heads, dim, page, kind):
     assert torch.equal(o, again) and torch.equal(lse, lse_again)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("lens,new,heads,kv_heads,dim,page", [([9000, 500], [1, 2], 6, 3, 128, 16), ([4000, 1, 2600], [2, 1, 9], 20, 5, 64, 16), ([6000, 0, 3000], [1, 0, 1], 40, 10, 128, 64),
+                                                              ([5000], [3], 12, 12, 96, 20), ([3000, 700], [1, 4], 24, 24, 256, 32), ([300, 40], [1, 2], 600, 600, 64, 16)])
+def test_numbers_of_heads_that_divide_no_power_of_two(lens, new, heads, kv_heads, dim, page, kind):
+    """Shares of a head that are not its part of 512, with blocks that are cut; more heads than 512."""
+    c = Case(lens, new, heads, kv_heads, dim, page, kind)
+    print(heads, kv_heads, dim, page, kind, flush=True)
+    o, lse = c.run()
+    c.check(o, lse)
+
+
 def test_without_lse_into_wider_rows():
     c = Case(LENS, [1] * len(LENS), 8, 2, 128, 16)
     wide = torch.full((c.total, 8 * 128 + 5), 7.0, dtype=BF16, device="cuda")
