@@ -744,9 +744,11 @@ int check_desc(const paged_attn_desc* d) {
     return CHUNK_ATTN_INVALID_ARG;
   return CHUNK_ATTN_OK;
 }
-// Workgroups for each key/value head: two to a compute unit, and no more than there can be shares.
+// Workgroups for each key/value head: as many as two to a compute unit are, and no more than there can be shares.  All shares are equally long and a compute unit holds two (head dimension 64: three), so
+// what is past two to each would begin when the first ones end: rounded down.  Not past half as many heads as that, where it would leave half of the places empty.  Rounded down / up, us, a query head to a
+// key/value head of 128, bf16, 12000 to 134000 keys: 24 heads 291 / 329, 40 heads 254 / 291, 100 heads 283 / 314, 200 heads 312 / 319; 260 heads 430 / 348, 300 heads 570 / 464 (but 400 heads 461 / 484).
 int count_shares(const paged_attn_desc* d) {
-  const int64_t fill = (kMostShares + d->num_kv_heads - 1) / d->num_kv_heads;
+  const int64_t fill = (kMostShares + (d->num_kv_heads > kMostShares / 2 ? d->num_kv_heads - 1 : 0)) / d->num_kv_heads;
   return (int)std::max<int64_t>(1, std::min(fill, most_units(d)));
 }
 int count_subs(const paged_attn_desc* d) {

@@ -188,3 +188,12 @@ def test_division_of_work_in_any_numbers(tmp_path):
     assert r.returncode == 0, r.stderr[-2000:]
     r = subprocess.run([exe], capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and r.stdout.strip() == "ok", r.stdout[-2000:]
+
+
+@pytest.mark.parametrize("heads", [1, 3, 5, 8, 10, 12, 24, 40, 96, 200, 255, 256, 257, 300, 512, 600])
+def test_no_more_workgroups_than_fit_at_once(ca, heads):
+    """Two workgroups to each of 256 compute units: shares of all heads, by the parts that the workspace has room for, are no more, but for more heads than half of that."""
+    from paper_2509_21275_amd import paged_attn as pa
+    size = pa.paged_attn_workspace_bytes(pa.make_desc(heads, heads, 128, 8, 8, 16, 4096, 512, 0.1))
+    shares, rest = divmod(size, 2 * heads * 32 * 130 * 4 + 16)
+    assert rest == 0 and shares == (512 // heads if heads <= 256 else 2 if heads < 512 else 1)
