@@ -13,7 +13,8 @@
  *   kv_len   : [num_seqs] int32;  q_start: [num_seqs + 1] int32, in increasing order from 0
  * What kv_len, q_start and table hold is not known to the host, so nothing in them is an error: lengths count as at most max_pages * page_size, rows outside [0, total_q) as not there (n counts the
  * others), and tokens on a page whose number is none, which no row sees, as masked; a row that starts which do not increase give to several sequences holds what any of them leaves there.
- * What lies in the cache where a row sees nothing (other rows of a page, tokens behind it) does not reach it, whatever it is.
+ * What lies in the cache where a row sees nothing (other rows of a page, tokens behind it) does not reach it, whatever it is; a value that is not finite in a key that it sees leaves its dimension not
+ * finite (an infinity may become NaN).
  *
  * Any number of new tokens is right; many of them (hundreds) read a sequence's keys and values once for every 128 rows of a key/value head (32 for head dimension 256), and are
  * faster with chunk_attn_fwd.  Scores, softmax and sums are float32; weights go into the products with values as two bf16 terms, with e4m3 values as one float16 term; a result is rounded once.

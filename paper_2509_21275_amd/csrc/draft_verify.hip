@@ -3,7 +3,7 @@
 // Bound by memory: one row of the target's probabilities, and one of the draft's where a token is rejected, of each request.  The sum of weights has to be known before the place
 // can be found where the running sum passes a share of it, so: sums_kernel finds the row and leaves the sum of every kGranule weights, taken by one wave; choose_kernel sums these up, finds the granule
 // and reads it again.  A weight is there or not by a comparison in float32, which is exact; sums are float64: differences that matter are exact, and sums of 10^5 weights are off by 10^-15 of them or so.
-// Measured: 256 requests, 131072 bf16 probabilities (134 MB) 29.7 us, of which the choice 6; 8 of 32000 4.3 + 5.6.  With both in one kernel, a workgroup of 16
+// Measured: 256 requests, 131072 bf16 probabilities (134 MB) 29.3 us, of which the choice 6; 8 of 32000 4.4 + 5.6.  With both in one kernel, a workgroup of 16
 // waves to a request: 27.6 us there, and 10.5 against 11.4 for one request of 32000, but 36 against 28 for 128 requests of 131072 float32, 66 against 49 for 300, 21 against 12 for one.
 #include <hip/hip_runtime.h>
 

@@ -14,7 +14,7 @@
 // Bound by memory: one token of 32/8 heads takes four operations for each byte of the cache, 32 rows 32.  Weights go into the product with V as two bf16 terms (one would leave the output with
 // 2.4e-3 of itself in place of 1.7e-3), for e4m3 values, which float16 has, as one float16 term (2^-11).  Measured: 64 sequences as above 194 us, 5.4 TB/s; 8 of 32768 keys 197, 5.45; 8 of 131072
 // keys of 8 bits 369, 5.8; one of 131072 keys of 8 bits with 40 rows 74, 3.6 TB/s: there vector units (48 % of the time) and matrix units (27 %) take turns.  What is short: a launch with one block of
-// 60 keys takes 8 us, of which 2 until the first loads, 2.5 for them, 1 for the tile, 2 to put results together; cutting adds a launch of 4 us.
+// 60 keys takes 8 us, of which 2 until the first loads, 2.5 for them, 1 for the tile, 2 to put results together; cutting adds a launch of 4.4 us.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

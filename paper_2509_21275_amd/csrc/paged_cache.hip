@@ -15,8 +15,7 @@ namespace {
 // ---- tables ----
 // Requests in order, pages in order: two running sums, of rows and of pages.  One workgroup of 1024 threads takes them, each thread over neighbouring requests; what follows
 // from the sums (slots of rows, entries of the table, entries of the stack) goes row by row and page by page.  Few requests with few rows: the same workgroup does that too, with the sums in LDS, in which
-// each row finds its request by halving (one launch, 3.4 us; a million pages
-// that are given back at once take it 0.9 ms, less than the attention of one layer took to read them).  Else the sums go to the workspace and a second launch fills the chip.
+// each row finds its request by halving (one launch, 3.7 us).  Else the sums go to the workspace and a second launch fills the chip.
 // Bound by latency: 4096 requests with 48000 rows, 0.4 MB, take 6 and 5 us, each a chain of four or five loads that depend on each other; with the requests read again for each sum, 64-bit sums, a store for
 // each number, and rows that looked for their request among all in memory, it was 16 and 8.
 constexpr int kScanThreads = 1024;
@@ -331,6 +330,9 @@ int run_tables(const paged_cache_desc* d, TableArgs a, void* workspace, size_t w
   a.num_pages = d->num_pages;
   a.sums = (int32_t*)workspace;
   a.by_page = Divide(d->page_size);
+  // One launch / two, us, in a graph.  Extensions: 64 requests with 64 rows 3.2 / 5.9, 1024 with 1024 4.3 / 8.2, 256 with 4096 8.9 / 9.9, 1024 with 4096 7.2 / 8.0; 64 with 4096 8.1 / 7.8, 64 with 16384
+  // 18.6 / 8.4.  Truncations, of which the host does not know how many pages they give back: rejected drafts and some requests' ends, 64 requests with 64 pages 4.5 / 5.2, 256 with 256 4.7 / 6.5, 1024 with 1024
+  // 6.3 / 6.7; everything at once, 256 with 4096 6.9 / 6.5, 1024 with 65536 61 / 6.7, with 2^20 1012 / 9.1, which is seldom, and is left to cost that.
   if (a.n <= kScanThreads && a.max_rows <= kInOne) {
     hipLaunchKernelGGL((tables_kernel<EXTEND, true, 1>), dim3(1), dim3(kScanThreads), 0, stream, a);
   } else {
