@@ -77,7 +77,7 @@ int paged_cache_truncate(const paged_cache_desc* desc, const int32_t* drop, cons
  * Rows whose slot is negative or >= num_pages * page_size are skipped; rows of the cache that no slot names stay as they are.  Where two rows have the same slot, what is left there is of
  * either, piece by piece.  cache_type PAGED_CACHE_E4M3: k_scale, v_scale [num_kv_heads] float32, > 0; the float32 quotient of the value and the scale is rounded to the nearest (ties to
  * even), what is past 448 to 448; signs are kept, of zeros too, and NaN stays NaN.  PAGED_CACHE_BF16: copied, k_scale and v_scale are not read and may be null.
- * head_dim 64, 96, 128 or 256, else CHUNK_ATTN_UNSUPPORTED; rows >= 0, rows * num_kv_heads * head_dim < 2^40.  The cache may overlap nothing else.
+ * head_dim 64, 96, 128 or 256, else CHUNK_ATTN_UNSUPPORTED; rows >= 0, rows * num_kv_heads * head_dim <= 2^35 - 2^11.  The cache may overlap nothing else.
  */
 int paged_cache_write(int32_t rows, int32_t num_kv_heads, int32_t head_dim, int32_t page_size, int32_t num_pages, int32_t cache_type, const void* k, int64_t k_stride,
                       const void* v, int64_t v_stride, const int64_t* slots, const float* k_scale, const float* v_scale, void* k_cache, void* v_cache, void* hip_stream);

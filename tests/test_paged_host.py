@@ -81,6 +81,17 @@ def test_write_refusals(ca):
         pc.paged_cache_write(None, None, None, None, None)
 
 
+def test_write_refuses_more_than_a_launch_has_threads_for(ca):
+    """A thread to eight elements, and below 2^32 threads: 2^35 - 2^11 elements are the most, as the header says."""
+    from paper_2509_21275_amd import paged_cache as pc
+    pc._bind()
+    text = open(os.path.join(ROOT, "include", "paged_cache.h")).read()
+    assert "rows * num_kv_heads * head_dim <= 2^35 - 2^11" in text
+    for rows, heads, dim in ((2**28, 1, 128), (2**28 - 15, 2, 64), (2**20, 256, 128), (2**21 - 1, 257, 64)):
+        assert rows * heads * dim > 2**35 - 2**11
+        assert ca._lib.paged_cache_write(rows, heads, dim, 16, 1000, 0, P, heads * dim, P, heads * dim, P, None, None, P, P, None) == ca.INVALID_ARG
+
+
 def test_attention_refusals(ca):
     from paper_2509_21275_amd import paged_attn as pa
     pa._bind()
